@@ -48,7 +48,9 @@ typedef enum {
     DBS_ERR_STATE = 5         /* object used in a wrong state */
 } dbs_status;
 
-typedef enum { DBS_F32 = 0, DBS_F16 = 1, DBS_PATTERN = 2 } dbs_dtype;
+/* DBS_BF16 is an element type of the dense layer operators only: matrices
+ * refuse it. */
+typedef enum { DBS_F32 = 0, DBS_F16 = 1, DBS_PATTERN = 2, DBS_BF16 = 3 } dbs_dtype;
 typedef enum { DBS_PLUS_TIMES = 0, DBS_OR_AND = 1 } dbs_semiring;
 typedef enum { DBS_PATH_AUTO = 0, DBS_PATH_PUSH = 1, DBS_PATH_PULL = 2 } dbs_path;
 
@@ -491,6 +493,110 @@ void dbs_basic_destroy(dbs_basic_matrix *B);
  * in time (the dense-x scratch is shared).                                 */
 dbs_status dbs_basic_spmspv(dbs_basic_matrix *B, dbs_path path, int32_t x_nnz, const int32_t *d_x_idx,
                             const float *d_x_val, float *d_y, void *stream);
+
+/* ---------------------------------------------------------------------- */
+/* Dense layer operators: the linear and gated feed-forward layers that    */
+/* stand beside the pruned ones (Sec. 4.3 decodes one activation at a time */
+/* against pruned weights; prompts, training and the layers left dense     */
+/* need these), their backward passes, and 8-bit activation checkpoints.   */
+/* ---------------------------------------------------------------------- */
+/* All tensors are 2-D, row-major with unit column stride and `ld...`
+ * elements from row to row (at least the number of columns; ignored for one
+ * row), aligned to their elements; any larger alignment or size is served.
+ * Values are DBS_F16 or DBS_BF16, the same for all tensors of a call.  Sums
+ * are taken in 32 bits and rounded once at the end; the products dz, dg and du
+ * below are rounded to the element type before they are multiplied again.
+ * Sizes are at most 2^30.  Outputs must not overlap inputs, except that y may
+ * be the residual itself.  NaN and infinities propagate as in the formulas. */
+
+/* A layer context holds the workspace of one stream: calls on it run in
+ * stream order and are asynchronous; it is used by one host thread at a time.
+ * Calls allocate nothing and may be captured into a graph.                  */
+typedef struct dbs_layer dbs_layer;
+dbs_status dbs_layer_create(void *stream, dbs_layer **out);
+dbs_status dbs_layer_set_stream(dbs_layer *L, void *stream);
+void dbs_layer_destroy(dbs_layer *L);
+
+/* act(z): z; max(z, 0); z / (1 + e^-z); z (1 + erf(z / sqrt 2)) / 2;
+ * z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2                         */
+typedef enum {
+    DBS_ACT_NONE = 0,
+    DBS_ACT_RELU = 1,
+    DBS_ACT_SILU = 2,
+    DBS_ACT_GELU = 3,
+    DBS_ACT_GELU_TANH = 4
+} dbs_act;
+
+/* Checkpoint: rows x cols codes (int8, contiguous) and one exponent byte for
+ * each group of DBS_CK_GROUP columns of a row (rows x ceil(cols / 32),
+ * contiguous).  With a the largest finite magnitude of a group and e the least
+ * integer with a <= 127 * 2^e (and e >= -127; DBS_F16: -24), the exponent byte
+ * is e + 127 and a code the whole number nearest to v * 2^-e, ties to even;
+ * -128 stands for a value that is not finite.  A code's value is code * 2^e,
+ * limited to the type's largest finite number; -128 gives NaN.              */
+#define DBS_CK_GROUP 32
+
+/* What a backward pass reads: 16-bit values, or a checkpoint (d_values NULL). */
+typedef struct {
+    const void *d_values;
+    int64_t ld;
+    const int8_t *d_codes;
+    const uint8_t *d_exps;
+} dbs_held;
+
+/* Where a forward pass keeps a projection, rounded to the element type: as it
+ * is, or as a checkpoint of the rounded values (d_values NULL).             */
+typedef struct {
+    void *d_values;
+    int64_t ld;
+    int8_t *d_codes;
+    uint8_t *d_exps;
+} dbs_keep;
+
+/* y = act(x w^T + bias) + residual:  x [tokens, n_in], w [n_out, n_in], bias
+ * [n_out] or NULL, residual [tokens, n_out] or NULL, y [tokens, n_out];
+ * pre (NULL allowed) receives x w^T + bias for the backward pass.            */
+dbs_status dbs_linear(dbs_layer *L, dbs_dtype dt, int32_t tokens, int32_t n_in, int32_t n_out, const void *d_x,
+                      int64_t ldx, const void *d_w, int64_t ldw, const void *d_bias, dbs_act act,
+                      const void *d_residual, int64_t ldr, void *d_y, int64_t ldy, const dbs_keep *pre);
+
+/* h = act(x w_gate^T) * (x w_up^T):  w_gate, w_up [n_out, n_in], h [tokens,
+ * n_out]; gate and up (both or neither, in one form) receive the projections.
+ * With DBS_ACT_RELU the zeros of h are entries that dbs_spmspv_dense skips.  */
+dbs_status dbs_gated(dbs_layer *L, dbs_dtype dt, int32_t tokens, int32_t n_in, int32_t n_out, const void *d_x,
+                     int64_t ldx, const void *d_w_gate, int64_t ldwg, const void *d_w_up, int64_t ldwu, dbs_act act,
+                     void *d_h, int64_t ldh, const dbs_keep *gate, const dbs_keep *up);
+
+/* Bytes of device memory that a backward call needs for its own use (what it
+ * is given must be aligned to 256 bytes, and is free again when the call is
+ * done): gated, act, the sizes, whether x is held as a checkpoint (and dw is
+ * wanted), whether db is wanted.                                             */
+dbs_status dbs_backward_work(const dbs_layer *L, int gated, dbs_act act, int32_t tokens, int32_t n_in, int32_t n_out,
+                             int x_codes, int want_db, size_t *bytes);
+
+/* Gradients of dbs_linear, with dz = dy * act'(pre):  dx = dz w, dw = dz^T x,
+ * db = the sum of dz over the tokens (the residual's gradient is dy itself).
+ * Outputs may be NULL; pre may be NULL with DBS_ACT_NONE, x without dw, w
+ * without dx.  act'(0) of DBS_ACT_RELU is 0.                                 */
+dbs_status dbs_linear_backward(dbs_layer *L, dbs_dtype dt, int32_t tokens, int32_t n_in, int32_t n_out,
+                               const void *d_dy, int64_t lddy, const dbs_held *x, const void *d_w, int64_t ldw,
+                               const dbs_held *pre, dbs_act act, void *d_dx, int64_t lddx, void *d_dw, int64_t lddw,
+                               void *d_db, void *d_work, size_t work_bytes);
+
+/* Gradients of dbs_gated, with dg = dh * up * act'(gate), du = dh * act(gate):
+ * dx = dg w_gate + du w_up, dw_gate = dg^T x, dw_up = du^T x (both or neither
+ * of the last two; dx may be NULL).                                          */
+dbs_status dbs_gated_backward(dbs_layer *L, dbs_dtype dt, int32_t tokens, int32_t n_in, int32_t n_out,
+                              const void *d_dh, int64_t lddh, const dbs_held *x, const void *d_w_gate, int64_t ldwg,
+                              const void *d_w_up, int64_t ldwu, const dbs_held *gate, const dbs_held *up, dbs_act act,
+                              void *d_dx, int64_t lddx, void *d_dw_gate, int64_t lddwg, void *d_dw_up, int64_t lddwu,
+                              void *d_work, size_t work_bytes);
+
+/* A checkpoint of x [rows, cols], and the values of one.                     */
+dbs_status dbs_pack(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t cols, const void *d_x, int64_t ldx,
+                    int8_t *d_codes, uint8_t *d_exps);
+dbs_status dbs_unpack(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t cols, const int8_t *d_codes,
+                      const uint8_t *d_exps, void *d_y, int64_t ldy);
 
 /* ---------------------------------------------------------------------- */
 /* Measurement hooks.                                                     */

@@ -11,6 +11,9 @@ current stream only.
     y_idx, y_val = ctx.spmspv(A, x_idx, x_val)                # torch CUDA tensors
     y16 = ctx.spmspv_dense(A, a16)                            # decode layer
     level, parent = ctx.bfs(A, source)
+
+The dense layers beside the pruned ones (linear, gated, their gradients, 8-bit
+activation checkpoints) run on a ``LayerContext`` (``layer.py``).
 """
 from __future__ import annotations
 
@@ -21,9 +24,10 @@ import numpy as np
 from . import _lib
 from ._lib import (BLOCK_TYPE_NAMES, DBS_F16, DBS_F32, DBS_OR_AND, DBS_PATH_AUTO, DBS_PATH_PULL,
                    DBS_PATH_PUSH, DBS_PATTERN, DBS_PLUS_TIMES, DbsError, check)
+from .layer import Checkpoint, LayerContext
 
 __all__ = ["HostMatrix", "Matrix", "Context", "BasicMatrix", "DbsError", "default_opts", "storage_model",
-           "spmspv_noalloc",
+           "spmspv_noalloc", "LayerContext", "Checkpoint",
            "DBS_F32", "DBS_F16", "DBS_PATTERN", "PATHS"]
 
 PATHS = {"auto": DBS_PATH_AUTO, "push": DBS_PATH_PUSH, "pull": DBS_PATH_PULL}

@@ -12,7 +12,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdbspmspv.so")
 
 DBS_OK, DBS_ERR_ARG, DBS_ERR_ALLOC, DBS_ERR_DEVICE, DBS_ERR_UNSUPPORTED, DBS_ERR_STATE = range(6)
-DBS_F32, DBS_F16, DBS_PATTERN = 0, 1, 2
+DBS_F32, DBS_F16, DBS_PATTERN, DBS_BF16 = 0, 1, 2, 3
+DBS_ACT_NONE, DBS_ACT_RELU, DBS_ACT_SILU, DBS_ACT_GELU, DBS_ACT_GELU_TANH = range(5)
+DBS_CK_GROUP = 32
 DBS_PLUS_TIMES, DBS_OR_AND = 0, 1
 DBS_PATH_AUTO, DBS_PATH_PUSH, DBS_PATH_PULL = 0, 1, 2
 DBS_BLK_COO, DBS_BLK_DENSE, DBS_BLK_FCSR, DBS_BLK_FCSC, DBS_BLK_CSR = range(5)
@@ -29,6 +31,8 @@ EXPORTED = [
     "dbs_ctx_read_timing", "dbs_last_error", "dbs_version", "dbs_basic_build", "dbs_basic_destroy",
     "dbs_basic_spmspv", "dbs_matrix_build_dense", "dbs_matrix_layout_get", "dbs_matrix_download",
     "dbs_spmspv_noalloc", "dbs_ctx_set_single_launch",
+    "dbs_layer_create", "dbs_layer_set_stream", "dbs_layer_destroy", "dbs_linear", "dbs_gated", "dbs_backward_work",
+    "dbs_linear_backward", "dbs_gated_backward", "dbs_pack", "dbs_unpack",
 ]
 DBS_NOALLOC_MAX_DIM = 1 << 20
 
@@ -83,6 +87,12 @@ class BfsStats(ctypes.Structure):
 
 class Timing(ctypes.Structure):
     _fields_ = [("ms", ctypes.c_double * 7), ("launches", ctypes.c_int64 * 7)]
+
+
+class Held(ctypes.Structure):
+    """dbs_held and dbs_keep."""
+    _fields_ = [("d_values", ctypes.c_void_p), ("ld", ctypes.c_int64), ("d_codes", ctypes.c_void_p),
+                ("d_exps", ctypes.c_void_p)]
 
 
 class DbsError(RuntimeError):
@@ -141,6 +151,21 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "dbs_basic_build": (ctypes.c_int, [i32, i32, i64, vp, vp, vp, P(vp)]),
         "dbs_basic_destroy": (None, [vp]),
         "dbs_basic_spmspv": (ctypes.c_int, [vp, ctypes.c_int, i32, vp, vp, vp, vp]),
+        "dbs_layer_create": (ctypes.c_int, [vp, P(vp)]),
+        "dbs_layer_set_stream": (ctypes.c_int, [vp, vp]),
+        "dbs_layer_destroy": (None, [vp]),
+        "dbs_linear": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, vp, i64, vp, i64, vp, ctypes.c_int, vp, i64, vp, i64,
+                                      P(Held)]),
+        "dbs_gated": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, vp, i64, vp, i64, vp, i64, ctypes.c_int, vp, i64,
+                                     P(Held), P(Held)]),
+        "dbs_backward_work": (ctypes.c_int, [vp, ctypes.c_int, ctypes.c_int, i32, i32, i32, ctypes.c_int, ctypes.c_int,
+                                             P(ctypes.c_size_t)]),
+        "dbs_linear_backward": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, vp, i64, P(Held), vp, i64, P(Held),
+                                               ctypes.c_int, vp, i64, vp, i64, vp, vp, ctypes.c_size_t]),
+        "dbs_gated_backward": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, vp, i64, P(Held), vp, i64, vp, i64, P(Held),
+                                              P(Held), ctypes.c_int, vp, i64, vp, i64, vp, i64, vp, ctypes.c_size_t]),
+        "dbs_pack": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, vp, i64, vp, vp]),
+        "dbs_unpack": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, vp, vp, vp, i64]),
         "dbs_last_error": (ctypes.c_char_p, []),
         "dbs_version": (ctypes.c_char_p, []),
     }

@@ -1,0 +1,212 @@
+// Shared parts of the dense layer operators: element types, activations, the
+// 8-bit checkpoint code, kernel arguments and launchers.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/dbspmspv.h"
+
+namespace dbs {
+
+typedef float f4_t __attribute__((ext_vector_type(4)));
+typedef float f2_t __attribute__((ext_vector_type(2)));
+
+// The two element types.  V8 is a 16-byte chunk of them, and mma() one
+// 16x16x32 step on the matrix cores: lane l gives row l % 16 of a and column
+// l % 16 of b, elements 8 (l / 16) .. + 7 of the sum, and holds rows
+// 4 (l / 16) .. + 3 of column l % 16 of the 32-bit result.
+struct Bf16 {
+    typedef __bf16 T;
+    typedef __bf16 V8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 V4 __attribute__((ext_vector_type(4)));
+    static constexpr float MAX = 3.38953138925153547590470800371487867e38f;
+    static constexpr int LEAST_EXP = -127;
+    __device__ static __forceinline__ f4_t mma(V8 a, V8 b, f4_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+struct Fp16 {
+    typedef _Float16 T;
+    typedef _Float16 V8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 V4 __attribute__((ext_vector_type(4)));
+    static constexpr float MAX = 65504.f;
+    static constexpr int LEAST_EXP = -24;
+    __device__ static __forceinline__ f4_t mma(V8 a, V8 b, f4_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+};
+
+// ---------------------------------------------------------------------------
+// activations
+// ---------------------------------------------------------------------------
+// act(z).  SiLU and the tanh form of GELU are both z times a logistic of
+// a z + b z^3 (1 + tanh(q) = 2 logistic(2 q)), which also keeps the relative
+// precision of the small values left of zero; GELU itself takes erf.
+struct Act {
+    int32_t kind;
+    float a, b;  // of the logistic
+    static Act of(dbs_act k)
+    {
+        const float c = 1.5957691216057308f;  // 2 sqrt(2 / pi)
+        return Act{(int32_t)k, k == DBS_ACT_GELU_TANH ? c : 1.f, k == DBS_ACT_GELU_TANH ? c * 0.044715f : 0.f};
+    }
+};
+__device__ __forceinline__ float logistic(float q) { return __builtin_amdgcn_rcpf(1.f + __expf(-q)); }
+
+__device__ __forceinline__ float act_value(Act f, float z)
+{
+    if (f.kind == DBS_ACT_NONE) return z;
+    if (f.kind == DBS_ACT_RELU) return z < 0.f ? 0.f : z;
+    if (f.kind == DBS_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    return z * logistic(z * (f.a + f.b * z * z));
+}
+// act(z) and act'(z).
+__device__ __forceinline__ float act_slope(Act f, float z, float &value)
+{
+    if (f.kind == DBS_ACT_NONE) {
+        value = z;
+        return 1.f;
+    }
+    if (f.kind == DBS_ACT_RELU) {
+        value = z < 0.f ? 0.f : z;
+        return z > 0.f ? 1.f : 0.f;
+    }
+    if (f.kind == DBS_ACT_GELU) {
+        const float c = 0.5f * (1.f + erff(z * 0.70710678118654752f));
+        value = z * c;
+        return c + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+    }
+    const float s = logistic(z * (f.a + f.b * z * z));
+    value = z * s;
+    // (where s is 0 or 1 the second term is 0, also where z^3 overflows)
+    const float d = s * (1.f - s);
+    return s + (d == 0.f ? 0.f : z * d * (f.a + 3.f * f.b * z * z));
+}
+
+// ---------------------------------------------------------------------------
+// 8-bit checkpoints
+// ---------------------------------------------------------------------------
+// A group of CK_GROUP columns of a row shares the exponent e, the least with
+// a <= 127 * 2^e for the largest finite magnitude a; a value is the whole
+// number nearest to v * 2^-e (ties to even), and -128 stands for a value that
+// is not finite.  A scale that is a power of two costs up to one of the seven
+// bits against a / 127, but every code * 2^e is a number of the 16-bit type,
+// so what the backward pass multiplies is what the checkpoint holds, with no
+// second rounding.
+constexpr int CK_GROUP = 32;
+constexpr int CK_BIAS = 127;
+
+// The finite magnitude of v, 0 if it is not finite.
+__device__ __forceinline__ float ck_mag(float v)
+{
+    const float a = __builtin_fabsf(v);
+    return a <= 3.402823466e38f ? a : 0.f;
+}
+// e of a group with largest magnitude a.
+template <class X> __device__ __forceinline__ int ck_exp(float a)
+{
+    const int k = __builtin_amdgcn_frexp_expf(a);         // a = m 2^k, m in [1/2, 1)
+    const float m = __builtin_amdgcn_frexp_mantf(a);
+    const int e = m <= 127.f / 128.f ? k - 7 : k - 6;
+    return a == 0.f || e < X::LEAST_EXP ? X::LEAST_EXP : e;
+}
+__device__ __forceinline__ int ck_code(float v, int e)
+{
+    const float c = __builtin_rintf(__builtin_amdgcn_ldexpf(v, -e));
+    return __builtin_fabsf(v) <= 3.402823466e38f ? (int)c : -128;
+}
+// The largest group magnitudes reach 64 * 2^e = 2^(e + 6) beyond the type's
+// largest number: such values come back as that number.
+template <class X> __device__ __forceinline__ float ck_value(int code, int e)
+{
+    const float v = __builtin_amdgcn_ldexpf((float)code, e);
+    const float w = __builtin_fminf(__builtin_fmaxf(v, -X::MAX), X::MAX);
+    return code == -128 ? __builtin_nanf("") : w;
+}
+
+// ---------------------------------------------------------------------------
+// kernel arguments
+// ---------------------------------------------------------------------------
+// Where an epilogue keeps 16-bit roundings of its sums: as they are, or as a
+// checkpoint (rows of `cols` codes, contiguous).
+struct SaveTo {
+    void *full;
+    int64_t ld;
+    int8_t *codes;
+    uint8_t *exps;
+    int32_t vec;  // 16-byte stores are aligned
+};
+// What a backward pass reads: 16-bit values, or a checkpoint.
+struct HeldIn {
+    const void *full;
+    int64_t ld;
+    const int8_t *codes;
+    const uint8_t *exps;
+};
+
+enum GemmKind { G_LINEAR, G_GATED, G_DX, G_DW };
+
+// One product: Y[q][p] = sum over k of Q[q][k] P[p][k], Y row-major with p
+// along its rows.
+//   G_LINEAR  P = w, Q = x; epilogue act(. + bias) + residual
+//   G_GATED   P = the rows of w_gate and w_up in turns, Q = x; act(gate) * up
+//   G_DX      Q = dz, P[p][k] = w[k][p]; the sum runs over `segs` pairs
+//   G_DW      Q[q][k] = dz[k][q], P[p][k] = x[k][p], k a token; `batch` pairs
+struct GemmArgs {
+    const void *p[2], *q[2];
+    int64_t ldp[2], ldq[2];
+    int32_t pn, qn, kn;      // sizes; pn of one matrix, kn of one pair
+    int32_t segs, batch;
+    void *y[2];
+    int64_t ldy[2];
+    const void *bias, *res;
+    int64_t ldr;
+    Act act;
+    SaveTo save[2];
+    int32_t vec;             // y and res take 16-byte (G_DX, G_DW: 8-byte) accesses
+    // filled by the launcher
+    int32_t tp, tq, splits;
+    float *part;             // splits' sums
+    int32_t *done;           // a word per tile, zero between calls
+    const void *zeros;       // 16 bytes of zeros
+};
+
+// Workspace of a layer context.
+struct LayerWork {
+    float *part;
+    size_t part_bytes;
+    int32_t *done;
+    int32_t ndone;
+    const void *zeros;
+    int32_t cus;
+};
+
+hipError_t launch_gemm(const LayerWork &w, bool bf16, GemmKind kind, GemmArgs a, hipStream_t s);
+
+// Activation gradients: dz = dy * act'(pre) or, gated, dz = dy * up * act'(gate)
+// and du = dy * act(gate), rounded to the element type, rows of `ldz` elements
+// with zeros behind the last column; sums of the columns of the unrounded dz.
+struct SlopeArgs {
+    const void *dy;
+    int64_t lddy;
+    HeldIn pre, up;
+    int32_t rows, cols;
+    Act act;
+    void *dz, *du;      // dz NULL: only the sums
+    int64_t ldz;
+    float *sums;        // NULL, or row_blocks x cols
+    void *db;
+    int32_t row_blocks; // workgroups along the rows
+};
+int32_t slope_row_blocks(int32_t rows, int32_t cols, int32_t cus);
+hipError_t launch_slope(bool bf16, bool gated, const SlopeArgs &a, hipStream_t s);
+
+hipError_t launch_pack(bool bf16, const void *x, int64_t ldx, int32_t rows, int32_t cols, int8_t *codes, uint8_t *exps,
+                       int32_t cus, hipStream_t s);
+hipError_t launch_unpack(bool bf16, const int8_t *codes, const uint8_t *exps, int32_t rows, int32_t cols, void *y,
+                         int64_t ldy, int32_t cus, hipStream_t s);
+
+}  // namespace dbs
