@@ -20,7 +20,7 @@ namespace {
 dbs_status layer_hip_fail(hipError_t e, const char *what)
 {
     (void)hipGetLastError();  // (or the next launch reports it)
-    return dbs_fail(e == hipErrorOutOfMemory ? DBS_ERR_ALLOC : DBS_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
+    return dbs_fail(e == hipErrorOutOfMemory ? DBS_ERR_ALLOC : e == hipErrorInvalidConfiguration ? DBS_ERR_UNSUPPORTED : DBS_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 
 #define LAYER_TRY(expr, what)                              \
@@ -29,8 +29,7 @@ dbs_status layer_hip_fail(hipError_t e, const char *what)
         if (e_ != hipSuccess) return layer_hip_fail(e_, what); \
     } while (0)
 
-constexpr size_t PART_BYTES = (size_t)64 << 20;  // sums of split tiles
-constexpr int32_t NDONE = 1 << 14;               // split tiles
+constexpr size_t PART_BYTES = (size_t)128 << 20;  // sums of split tiles
 constexpr int32_t MAX_DIM = 1 << 30;
 
 bool dense_type(dbs_dtype t) { return t == DBS_F16 || t == DBS_BF16; }
@@ -142,18 +141,16 @@ dbs_status dbs_layer_create(void *stream, dbs_layer **out)
         return dbs_fail(DBS_ERR_DEVICE, "dbs_layer_create: this build runs on gfx950, the device is %s", prop.gcnArchName);
     dbs_layer *L = new (std::nothrow) dbs_layer();
     if (!L) return dbs_fail(DBS_ERR_ALLOC, "dbs_layer_create: host allocation");
-    const size_t done = (size_t)NDONE * 4, zeros = 256;
-    hipError_t e = hipMalloc(&L->mem, done + zeros + PART_BYTES);
-    if (e == hipSuccess) e = hipMemset(L->mem, 0, done + zeros);
+    const size_t zeros = 256;
+    hipError_t e = hipMalloc(&L->mem, zeros + PART_BYTES);
+    if (e == hipSuccess) e = hipMemset(L->mem, 0, zeros);
     if (e == hipSuccess) e = hipDeviceGetAttribute(&L->w.cus, hipDeviceAttributeMultiprocessorCount, dev);
     if (e != hipSuccess) {
         dbs_layer_destroy(L);
         return layer_hip_fail(e, "dbs_layer_create");
     }
-    L->w.done = (int32_t *)L->mem;
-    L->w.ndone = NDONE;
-    L->w.zeros = (uint8_t *)L->mem + done;
-    L->w.part = (float *)((uint8_t *)L->mem + done + zeros);
+    L->w.zeros = L->mem;
+    L->w.part = (float *)((uint8_t *)L->mem + zeros);
     L->w.part_bytes = PART_BYTES;
     L->stream = (hipStream_t)stream;
     *out = L;
@@ -235,7 +232,7 @@ dbs_status dbs_backward_work(const dbs_layer *L, int gated, dbs_act act, int32_t
 // The products that both backward passes end in, dz (and du) given.
 static dbs_status gradients(dbs_layer *L, const char *fn, dbs_dtype dt, int32_t t, int32_t n_in, int32_t n_out, int n,
                             const void *const dz[2], int64_t ldz, const dbs_held *x, const BackwardWork &b,
-                            const void *const w[2], const int64_t ldw[2], void *d_dx, int64_t lddx, void *const dw[2],
+                            bool own_dz, const void *const w[2], const int64_t ldw[2], void *d_dx, int64_t lddx, void *const dw[2],
                             const int64_t lddw[2])
 {
     const bool bf = dt == DBS_BF16;
@@ -244,7 +241,7 @@ static dbs_status gradients(dbs_layer *L, const char *fn, dbs_dtype dt, int32_t 
         for (int i = 0; i < n; ++i) a.p[i] = w[i], a.ldp[i] = ldw[i], a.q[i] = dz[i], a.ldq[i] = ldz;
         a.pn = n_in, a.qn = t, a.kn = n_out, a.segs = n, a.batch = 1;
         a.y[0] = d_dx, a.ldy[0] = lddx;
-        a.vec = aligned(d_dx, lddx, 8);
+        a.vec = aligned(d_dx, lddx, 8), a.q_padded = own_dz;
         LAYER_TRY(launch_gemm(L->w, bf, G_DX, a, L->stream), fn);
     }
     if (dw[0]) {
@@ -260,7 +257,7 @@ static dbs_status gradients(dbs_layer *L, const char *fn, dbs_dtype dt, int32_t 
             a.q[i] = dz[i], a.ldq[i] = ldz, a.y[i] = dw[i], a.ldy[i] = lddw[i];
             a.vec = a.vec && aligned(dw[i], lddw[i], 8);
         }
-        a.p[0] = xv, a.ldp[0] = ldx;
+        a.p[0] = xv, a.ldp[0] = ldx, a.p_padded = b.x != nullptr, a.q_padded = own_dz;
         a.pn = n_in, a.qn = n_out, a.kn = t, a.segs = 1, a.batch = n;
         LAYER_TRY(launch_gemm(L->w, bf, G_DW, a, L->stream), fn);
     }
@@ -299,7 +296,7 @@ dbs_status dbs_linear_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_
     const void *dz[2] = {slope ? b.dz : d_dy, nullptr}, *w[2] = {d_w, nullptr};
     void *dw[2] = {d_dw, nullptr};
     const int64_t ldws[2] = {ldw, 0}, lddws[2] = {lddw, 0};
-    return gradients(L, fn, dt, t, n_in, n_out, 1, dz, slope ? b.ldz : lddy, x, b, w, ldws, d_dx, lddx, dw, lddws);
+    return gradients(L, fn, dt, t, n_in, n_out, 1, dz, slope ? b.ldz : lddy, x, b, slope, w, ldws, d_dx, lddx, dw, lddws);
 }
 
 dbs_status dbs_gated_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_in, int32_t n_out, const void *d_dh,
@@ -337,7 +334,7 @@ dbs_status dbs_gated_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_i
     const void *dz[2] = {b.dz, b.du}, *w[2] = {d_wg, d_wu};
     void *dw[2] = {d_dwg, d_dwu};
     const int64_t ldw[2] = {ldwg, ldwu}, lddw[2] = {lddwg, lddwu};
-    return gradients(L, fn, dt, t, n_in, n_out, 2, dz, b.ldz, x, b, w, ldw, d_dx, lddx, dw, lddw);
+    return gradients(L, fn, dt, t, n_in, n_out, 2, dz, b.ldz, x, b, true, w, ldw, d_dx, lddx, dw, lddw);
 }
 
 dbs_status dbs_pack(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t cols, const void *d_x, int64_t ldx, int8_t *d_codes,

@@ -56,12 +56,20 @@ struct Act {
 };
 __device__ __forceinline__ float logistic(float q) { return __builtin_amdgcn_rcpf(1.f + __expf(-q)); }
 
-__device__ __forceinline__ float act_value(Act f, float z)
+// v = act(v) for N values
+template <int N> __device__ __forceinline__ void act_values(Act f, float (&v)[N])
 {
-    if (f.kind == DBS_ACT_NONE) return z;
-    if (f.kind == DBS_ACT_RELU) return z < 0.f ? 0.f : z;
-    if (f.kind == DBS_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    return z * logistic(z * (f.a + f.b * z * z));
+    if (f.kind == DBS_ACT_NONE) return;
+    if (f.kind == DBS_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
+    } else if (f.kind == DBS_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * (1.f + erff(v[i] * 0.70710678118654752f));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] * logistic(v[i] * (f.a + f.b * v[i] * v[i]));
+    }
 }
 // act(z) and act'(z).
 __device__ __forceinline__ float act_slope(Act f, float z, float &value)
@@ -167,10 +175,12 @@ struct GemmArgs {
     Act act;
     SaveTo save[2];
     int32_t vec;             // y and res take 16-byte (G_DX, G_DW: 8-byte) accesses
+    int32_t p_padded, q_padded;  // rows of P, Q go on to a whole 16 bytes (Q of G_DX: with zeros)
     // filled by the launcher
-    int32_t tp, tq, splits;
-    float *part;             // splits' sums
-    int32_t *done;           // a word per tile, zero between calls
+    int32_t chunks;          // P and Q are made of whole 16-byte chunks
+    int32_t tp, tq;          // tiles along p and q
+    int32_t full, splits;    // tiles taken whole; parts of each of the others along k
+    float *part;             // the parts' sums
     const void *zeros;       // 16 bytes of zeros
 };
 
@@ -178,8 +188,6 @@ struct GemmArgs {
 struct LayerWork {
     float *part;
     size_t part_bytes;
-    int32_t *done;
-    int32_t ndone;
     const void *zeros;
     int32_t cus;
 };

@@ -1,13 +1,17 @@
 // Matrix products of the dense layer operators on the matrix cores, in tiles
 // through LDS, with their epilogues.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "layer.hpp"
 
 namespace dbs {
 
-constexpr int BK = 64;  // elements of the sum per step
+constexpr int BK = 64;    // elements of the sum per step
+constexpr int GROUP = 4;  // rows of tiles that are worked on together
+constexpr int64_t MAX_TILES = 1 << 30;
+constexpr double JOIN_STEPS = 1.5;  // steps that a tile's sums take to memory or back
 
 typedef short s4_t __attribute__((ext_vector_type(4)));
 
@@ -63,8 +67,203 @@ template <int KIND> __device__ __forceinline__ int p_row(int r, int &mat)
     return r;
 }
 
+// Rounds and stores a wave's 16 MT x 64 sums (gated: 32 columns of each
+// projection): q0 and p0 are its first row and column, z the product of a batch.
+template <class X, int KIND, int MT>
+__device__ __forceinline__ void epilogue(const GemmArgs &a, const f4_t (&acc)[MT][4], int q0, int p0, int z)
+{
+    typedef typename X::T T;
+    typedef typename X::V8 V8;
+    typedef typename X::V4 V4;
+    const int lane = lane_id(), r = lane & 15, g = lane >> 4;
+    if constexpr ((KIND == G_DX || KIND == G_DW)) {
+        T *y = (T *)a.y[z];
+        const int64_t ld = a.ldy[z];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const int row = q0 + 16 * m + r;
+            if (row >= a.qn) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int col = p0 + 16 * j + 4 * g;
+                T *dst = y + (int64_t)row * ld + col;
+                V4 v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = (T)acc[m][j][i];
+                if (a.vec && col + 4 <= a.pn) *(V4 *)dst = v;
+                else
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (col + i < a.pn) dst[i] = v[i];
+            }
+        }
+    } else {
+        // a lane's columns: 16 in a row (gated: 8 of gate and the same 8 of up)
+        constexpr int NC = KIND == G_GATED ? 8 : 16;
+        const int col = p0 + (KIND == G_GATED ? 8 * g : 16 * g);
+        // rounds to the element type, keeps v, lanes of a group of 32 columns together
+        auto save = [&](const SaveTo &to, const float (&v)[NC], int row) {
+            T t[NC];
+#pragma unroll
+            for (int i = 0; i < NC; ++i) t[i] = (T)v[i];
+            if (to.full) {
+                if (row >= a.qn) return;
+                T *dst = (T *)to.full + (int64_t)row * to.ld + col;
+                if (to.vec && col + NC <= a.pn) {
+#pragma unroll
+                    for (int i = 0; i < NC; i += 8) *(V8 *)(dst + i) = *(const V8 *)(t + i);
+                } else
+#pragma unroll
+                    for (int i = 0; i < NC; ++i)
+                        if (col + i < a.pn) dst[i] = t[i];
+                return;
+            }
+            float big = 0.f;
+#pragma unroll
+            for (int i = 0; i < NC; ++i) big = fmaxf(big, col + i < a.pn ? ck_mag((float)t[i]) : 0.f);
+            big = fmaxf(big, __shfl_xor(big, 16, 64));
+            if (NC == 8) big = fmaxf(big, __shfl_xor(big, 32, 64));
+            if (row >= a.qn || col >= a.pn) return;
+            const int e = ck_exp<X>(big);
+            const int64_t ngroup = (a.pn + CK_GROUP - 1) / CK_GROUP;
+            if (col % CK_GROUP == 0) to.exps[row * ngroup + col / CK_GROUP] = (uint8_t)(e + CK_BIAS);
+            int8_t *dst = to.codes + (int64_t)row * a.pn + col;
+            int8_t code[NC];
+#pragma unroll
+            for (int i = 0; i < NC; ++i) code[i] = (int8_t)ck_code((float)t[i], e);
+            if (to.vec && col + NC <= a.pn) {
+                uint32_t w[NC / 4];
+#pragma unroll
+                for (int i = 0; i < NC / 4; ++i)
+                    w[i] = (uint32_t)(uint8_t)code[4 * i] | (uint32_t)(uint8_t)code[4 * i + 1] << 8 |
+                           (uint32_t)(uint8_t)code[4 * i + 2] << 16 | (uint32_t)(uint8_t)code[4 * i + 3] << 24;
+                if (NC == 16) *(uint4 *)dst = make_uint4(w[0], w[1], w[NC / 4 - 2], w[NC / 4 - 1]);
+                else *(uint2 *)dst = make_uint2(w[0], w[1]);
+            } else
+#pragma unroll
+                for (int i = 0; i < NC; ++i)
+                    if (col + i < a.pn) dst[i] = code[i];
+        };
+        float bias[NC];
+        if constexpr (KIND == G_LINEAR) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) bias[i] = a.bias && col + i < a.pn ? (float)((const T *)a.bias)[col + i] : 0.f;
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const int row = q0 + 16 * m + r;
+            float v[NC];
+            if constexpr (KIND == G_GATED) {
+                float up[NC];
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    v[i] = acc[m][i >> 2][i & 3];
+                    up[i] = acc[m][2 + (i >> 2)][i & 3];
+                }
+                if (a.save[0].full || a.save[0].codes) {
+                    save(a.save[0], v, row);
+                    save(a.save[1], up, row);
+                }
+                act_values(a.act, v);
+#pragma unroll
+                for (int i = 0; i < NC; ++i) v[i] *= up[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < NC; ++i) v[i] = acc[m][i >> 2][i & 3] + bias[i];
+                if (a.save[0].full || a.save[0].codes) save(a.save[0], v, row);
+                act_values(a.act, v);
+            }
+            if (row >= a.qn || col >= a.pn) continue;
+            T *dst = (T *)a.y[0] + (int64_t)row * a.ldy[0] + col;
+            const T *res = KIND == G_LINEAR && a.res ? (const T *)a.res + (int64_t)row * a.ldr + col : nullptr;
+            if (a.vec && col + NC <= a.pn) {
+#pragma unroll
+                for (int h = 0; h < NC; h += 8) {
+                    V8 o;
+                    if (res) {
+                        const V8 add = *(const V8 *)(res + h);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[h + i] += (float)add[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) o[i] = (T)v[h + i];
+                    *(V8 *)(dst + h) = o;
+                }
+            } else
+#pragma unroll
+                for (int i = 0; i < NC; ++i)
+                    if (col + i < a.pn) dst[i] = (T)(v[i] + (res ? (float)res[i] : 0.f));
+        }
+    }
+}
+
+// What a workgroup does: steps s0 .. s1 - 1 of a tile.
+struct Unit {
+    int q0, p0, z, s0, s1;
+    int tile;  // of those in parts, -1: whole
+    int part;
+};
+// Tiles follow each other in groups of GROUP rows of tiles.
+template <int DQ, int DP> __device__ __forceinline__ Unit place_of(const GemmArgs &a, int tile)
+{
+    Unit u{};
+    u.z = tile / (a.tp * a.tq);
+    tile -= u.z * a.tp * a.tq;
+    const int per = GROUP * a.tp, grp = tile / per, first = grp * GROUP, gsz = min(GROUP, a.tq - first);
+    u.q0 = (first + (tile - grp * per) % gsz) * DQ;
+    u.p0 = (tile - grp * per) / gsz * DP;
+    return u;
+}
+// The first `full` tiles are taken whole, one round of workgroups after the
+// other; the rest, which would leave most compute units idle in the last round,
+// in parts along k.  Each XCD has a stretch of neighbouring tiles, for its L2.
+template <int DQ, int DP> __device__ __forceinline__ Unit unit_of(const GemmArgs &a)
+{
+    const int ntile = a.tp * a.tq * a.batch, steps = (a.kn + BK - 1) / BK * a.segs;
+    const int id = (int)blockIdx.x, rest = id >= a.full;
+    const int n = rest ? (ntile - a.full) * a.splits : a.full, i = rest ? id - a.full : id;
+    const int x = i & 7, each = n >> 3, rem = n & 7;
+    const int at = x * each + min(x, rem) + (i >> 3);
+    Unit u;
+    u.part = rest ? at % a.splits : 0;
+    u.tile = rest && a.splits > 1 ? at / a.splits : -1;
+    u.s0 = rest ? (int)((int64_t)steps * u.part / a.splits) : 0;
+    u.s1 = rest ? (int)((int64_t)steps * (u.part + 1) / a.splits) : steps;
+    const Unit at_tile = place_of<DQ, DP>(a, rest ? a.full + at / a.splits : at);
+    u.q0 = at_tile.q0, u.p0 = at_tile.p0, u.z = at_tile.z;
+    return u;
+}
+
+// A tile in parts: each workgroup leaves its sums in memory.
+template <int NT, int MT> __device__ __forceinline__ void leave_part(const GemmArgs &a, const Unit &u, const f4_t (&acc)[MT][4])
+{
+    f4_t *own = (f4_t *)a.part + (int64_t)(u.tile * a.splits + u.part) * MT * 4 * NT + threadIdx.x;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) own[(m * 4 + j) * NT] = acc[m][j];
+}
+
+// The sums of the tiles in parts, added in the order of the parts; a workgroup
+// takes 16 rows of each of a tile's waves.
+template <class X, int KIND, int NWQ, int NWP, int MT> __global__ __launch_bounds__(64 * NWQ * NWP) void k_join(GemmArgs a)
+{
+    using C = Tile<X, KIND, NWQ, NWP, MT>;
+    const int tid = (int)threadIdx.x, wave = wave_id(), wq = wave / NWP, wp = wave % NWP;
+    const int tile = (int)blockIdx.x / MT, m = (int)blockIdx.x % MT;
+    const Unit u = place_of<C::TQ, KIND == G_GATED ? C::TP / 2 : C::TP>(a, a.full + tile);
+    const f4_t *all = (const f4_t *)a.part + ((int64_t)tile * a.splits * MT + m) * 4 * C::NT + tid;
+    f4_t acc[1][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[0][j] = all[j * C::NT];
+    for (int p = 1; p < a.splits; ++p)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[0][j] += all[((int64_t)p * MT * 4 + j) * C::NT];
+    epilogue<X, KIND, 1>(a, acc, u.q0 + 16 * (MT * wq + m), u.p0 + (KIND == G_GATED ? 32 : 64) * wp, u.z);
+}
+
 template <class X, int KIND, int NWQ, int NWP, int MT>
-__global__ __launch_bounds__(64 * NWQ * NWP) void k_tile(GemmArgs a)
+__global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_tile(GemmArgs a)
 {
     using C = Tile<X, KIND, NWQ, NWP, MT>;
     typedef typename X::T T;
@@ -74,22 +273,9 @@ __global__ __launch_bounds__(64 * NWQ * NWP) void k_tile(GemmArgs a)
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = wave_id();
     const int wq = wave / NWP, wp = wave % NWP, r = lane & 15, g = lane >> 4;
 
-    // tiles in groups of 8 rows of tiles, each XCD a stretch of its own
-    const int ntile = a.tp * a.tq, total = ntile * a.splits;
-    int id = (int)blockIdx.x;
-    {
-        const int x = id & 7, qn = total >> 3, rem = total & 7;
-        id = x * qn + (x < rem ? x : rem) + (id >> 3);
-    }
-    const int tile = id / a.splits, split = id - tile * a.splits;
-    const int per = 8 * a.tp, grp = tile / per, first = grp * 8, gsz = min(8, a.tq - first);
-    const int tqi = first + (tile - grp * per) % gsz, tpi = (tile - grp * per) / gsz;
-    const int z = (int)blockIdx.y;
-    const int q0 = tqi * C::TQ;
-    const int p0 = tpi * (KIND == G_GATED ? C::TP / 2 : C::TP);
-
-    const int ksteps = (a.kn + BK - 1) / BK, steps = ksteps * a.segs;
-    const int s0 = (int)((int64_t)steps * split / a.splits), s1 = (int)((int64_t)steps * (split + 1) / a.splits);
+    const Unit u = unit_of<C::TQ, KIND == G_GATED ? C::TP / 2 : C::TP>(a);
+    const int q0 = u.q0, p0 = u.p0, z = u.z, s0 = u.s0, s1 = u.s1;
+    const int ksteps = (a.kn + BK - 1) / BK;
 
     V8 rp[C::LP], rq[C::LQ];
     auto fetch = [&](int step) {
@@ -186,154 +372,242 @@ __global__ __launch_bounds__(64 * NWQ * NWP) void k_tile(GemmArgs a)
         if (t + 1 < s1) stage(buf ^ 1);
     }
 
-    // ---- epilogue
-    if constexpr (C::PKS) {
-        T *y = (T *)a.y[z];
-        const int64_t ld = a.ldy[z];
+    if (u.tile >= 0) leave_part<C::NT, MT>(a, u, acc);
+    else epilogue<X, KIND, MT>(a, acc, q0 + 16 * MT * wq, p0 + (KIND == G_GATED ? 32 : 64) * wp, z);
+}
+
+
+#define LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
+#define GLB_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
+
+template <class X, int KIND, int NWQ, int NWP, int MT>
+__global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_block(GemmArgs a)
+{
+    using C = Tile<X, KIND, NWQ, NWP, MT>;
+    typedef typename X::V8 V8;
+    typedef typename X::V4 V4;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][C::PB + C::QB];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = wave_id();
+    const int wq = wave / NWP, wp = wave % NWP, r = lane & 15, g = lane >> 4;
+
+    const Unit u = unit_of<C::TQ, KIND == G_GATED ? C::TP / 2 : C::TP>(a);
+    const int q0 = u.q0, p0 = u.p0, z = u.z, s0 = u.s0, s1 = u.s1;
+    const int ksteps = (a.kn + BK - 1) / BK;
+
+    // where a thread's chunks are, in bytes from the tile's first element of a step
+    uint32_t vp[C::LP], vq[C::LQ];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int row = q0 + 16 * (MT * wq + m) + r;
-            if (row >= a.qn) continue;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int col = p0 + 64 * wp + 16 * j + 4 * g;
-                T *dst = y + (int64_t)row * ld + col;
-                V4 v;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = (T)acc[m][j][i];
-                if (a.vec && col + 4 <= a.pn) *(V4 *)dst = v;
-                else
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (col + i < a.pn) dst[i] = v[i];
-            }
+    for (int i = 0; i < C::LP; ++i) {
+        const int c = i * C::NT + tid;
+        if constexpr (C::PKS) {
+            const int k = c / (C::TP / 8), col = 8 * ((c % (C::TP / 8)) ^ swz_k<C::TP>(k));
+            vp[i] = (uint32_t)(k * (int)a.ldp[0] + min(col, (a.pn - 1 - p0) & ~7)) * 2u;
+        } else {
+            int mat;
+            const int row = p_row<KIND>(c >> 3, mat);
+            vp[i] = (uint32_t)(min(row, a.pn - 1 - p0) * (int)a.ldp[mat] + 8 * ((c & 7) ^ swz_p<KIND>(c >> 3))) * 2u;
         }
-    } else {
-        // a lane's columns: 16 in a row (gated: 8 of gate and the same 8 of up)
-        constexpr int NC = KIND == G_GATED ? 8 : 16;
-        const int col = p0 + (KIND == G_GATED ? 32 * wp + 8 * g : 64 * wp + 16 * g);
-        // rounds to the element type, keeps v, lanes of a group of 32 columns together
-        auto save = [&](const SaveTo &to, const float (&v)[NC], int row) {
-            T t[NC];
+    }
 #pragma unroll
-            for (int i = 0; i < NC; ++i) t[i] = (T)v[i];
-            if (to.full) {
-                if (row >= a.qn) return;
-                T *dst = (T *)to.full + (int64_t)row * to.ld + col;
-                if (to.vec && col + NC <= a.pn) {
-#pragma unroll
-                    for (int i = 0; i < NC; i += 8) *(V8 *)(dst + i) = *(const V8 *)(t + i);
-                } else
-#pragma unroll
-                    for (int i = 0; i < NC; ++i)
-                        if (col + i < a.pn) dst[i] = t[i];
-                return;
-            }
-            float big = 0.f;
-#pragma unroll
-            for (int i = 0; i < NC; ++i) big = fmaxf(big, col + i < a.pn ? ck_mag((float)t[i]) : 0.f);
-            big = fmaxf(big, __shfl_xor(big, 16, 64));
-            if (NC == 8) big = fmaxf(big, __shfl_xor(big, 32, 64));
-            if (row >= a.qn || col >= a.pn) return;
-            const int e = ck_exp<X>(big);
-            const int64_t ngroup = (a.pn + CK_GROUP - 1) / CK_GROUP;
-            if (col % CK_GROUP == 0) to.exps[row * ngroup + col / CK_GROUP] = (uint8_t)(e + CK_BIAS);
-            int8_t *dst = to.codes + (int64_t)row * a.pn + col;
-            int8_t code[NC];
-#pragma unroll
-            for (int i = 0; i < NC; ++i) code[i] = (int8_t)ck_code((float)t[i], e);
-            if (to.vec && col + NC <= a.pn) {
-                uint32_t w[NC / 4];
-#pragma unroll
-                for (int i = 0; i < NC / 4; ++i)
-                    w[i] = (uint32_t)(uint8_t)code[4 * i] | (uint32_t)(uint8_t)code[4 * i + 1] << 8 |
-                           (uint32_t)(uint8_t)code[4 * i + 2] << 16 | (uint32_t)(uint8_t)code[4 * i + 3] << 24;
-                if (NC == 16) *(uint4 *)dst = make_uint4(w[0], w[1], w[NC / 4 - 2], w[NC / 4 - 1]);
-                else *(uint2 *)dst = make_uint2(w[0], w[1]);
-            } else
-#pragma unroll
-                for (int i = 0; i < NC; ++i)
-                    if (col + i < a.pn) dst[i] = code[i];
-        };
-        float bias[NC];
-        if constexpr (KIND == G_LINEAR) {
-#pragma unroll
-            for (int i = 0; i < NC; ++i) bias[i] = a.bias && col + i < a.pn ? (float)((const T *)a.bias)[col + i] : 0.f;
+    for (int i = 0; i < C::LQ; ++i) {
+        const int c = i * C::NT + tid;
+        if constexpr (C::QKS) {
+            const int k = c / (C::TQ / 8), col = 8 * ((c % (C::TQ / 8)) ^ swz_k<C::TQ>(k));
+            vq[i] = (uint32_t)(k * (int)a.ldq[0] + min(col, (a.qn - 1 - q0) & ~7)) * 2u;
+        } else {
+            vq[i] = (uint32_t)(min(c >> 3, a.qn - 1 - q0) * (int)a.ldq[0] + 8 * ((c & 7) ^ swz_q(c >> 3))) * 2u;
         }
+    }
+    // a step's chunks of P and Q straight into LDS; TAIL: zeros past the last k
+    auto load = [&](auto tail, int step, int buf) {
+        constexpr bool TAIL = decltype(tail)::value;
+        const int seg = a.segs > 1 && step >= ksteps ? 1 : 0;
+        const int k0 = (step - seg * ksteps) * BK;
+        uint8_t *lp = lds[buf] + wave * 1024, *lq = lp + C::PB;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int row = q0 + 16 * (MT * wq + m) + r;
-            float v[NC];
-            if constexpr (KIND == G_GATED) {
-                float up[NC];
-#pragma unroll
-                for (int i = 0; i < NC; ++i) {
-                    v[i] = acc[m][i >> 2][i & 3];
-                    up[i] = acc[m][2 + (i >> 2)][i & 3];
-                }
-                if (a.save[0].full || a.save[0].codes) {
-                    save(a.save[0], v, row);
-                    save(a.save[1], up, row);
-                }
-#pragma unroll
-                for (int i = 0; i < NC; ++i) v[i] = act_value(a.act, v[i]) * up[i];
+        for (int i = 0; i < C::LP; ++i) {
+            const int c = i * C::NT + tid;
+            const uint8_t *b;
+            int k;
+            if constexpr (C::PKS) {
+                b = (const uint8_t *)a.p[seg] + ((int64_t)k0 * a.ldp[seg] + p0) * 2;
+                k = c / (C::TP / 8);
             } else {
-#pragma unroll
-                for (int i = 0; i < NC; ++i) v[i] = acc[m][i >> 2][i & 3] + bias[i];
-                if (a.save[0].full || a.save[0].codes) save(a.save[0], v, row);
-#pragma unroll
-                for (int i = 0; i < NC; ++i) v[i] = act_value(a.act, v[i]);
+                const int mat = KIND == G_GATED ? ((i * C::NT / 8 + wave * 8) >> 5) & 1 : 0;
+                b = (const uint8_t *)a.p[mat] + ((int64_t)p0 * a.ldp[mat] + k0) * 2;
+                k = 8 * ((c & 7) ^ swz_p<KIND>(c >> 3));
             }
-            if (row >= a.qn || col >= a.pn) continue;
-            T *dst = (T *)a.y[0] + (int64_t)row * a.ldy[0] + col;
-            const T *res = KIND == G_LINEAR && a.res ? (const T *)a.res + (int64_t)row * a.ldr + col : nullptr;
-            if (a.vec && col + NC <= a.pn) {
-#pragma unroll
-                for (int h = 0; h < NC; h += 8) {
-                    V8 o;
-                    if (res) {
-                        const V8 add = *(const V8 *)(res + h);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) v[h + i] += (float)add[i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] = (T)v[h + i];
-                    *(V8 *)(dst + h) = o;
-                }
-            } else
-#pragma unroll
-                for (int i = 0; i < NC; ++i)
-                    if (col + i < a.pn) dst[i] = (T)(v[i] + (res ? (float)res[i] : 0.f));
+            const uint8_t *src = b + vp[i];
+            if (TAIL && k0 + k >= a.kn) src = (const uint8_t *)a.zeros;
+            __builtin_amdgcn_global_load_lds(GLB_PTR(src), LDS_PTR(lp + i * C::NT * 16), 16, 0, 0);
         }
+#pragma unroll
+        for (int i = 0; i < C::LQ; ++i) {
+            const int c = i * C::NT + tid;
+            const uint8_t *b;
+            int k;
+            if constexpr (C::QKS) {
+                b = (const uint8_t *)a.q[z] + ((int64_t)k0 * a.ldq[z] + q0) * 2;
+                k = c / (C::TQ / 8);
+            } else {
+                b = (const uint8_t *)a.q[seg] + ((int64_t)q0 * a.ldq[seg] + k0) * 2;
+                k = 8 * ((c & 7) ^ swz_q(c >> 3));
+            }
+            const uint8_t *src = b + vq[i];
+            if (TAIL && k0 + k >= a.kn) src = (const uint8_t *)a.zeros;
+            __builtin_amdgcn_global_load_lds(GLB_PTR(src), LDS_PTR(lq + i * C::NT * 16), 16, 0, 0);
+        }
+    };
+    const bool ragged = a.kn % BK != 0;
+    auto fetch = [&](int step, int buf) {
+        if (ragged && (step == ksteps - 1 || step == 2 * ksteps - 1)) load(std::true_type{}, step, buf);
+        else load(std::false_type{}, step, buf);
+    };
+
+    f4_t acc[MT][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[m][j] = f4_t{0.f, 0.f, 0.f, 0.f};
+
+    auto tr = [&](const uint8_t *p) {
+        return __builtin_bit_cast(V4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4_t *)p));
+    };
+    auto across = [&](const uint8_t *base, int tcols, int swz, int s, int unit) {
+        const int k = 32 * s + 8 * g + (r >> 2);
+        const uint8_t *p = base + k * tcols * 2 + (((unit << 1) ^ swz) + ((r >> 1) & 1)) * 16 + (r & 1) * 8;
+        const V4 lo = tr(p), hi = tr(p + 4 * tcols * 2);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    V8 fp[2][4], fq[2][MT];
+    auto fragments = [&](int buf, int s) {
+        const uint8_t *lp = lds[buf], *lq = lds[buf] + C::PB;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (C::PKS) fp[s][j] = across(lp, C::TP, swz_k<C::TP>(8 * g + (r >> 2)), s, 4 * wp + j);
+            else {
+                const int row = KIND == G_GATED ? 64 * wp + 32 * (j >> 1) + 8 * (r >> 2) + 4 * (j & 1) + (r & 3)
+                                                : 64 * wp + 16 * (r >> 2) + 4 * j + (r & 3);
+                fp[s][j] = *(const V8 *)(lp + row * 128 + ((4 * s + g) ^ swz_p<KIND>(row)) * 16);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            if constexpr (C::QKS) fq[s][m] = across(lq, C::TQ, swz_k<C::TQ>(8 * g + (r >> 2)), s, MT * wq + m);
+            else {
+                const int row = 16 * (MT * wq + m) + r;
+                fq[s][m] = *(const V8 *)(lq + row * 128 + ((4 * s + g) ^ swz_q(row)) * 16);
+            }
+        }
+    };
+    // one half of a step, its products spread between the reads of the next half
+    auto multiply = [&](int s) {
+        constexpr int READS = (C::PKS ? 8 : 4) + (C::QKS ? 2 : 1) * MT, MMAS = 4 * MT, EACH = MMAS / READS;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[m][j] = X::mma(fp[s][j], fq[s][m], acc[m][j]);
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an LDS read
+            __builtin_amdgcn_sched_group_barrier(0x8, EACH, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, MMAS - READS * EACH, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    if (s0 < s1) {
+        fetch(s0, 0);
+        __syncthreads();
+        if (s0 + 1 < s1) fetch(s0 + 1, 1);
+        fragments(0, 0);
+        for (int t = s0; t < s1; ++t) {
+            const int buf = (t - s0) & 1;
+            fragments(buf, 1);
+            multiply(0);
+            // the next step has arrived, and every wave has read this one
+            __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
+            if (t + 2 < s1) fetch(t + 2, buf);
+            __builtin_amdgcn_s_setprio(1);
+            fragments(buf ^ 1, 0);  // (after the last step: not used)
+            multiply(1);
+            __builtin_amdgcn_s_setprio(0);
+        }
+    }
+    if (u.tile >= 0) leave_part<C::NT, MT>(a, u, acc);
+    else epilogue<X, KIND, MT>(a, acc, q0 + 16 * MT * wq, p0 + (KIND == G_GATED ? 32 : 64) * wp, z);
+}
+
+// How many tiles are taken whole and in how many parts the others: the time of
+// the last round in steps, and what joining costs (a tile's sums written, and
+// those of all its parts read by one workgroup).
+static void plan_parts(GemmArgs &a, const LayerWork &w, int64_t ntile, int per_cu, int64_t tile_bytes)
+{
+    const int64_t slots = (int64_t)w.cus * per_cu, steps = (int64_t)((a.kn + BK - 1) / BK) * a.segs;
+    const int64_t rest = ntile % slots;
+    a.full = (int32_t)(ntile - rest), a.splits = 1;
+    if (rest == 0) return;
+    double best = (double)steps;
+    for (int64_t s = 2; s <= 16 && s * 2 <= steps && rest * s * tile_bytes <= (int64_t)w.part_bytes; ++s) {
+        const double cost = (double)((rest * s + slots - 1) / slots) * (double)((steps + s - 1) / s) + JOIN_STEPS * (1.0 + s);
+        if (cost < best) best = cost, a.splits = (int32_t)s;
     }
 }
 
-template <class X, int KIND, int NWQ, int NWP, int MT> hipError_t launch_tile(GemmArgs a, hipStream_t s)
+template <class X, int KIND, int NWQ, int NWP, int MT, bool BLOCK>
+hipError_t launch_tile(const LayerWork &w, GemmArgs a, hipStream_t s)
 {
     using C = Tile<X, KIND, NWQ, NWP, MT>;
-    a.tq = (a.qn + C::TQ - 1) / C::TQ;
-    a.tp = KIND == G_GATED ? (a.pn + C::TP / 2 - 1) / (C::TP / 2) : (a.pn + C::TP - 1) / C::TP;
-    a.splits = 1;
-    if (a.tq == 0 || a.tp == 0) return hipSuccess;
-    hipLaunchKernelGGL((k_tile<X, KIND, NWQ, NWP, MT>), dim3((unsigned)(a.tp * a.tq), (unsigned)a.batch), dim3(C::NT), 0,
-                       s, a);
+    constexpr int DP = KIND == G_GATED ? C::TP / 2 : C::TP;
+    const int64_t tq = ((int64_t)a.qn + C::TQ - 1) / C::TQ, tp = ((int64_t)a.pn + DP - 1) / DP, ntile = tq * tp * a.batch;
+    if (ntile == 0) return hipSuccess;
+    if (ntile > MAX_TILES) return hipErrorInvalidConfiguration;
+    a.tq = (int32_t)tq, a.tp = (int32_t)tp;
+    plan_parts(a, w, ntile, 160 * 1024 / (2 * (C::PB + C::QB)), (int64_t)C::TP * C::TQ * 4);
+    const unsigned grid = (unsigned)(a.full + (ntile - a.full) * a.splits);
+    if constexpr (BLOCK) hipLaunchKernelGGL((k_block<X, KIND, NWQ, NWP, MT>), dim3(grid), dim3(C::NT), 0, s, a);
+    else hipLaunchKernelGGL((k_tile<X, KIND, NWQ, NWP, MT>), dim3(grid), dim3(C::NT), 0, s, a);
+    if (a.splits > 1)
+        hipLaunchKernelGGL((k_join<X, KIND, NWQ, NWP, MT>), dim3((unsigned)((ntile - a.full) * MT)), dim3(C::NT), 0, s, a);
     return hipGetLastError();
 }
 
-template <class X> hipError_t launch_kind(GemmKind kind, const GemmArgs &a, hipStream_t s)
+template <class X, int KIND> hipError_t launch_kind(const LayerWork &w, const GemmArgs &a, hipStream_t s)
+{
+    if (a.chunks) return launch_tile<X, KIND, 2, 4, 8, true>(w, a, s);
+    return launch_tile<X, KIND, 2, 2, 4, false>(w, a, s);
+}
+
+template <class X> hipError_t launch_type(const LayerWork &w, GemmKind kind, const GemmArgs &a, hipStream_t s)
 {
     switch (kind) {
-    case G_LINEAR: return launch_tile<X, G_LINEAR, 2, 2, 4>(a, s);
-    case G_GATED: return launch_tile<X, G_GATED, 2, 2, 4>(a, s);
-    case G_DX: return launch_tile<X, G_DX, 2, 2, 4>(a, s);
-    default: return launch_tile<X, G_DW, 2, 2, 4>(a, s);
+    case G_LINEAR: return launch_kind<X, G_LINEAR>(w, a, s);
+    case G_GATED: return launch_kind<X, G_GATED>(w, a, s);
+    case G_DX: return launch_kind<X, G_DX>(w, a, s);
+    default: return launch_kind<X, G_DW>(w, a, s);
     }
+}
+
+// Whether an operand is made of whole 16-byte chunks, as loads straight into
+// LDS need it, near enough to each other for 32-bit offsets within a tile.
+static bool whole_chunks(const void *p, int64_t ld, int64_t contiguous, bool padded)
+{
+    return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld <= (1 << 21) && (padded || contiguous % 8 == 0);
 }
 
 hipError_t launch_gemm(const LayerWork &w, bool bf16, GemmKind kind, GemmArgs a, hipStream_t s)
 {
-    (void)w;
-    return bf16 ? launch_kind<Bf16>(kind, a, s) : launch_kind<Fp16>(kind, a, s);
+    a.zeros = w.zeros, a.part = w.part;
+    const bool pks = kind == G_DX || kind == G_DW, qks = kind == G_DW;
+    const int np = kind == G_GATED || kind == G_DX ? (kind == G_GATED ? 2 : a.segs) : 1;
+    const int nq = kind == G_DX ? a.segs : a.batch;
+    a.chunks = 1;
+    for (int i = 0; i < np; ++i)
+        a.chunks &= whole_chunks(a.p[i], a.ldp[i], pks ? a.pn : a.kn, a.p_padded) && (kind != G_DX || a.ldp[i] == a.ldp[0]);
+    for (int i = 0; i < nq; ++i)
+        a.chunks &= whole_chunks(a.q[i], a.ldq[i], qks ? a.qn : a.kn, a.q_padded) && a.ldq[i] == a.ldq[0];
+    return bf16 ? launch_type<Bf16>(w, kind, a, s) : launch_type<Fp16>(w, kind, a, s);
 }
 
 }  // namespace dbs

@@ -136,16 +136,16 @@ class LayerContext:
         self.stream = torch.cuda.current_stream() if stream is None else stream
         self.device = self.stream.device
         self._raw = self.stream.cuda_stream
+        self._fn = _lib.load()
         out = ctypes.c_void_p()
         with torch.cuda.device(self.device):
-            check(_lib.load().dbs_layer_create(ctypes.c_void_p(self._raw), ctypes.byref(out)))
+            check(self._fn.dbs_layer_create(ctypes.c_void_p(self._raw), ctypes.byref(out)))
         self._h = out
-        self._fn = _lib.load()
 
     def __del__(self):
         h = getattr(self, "_h", None)
         if h is not None and h.value:
-            _lib.load().dbs_layer_destroy(h)
+            self._fn.dbs_layer_destroy(h)
             self._h = None
 
     # -- a call: outputs are allocated and the kernels launched in here
