@@ -26,7 +26,7 @@ HIP_FLAGS = [
 CXX_FLAGS = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-pthread"]
 
 HIP_SOURCES = ["kernels.hip", "entries.hip", "bfs.hip", "decode.hip", "api.hip", "basic.hip", "convert.hip",
-               "layer.hip", "layer_gemm.hip", "checkpoint.hip"]
+               "layer.hip", "layer_gemm.hip", "layer_rows.hip", "checkpoint.hip"]
 CXX_SOURCES = ["builder.cpp"]
 
 

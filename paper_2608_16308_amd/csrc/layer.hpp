@@ -194,6 +194,10 @@ struct LayerWork {
 
 hipError_t launch_gemm(const LayerWork &w, bool bf16, GemmKind kind, GemmArgs a, hipStream_t s);
 
+// G_LINEAR and G_GATED for up to ROWS_TOKENS tokens.
+constexpr int ROWS_TOKENS = 32;
+hipError_t launch_rows(const LayerWork &w, bool bf16, bool gated, const GemmArgs &a, hipStream_t s);
+
 // Activation gradients: dz = dy * act'(pre) or, gated, dz = dy * up * act'(gate)
 // and du = dy * act(gate), rounded to the element type, rows of `ldz` elements
 // with zeros behind the last column; sums of the columns of the unrounded dz.
