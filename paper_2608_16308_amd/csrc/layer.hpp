@@ -194,8 +194,10 @@ struct LayerWork {
 
 hipError_t launch_gemm(const LayerWork &w, bool bf16, GemmKind kind, GemmArgs a, hipStream_t s);
 
-// G_LINEAR and G_GATED for up to ROWS_TOKENS tokens.
-constexpr int ROWS_TOKENS = 32;
+// G_LINEAR and G_GATED for few tokens; whether these kernels take a call: up to
+// ROWS_TOKENS tokens, rows of at least a load, 16 of them within 32-bit offsets.
+constexpr int ROWS_TOKENS = 16;
+bool rows_take(bool gated, const GemmArgs &a);
 hipError_t launch_rows(const LayerWork &w, bool bf16, bool gated, const GemmArgs &a, hipStream_t s);
 
 // Activation gradients: dz = dy * act'(pre) or, gated, dz = dy * up * act'(gate)

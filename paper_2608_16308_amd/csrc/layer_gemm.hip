@@ -599,7 +599,8 @@ static bool whole_chunks(const void *p, int64_t ld, int64_t contiguous, bool pad
 hipError_t launch_gemm(const LayerWork &w, bool bf16, GemmKind kind, GemmArgs a, hipStream_t s)
 {
     a.zeros = w.zeros, a.part = w.part;
-    if ((kind == G_LINEAR || kind == G_GATED) && a.qn <= ROWS_TOKENS) return launch_rows(w, bf16, kind == G_GATED, a, s);
+    if ((kind == G_LINEAR || kind == G_GATED) && rows_take(kind == G_GATED, a))
+        return launch_rows(w, bf16, kind == G_GATED, a, s);
     const bool pks = kind == G_DX || kind == G_DW, qks = kind == G_DW;
     const int np = kind == G_GATED || kind == G_DX ? (kind == G_GATED ? 2 : a.segs) : 1;
     const int nq = kind == G_DX ? a.segs : a.batch;

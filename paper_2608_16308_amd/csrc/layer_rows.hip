@@ -14,164 +14,296 @@ template <class X> __device__ __forceinline__ typename X::V8 load_eight(const ty
 {
     return ((const Eight<X> *)p)->v;
 }
-// Eight elements, of which the first `left` exist.
-template <class X> __device__ __forceinline__ typename X::V8 load_some(const typename X::T *p, int left)
+// (weights pass once: they need not stay in the caches)
+template <class X> __device__ __forceinline__ typename X::V8 load_once(const typename X::T *p)
 {
-    if (left >= 8) return load_eight<X>(p);
-    typename X::V8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (typename X::T)0.f;
-    return v;
+    typedef typename X::V8 V8u __attribute__((aligned(2)));
+    return __builtin_nontemporal_load((const V8u *)p);
+}
+// Elements k .. k + 7 of a row of n >= 8, zeros past its end: what stands at
+// its last eight, moved down.
+template <class X> __device__ __forceinline__ typename X::V8 load_end(const typename X::T *row, int k, int n)
+{
+    const int at = min(k, n - 8), by = k - at;
+    struct Two {
+        uint64_t lo, hi;
+    } v = __builtin_bit_cast(Two, load_eight<X>(row + at));
+    if (by >= 4) v.lo = v.hi, v.hi = 0;
+    const int bits = 16 * (by & 3);
+    v.lo = v.lo >> bits | (v.hi << 1) << (63 - bits);
+    v.hi >>= bits;
+    if (by >= 8) v.lo = v.hi = 0;
+    return __builtin_bit_cast(typename X::V8, v);
 }
 
-constexpr int RW_U = 8;               // products of 32 k in flight
-constexpr int RW_K = 32 * RW_U;       // k of a wave's turn
-constexpr int RW_MAX_WAVES = 16;
+// Keeps a projection of token t, a column a lane: in 16 bits, or in 8, where 32
+// neighbouring lanes hold the columns of a group (`in`: one that exists).
+template <class X>
+__device__ __forceinline__ void keep_one(const SaveTo &to, float v, bool in, int t, int col, int cols, int64_t ngroup)
+{
+    typedef typename X::T T;
+    const T q = (T)v;
+    if (to.full) {
+        if (in) ((T *)to.full)[(int64_t)t * to.ld + col] = q;
+    } else if (to.codes) {
+        float big = in ? ck_mag((float)q) : 0.f;
+#pragma unroll
+        for (int o = 1; o < CK_GROUP; o <<= 1) big = fmaxf(big, __shfl_xor(big, o, 64));
+        if (!in) return;
+        const int e = ck_exp<X>(big);
+        to.codes[(int64_t)t * cols + col] = (int8_t)ck_code((float)q, e);
+        if (col % CK_GROUP == 0) to.exps[t * ngroup + col / CK_GROUP] = (uint8_t)(e + CK_BIAS);
+    }
+}
 
-// A wave multiplies 16 rows of w (RG times 16; gated: of both matrices) with
-// 16 TT tokens over its turns of RW_K elements; the waves' sums are added in
-// LDS, in their order.  Rows past the last are read as the last one, and not
-// written.
-template <class X, bool GATED, int RG, int TT>
-__global__ __launch_bounds__(64 * RW_MAX_WAVES) void k_rows_dense(GemmArgs a)
+// A column of token t from its sum (gated: of both projections).
+template <class X, bool GATED>
+__device__ __forceinline__ void finish_one(const GemmArgs &a, float sum, float up, bool in, int t, int col, int64_t ngroup)
+{
+    typedef typename X::T T;
+    float v[1] = {sum};
+    if (!GATED && a.bias && in) v[0] += (float)((const T *)a.bias)[col];
+    keep_one<X>(a.save[0], v[0], in, t, col, a.pn, ngroup);
+    if (GATED) keep_one<X>(a.save[1], up, in, t, col, a.pn, ngroup);
+    act_values(a.act, v);
+    if (GATED) v[0] *= up;
+    else if (a.res && in) v[0] += (float)((const T *)a.res)[(int64_t)t * a.ldr + col];
+    if (in) ((T *)a.y[0])[(int64_t)t * a.ldy[0] + col] = (T)v[0];
+}
+
+constexpr int RW_U = 8;                // products of 32 k in a wave's turn
+constexpr int RW_K = 32 * RW_U;
+constexpr int RW_MAX_WAVES = 8;
+constexpr int RW_ROW = RW_K * 2 + 16;  // bytes of a row in LDS: 16 rows start in different banks
+
+// A wave multiplies 16 rows of w (gated: 8 of either matrix) with up to 16
+// tokens over its turns of RW_K elements; the waves' sums are added in LDS, in
+// their order.  A workgroup does `groups` times 16 rows, one after the other (32
+// columns, a group of a checkpoint, where one is kept).  Rows and tokens past the
+// last are read as the last one, and not written.
+//
+// Loads follow the rows, 512 bytes of two rows an instruction, and a bounce
+// through LDS that is private to the wave brings them to the operands' order;
+// those of the next turn are on their way while one is multiplied.
+template <class X, bool GATED>
+__global__ __launch_bounds__(64 * RW_MAX_WAVES, 3) void k_rows_dense(GemmArgs a, int groups)
 {
     typedef typename X::T T;
     typedef typename X::V8 V8;
-    constexpr int NG = RG * (GATED ? 2 : 1), COLS = 16 * RG;
-    extern __shared__ float sums[];  // [waves][NG][TT][4][64], then the totals [NG][16 TT][16]
+    constexpr int COLS = GATED ? 8 : 16;  // of a group of rows
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = lane_id(), wave = wave_id(), waves = (int)blockDim.x / 64, r = lane & 15, g = lane >> 4;
-    const int p0 = (int)blockIdx.x * COLS;
-    const T *w[NG], *x[TT];
+    const int half = lane >> 5, at = 8 * (lane & 31);
+    uint8_t *lw = lds + wave * (16 + a.qn) * RW_ROW, *lx = lw + 16 * RW_ROW;
+    const uint8_t *rw = lw + r * RW_ROW + 16 * g, *rx = lx + min(r, a.qn - 1) * RW_ROW + 16 * g;
+    float *sums = (float *)lds, *total = sums + max(waves * 256, waves * (16 + a.qn) * (RW_ROW / 4));
+    // rows of x, in elements from the first
+    uint32_t ox[8];
 #pragma unroll
-    for (int n = 0; n < NG; ++n) {
-        const int mat = GATED ? n / RG : 0;
-        w[n] = (const T *)a.p[mat] + (int64_t)min(p0 + 16 * (n % RG) + r, a.pn - 1) * a.ldp[mat] + 8 * g;
-    }
-#pragma unroll
-    for (int t = 0; t < TT; ++t) x[t] = (const T *)a.q[0] + (int64_t)min(16 * t + r, a.qn - 1) * a.ldq[0] + 8 * g;
-    f4_t acc[NG][TT];
-#pragma unroll
-    for (int n = 0; n < NG; ++n)
-#pragma unroll
-        for (int t = 0; t < TT; ++t) acc[n][t] = f4_t{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < 8; ++t) ox[t] = (uint32_t)min(2 * t + half, a.qn - 1) * (uint32_t)a.ldq[0] + at;
+    const T *x = (const T *)a.q[0];
 
-    int k = wave * RW_K;
-    for (; k + RW_K <= a.kn; k += waves * RW_K) {
-        V8 vw[NG][RW_U], vx[TT][RW_U];
+    for (int n = 0; n < groups; ++n) {
+        // (a checkpoint's last group of columns may have no rows left)
+        const int p0 = min(((int)blockIdx.x * groups + n) * COLS, a.pn - 1);
+        // rows of w, from the first of their matrix
+        const T *w[2];
+        uint32_t ow[8];
 #pragma unroll
-        for (int n = 0; n < NG; ++n)
+        for (int m = 0; m < (GATED ? 2 : 1); ++m) w[m] = (const T *)a.p[m] + (int64_t)p0 * a.ldp[m];
 #pragma unroll
-            for (int u = 0; u < RW_U; ++u) vw[n][u] = load_eight<X>(w[n] + k + 32 * u);
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-#pragma unroll
-            for (int u = 0; u < RW_U; ++u) vx[t][u] = load_eight<X>(x[t] + k + 32 * u);
-#pragma unroll
-        for (int u = 0; u < RW_U; ++u)
-#pragma unroll
-            for (int n = 0; n < NG; ++n)
-#pragma unroll
-                for (int t = 0; t < TT; ++t) acc[n][t] = X::mma(vw[n][u], vx[t][u], acc[n][t]);
-    }
-    if (k < a.kn)  // the last turn, ragged
-        for (int u = 0; u < RW_U && k + 32 * u < a.kn; ++u) {
-            const int left = a.kn - (k + 32 * u + 8 * g);
-            V8 vx[TT];
-#pragma unroll
-            for (int t = 0; t < TT; ++t) vx[t] = load_some<X>(x[t] + k + 32 * u, left);
-#pragma unroll
-            for (int n = 0; n < NG; ++n) {
-                const V8 vw = load_some<X>(w[n] + k + 32 * u, left);
-#pragma unroll
-                for (int t = 0; t < TT; ++t) acc[n][t] = X::mma(vw, vx[t], acc[n][t]);
-            }
+        for (int i = 0; i < 8; ++i) {
+            const int row = 2 * i + half, m = 2 * i / COLS;
+            ow[i] = (uint32_t)min(row % COLS, a.pn - 1 - p0) * (uint32_t)a.ldp[m] + at;
         }
-
-    // lane (g, r) holds rows 4 g .. + 3 of w for token r
+        V8 vw[8], vx[8];
+        auto fetch = [&](int k) {
 #pragma unroll
-    for (int n = 0; n < NG; ++n)
+            for (int t = 0; t < 8; ++t)
+                if (2 * t < a.qn) vx[t] = load_eight<X>(x + k + ox[t]);
 #pragma unroll
-        for (int t = 0; t < TT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sums[(((wave * NG + n) * TT + t) * 4 + i) * 64 + lane] = acc[n][t][i];
-    __syncthreads();
-    float *total = sums + waves * NG * TT * 256;
-    for (int c = (int)threadIdx.x; c < NG * TT * 256; c += (int)blockDim.x) {
-        float s = sums[c];
-        for (int v = 1; v < waves; ++v) s += sums[v * NG * TT * 256 + c];
-        // c = ((n TT + t) 4 + i) 64 + 16 g + r: column 4 g + i of token 16 t + r
-        const int l = c & 63, i = (c >> 6) & 3, nt = c >> 8;
-        total[((nt / TT) * TT + nt % TT) * 256 + (l & 15) * 16 + 4 * (l >> 4) + i] = s;
-    }
-    __syncthreads();
-    // a thread per token and column, a row of COLS columns in neighbouring lanes
-    const int64_t ngroup = (a.pn + CK_GROUP - 1) / CK_GROUP;
-    for (int c = (int)threadIdx.x; c < 16 * TT * COLS; c += (int)blockDim.x) {
-        const int token = c / COLS, cc = c % COLS, col = p0 + cc;
-        const bool in = token < a.qn && col < a.pn;
-        auto value = [&](int mat) { return total[((mat * RG + cc / 16) * TT + token / 16) * 256 + (token & 15) * 16 + (cc & 15)]; };
-        auto save = [&](const SaveTo &to, float v) {
-            const T q = (T)v;
-            if (to.full) {
-                if (in) ((T *)to.full)[(int64_t)token * to.ld + col] = q;
-            } else if (RG == 2) {
-                float big = in ? ck_mag((float)q) : 0.f;
-#pragma unroll
-                for (int o = 1; o < CK_GROUP; o <<= 1) big = fmaxf(big, __shfl_xor(big, o, 64));
-                if (!in) return;
-                const int e = ck_exp<X>(big);
-                to.codes[(int64_t)token * a.pn + col] = (int8_t)ck_code((float)q, e);
-                if (cc == 0) to.exps[token * ngroup + col / CK_GROUP] = (uint8_t)(e + CK_BIAS);
-            }
+            for (int i = 0; i < 8; ++i) vw[i] = load_once<X>(w[2 * i / COLS] + k + ow[i]);
         };
-        float v[1] = {value(0)};
-        if (GATED) {
-            const float up = value(1);
-            if (a.save[0].full || a.save[0].codes) {
-                save(a.save[0], v[0]);
-                save(a.save[1], up);
+        f4_t acc = {0.f, 0.f, 0.f, 0.f};
+        auto multiply = [&]() {
+            wave_lds_sync();
+#pragma unroll
+            for (int u = 0; u < RW_U; ++u) {
+                acc = X::mma(*(const V8 *)(rw + 64 * u), *(const V8 *)(rx + 64 * u), acc);
+                if (u % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (registers for the loads in flight)
             }
-            act_values(a.act, v);
-            v[0] *= up;
-        } else {
-            if (a.bias && in) v[0] += (float)((const T *)a.bias)[col];
-            if (a.save[0].full || a.save[0].codes) save(a.save[0], v[0]);
-            act_values(a.act, v);
-            if (a.res && in) v[0] += (float)((const T *)a.res)[(int64_t)token * a.ldr + col];
+            wave_lds_sync();
+        };
+        int k = wave * RW_K;
+        if (k + RW_K <= a.kn) fetch(k);
+        for (; k + RW_K <= a.kn; k += waves * RW_K) {
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                if (2 * t + half < a.qn) *(V8 *)(lx + (2 * t + half) * RW_ROW + 2 * at) = vx[t];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) *(V8 *)(lw + (2 * i + half) * RW_ROW + 2 * at) = vw[i];
+            const int next = k + waves * RW_K;
+            if (next + RW_K <= a.kn) fetch(next);
+            multiply();
         }
-        if (in) ((T *)a.y[0])[(int64_t)token * a.ldy[0] + col] = (T)v[0];
+        if (k < a.kn) {  // the last turn, ragged
+#pragma unroll 4
+            for (int t = 0; 2 * t < a.qn; ++t) {
+                const int row = min(2 * t + half, a.qn - 1);
+                *(V8 *)(lx + row * RW_ROW + 2 * at) = load_end<X>(x + (int64_t)row * a.ldq[0], k + at, a.kn);
+            }
+#pragma unroll 4
+            for (int i = 0; i < 8; ++i) {
+                const int row = 2 * i + half, m = 2 * i / COLS;
+                *(V8 *)(lw + row * RW_ROW + 2 * at) =
+                    load_end<X>((const T *)a.p[m] + (int64_t)min(p0 + row % COLS, a.pn - 1) * a.ldp[m], k + at, a.kn);
+            }
+            multiply();
+        }
+        __syncthreads();
+        // lane (g, r) holds rows 4 g .. + 3 of w for token r
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[(wave * 4 + i) * 64 + lane] = acc[i];
+        __syncthreads();
+        for (int c = (int)threadIdx.x; c < 256; c += (int)blockDim.x) {
+            float s = sums[c];
+            for (int v = 1; v < waves; ++v) s += sums[v * 256 + c];
+            // c = 64 i + 16 g + r: row 4 g + i of token r
+            total[(n * 16 + (c & 15)) * 16 + 4 * ((c >> 4) & 3) + (c >> 6)] = s;
+        }
+        __syncthreads();
+    }
+    // a thread per token and column, a row of columns in neighbouring lanes
+    const int cols = COLS * groups;
+    const int64_t ngroup = (a.pn + CK_GROUP - 1) / CK_GROUP;
+    for (int c = (int)threadIdx.x; c < 16 * cols; c += (int)blockDim.x) {
+        const int token = c / cols, cc = c % cols, col = (int)blockIdx.x * cols + cc;
+        const bool in = token < a.qn && col < a.pn;
+        const float *of = total + ((cc / COLS) * 16 + token) * 16 + cc % COLS;
+        finish_one<X, GATED>(a, of[0], GATED ? of[8] : 0.f, in, token, col, ngroup);
     }
 }
 
-// Waves of a workgroup: a turn each at least, and no more than fill the device
-// (each wave has RW_U loads of 1 KB in flight).
+// Waves of a workgroup: as many as fill the device (each has 8 KB and more in
+// flight), with turns that they share out evenly where that costs less than
+// half of them.  What is kept does not matter here, so that it does not change
+// the order of a sum.
 static int waves_of(const LayerWork &w, int64_t groups, int64_t kn)
 {
-    const int64_t turns = (kn + RW_K - 1) / RW_K, want = (16 * (int64_t)w.cus + groups - 1) / groups;
-    int64_t n = std::max<int64_t>(1, std::min<int64_t>({turns, std::max<int64_t>(want, 4), RW_MAX_WAVES}));
-    return (int)n;
+    const int64_t turns = (kn + RW_K - 1) / RW_K, fill = (16 * (int64_t)w.cus + groups - 1) / groups;
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>({turns, std::max<int64_t>(fill, 4), RW_MAX_WAVES}));
+    int64_t best = most;
+    for (int64_t n = most; 2 * n >= most; --n)
+        if ((turns + n - 1) / n * n < (turns + best - 1) / best * best) best = n;
+    return (int)best;
 }
 
-template <class X, bool GATED, int RG, int TT> static hipError_t rows_t(const LayerWork &w, const GemmArgs &a, hipStream_t s)
+template <class X, bool GATED> static hipError_t rows_t(const LayerWork &w, const GemmArgs &a, hipStream_t s)
 {
-    constexpr int NG = RG * (GATED ? 2 : 1);
-    const int64_t groups = ((int64_t)a.pn + 16 * RG - 1) / (16 * RG);
-    const int waves = waves_of(w, groups, a.kn);
-    hipLaunchKernelGGL((k_rows_dense<X, GATED, RG, TT>), dim3((unsigned)groups), dim3((unsigned)(64 * waves)),
-                       (size_t)(waves + 1) * NG * TT * 1024, s, a);
+    constexpr int COLS = GATED ? 8 : 16;
+    const int64_t groups = ((int64_t)a.pn + COLS - 1) / COLS;
+    const int waves = waves_of(w, groups, a.kn), each = a.save[0].codes ? CK_GROUP / COLS : 1;
+    const size_t lds = (size_t)std::max(waves * 1024, waves * (16 + a.qn) * RW_ROW) + each * 1024;
+    hipLaunchKernelGGL((k_rows_dense<X, GATED>), dim3((unsigned)((groups + each - 1) / each)), dim3((unsigned)(64 * waves)), lds,
+                       s, a, each);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// one token
+// ---------------------------------------------------------------------------
+constexpr int DT_WAVES = 8, DT_CHUNKS = 4, DT_TURN = 512 * DT_CHUNKS;
+
+// A wave takes two rows of w (gated: one of either matrix) and reads them along
+// their length, 1 KB an instruction; with few rows, `ks` waves share a pair's
+// turns.  A workgroup does `pairs` pairs, one after the other where they are
+// more than its waves (32 columns, a group, where a checkpoint is kept).
+// Products in 32 bits on the vector ALUs, which have room for it.
+template <class X, bool GATED>
+__global__ __launch_bounds__(64 * DT_WAVES) void k_rows_dot(GemmArgs a, int ks, int pairs)
+{
+    typedef typename X::T T;
+    typedef typename X::V8 V8;
+    __shared__ float sums[CK_GROUP * DT_WAVES][2];  // a row per pair and wave on it
+    const int lane = lane_id(), wave = wave_id(), at = 8 * lane;
+    const T *w[2], *x = (const T *)a.q[0];
+    auto add = [&](V8 vw, V8 vx, float &s) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = __builtin_fmaf((float)vw[i], (float)vx[i], s);
+    };
+    for (int pair = wave / ks; pair < pairs; pair += DT_WAVES / ks) {
+        const int first = (int)blockIdx.x * pairs + pair;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+            w[n] = (const T *)a.p[GATED ? n : 0] + (int64_t)min(GATED ? first : 2 * first + n, a.pn - 1) * a.ldp[GATED ? n : 0];
+        float acc[2] = {0.f, 0.f};
+        int k = (wave % ks) * DT_TURN;
+        for (; k + DT_TURN <= a.kn; k += ks * DT_TURN) {
+            V8 vw[2][DT_CHUNKS], vx[DT_CHUNKS];
+#pragma unroll
+            for (int c = 0; c < DT_CHUNKS; ++c)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) vw[n][c] = load_once<X>(w[n] + k + 512 * c + at);
+#pragma unroll
+            for (int c = 0; c < DT_CHUNKS; ++c) vx[c] = load_eight<X>(x + k + 512 * c + at);
+#pragma unroll
+            for (int c = 0; c < DT_CHUNKS; ++c)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) add(vw[n][c], vx[c], acc[n]);
+        }
+        for (int c = 0; c < DT_CHUNKS && k + 512 * c < a.kn; ++c) {  // the last turn, ragged
+            V8 vw[2];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) vw[n] = load_end<X>(w[n], k + 512 * c + at, a.kn);
+            const V8 vx = load_end<X>(x, k + 512 * c + at, a.kn);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) add(vw[n], vx, acc[n]);
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const float s = wave_sum(acc[n]);
+            if (lane == 0) sums[pair * ks + wave % ks][n] = s;
+        }
+    }
+    __syncthreads();
+    // a lane per column
+    const int cols = GATED ? pairs : 2 * pairs, c = (int)threadIdx.x, col = (int)blockIdx.x * cols + c;
+    if (c >= cols) return;
+    auto value = [&](int n) {
+        const float(*p)[2] = sums + (GATED ? c : c / 2) * ks;
+        float s = p[0][n];
+        for (int i = 1; i < ks; ++i) s += p[i][n];
+        return s;
+    };
+    finish_one<X, GATED>(a, value(GATED ? 0 : c % 2), GATED ? value(1) : 0.f, col < a.pn, 0, col,
+                         (a.pn + CK_GROUP - 1) / CK_GROUP);
+}
+
+template <class X, bool GATED> static hipError_t dot_t(const LayerWork &w, const GemmArgs &a, hipStream_t s)
+{
+    const int64_t pairs = GATED ? a.pn : ((int64_t)a.pn + 1) / 2, turns = ((int64_t)a.kn + DT_TURN - 1) / DT_TURN;
+    int ks = 1;
+    while (ks < DT_WAVES && 2 * ks <= turns && pairs * ks < 8 * (int64_t)w.cus) ks *= 2;
+    const int per = a.save[0].codes ? CK_GROUP / (GATED ? 1 : 2) : DT_WAVES / ks;
+    hipLaunchKernelGGL((k_rows_dot<X, GATED>), dim3((unsigned)((pairs + per - 1) / per)), dim3(64 * DT_WAVES), 0, s, a, ks,
+                       per);
     return hipGetLastError();
 }
 
 template <class X, bool GATED> static hipError_t rows_g(const LayerWork &w, const GemmArgs &a, hipStream_t s)
 {
-    // a group of a checkpoint is 32 columns
-    if (a.save[0].codes) return a.qn <= 16 ? rows_t<X, GATED, 2, 1>(w, a, s) : rows_t<X, GATED, 2, 2>(w, a, s);
-    return a.qn <= 16 ? rows_t<X, GATED, 1, 1>(w, a, s) : rows_t<X, GATED, 1, 2>(w, a, s);
+    return a.qn == 1 ? dot_t<X, GATED>(w, a, s) : rows_t<X, GATED>(w, a, s);
+}
+
+bool rows_take(bool gated, const GemmArgs &a)
+{
+    const int64_t far = std::max({a.ldq[0], a.ldp[0], gated ? a.ldp[1] : 0});
+    return a.qn >= 1 && a.qn <= ROWS_TOKENS && a.kn >= 8 && far <= 1 << 27;
 }
 
 hipError_t launch_rows(const LayerWork &w, bool bf16, bool gated, const GemmArgs &a, hipStream_t s)
 {
-    if (a.qn == 0 || a.pn == 0) return hipSuccess;
+    if (a.pn == 0) return hipSuccess;
     if (gated) return bf16 ? rows_g<Bf16, true>(w, a, s) : rows_g<Fp16, true>(w, a, s);
     return bf16 ? rows_g<Bf16, false>(w, a, s) : rows_g<Fp16, false>(w, a, s);
 }
