@@ -553,26 +553,35 @@ typedef struct {
     uint8_t *d_exps;
 } dbs_keep;
 
+/* Device memory that a call may be given for its own use (aligned to 256 bytes,
+ * free again when the call is done).  Inputs whose rows do not all start and end
+ * at multiples of 16 bytes (n_in, n_out or a row's stride not a multiple of 8)
+ * are copied there into such rows where that makes the call faster.
+ * dbs_forward_work: what dbs_linear (gated = 0) and dbs_gated can use of it for
+ * that; with less, or NULL, they read such inputs as they are.  Inputs in whole
+ * 16-byte chunks need none.
+ * dbs_backward_work: what a backward call needs and can use: its activation, the
+ * sizes, whether x is held as a checkpoint (and dw is wanted), whether db is
+ * wanted, and whether all 16-bit inputs are in whole chunks (0 is enough for
+ * any).                                                                       */
+dbs_status dbs_forward_work(const dbs_layer *L, int gated, int32_t tokens, int32_t n_in, int32_t n_out, size_t *bytes);
+dbs_status dbs_backward_work(const dbs_layer *L, int gated, dbs_act act, int32_t tokens, int32_t n_in, int32_t n_out,
+                             int x_codes, int want_db, int whole, size_t *bytes);
+
 /* y = act(x w^T + bias) + residual:  x [tokens, n_in], w [n_out, n_in], bias
  * [n_out] or NULL, residual [tokens, n_out] or NULL, y [tokens, n_out];
  * pre (NULL allowed) receives x w^T + bias for the backward pass.            */
 dbs_status dbs_linear(dbs_layer *L, dbs_dtype dt, int32_t tokens, int32_t n_in, int32_t n_out, const void *d_x,
                       int64_t ldx, const void *d_w, int64_t ldw, const void *d_bias, dbs_act act,
-                      const void *d_residual, int64_t ldr, void *d_y, int64_t ldy, const dbs_keep *pre);
+                      const void *d_residual, int64_t ldr, void *d_y, int64_t ldy, const dbs_keep *pre, void *d_work,
+                      size_t work_bytes);
 
 /* h = act(x w_gate^T) * (x w_up^T):  w_gate, w_up [n_out, n_in], h [tokens,
  * n_out]; gate and up (both or neither, in one form) receive the projections.
  * With DBS_ACT_RELU the zeros of h are entries that dbs_spmspv_dense skips.  */
 dbs_status dbs_gated(dbs_layer *L, dbs_dtype dt, int32_t tokens, int32_t n_in, int32_t n_out, const void *d_x,
                      int64_t ldx, const void *d_w_gate, int64_t ldwg, const void *d_w_up, int64_t ldwu, dbs_act act,
-                     void *d_h, int64_t ldh, const dbs_keep *gate, const dbs_keep *up);
-
-/* Bytes of device memory that a backward call needs for its own use (what it
- * is given must be aligned to 256 bytes, and is free again when the call is
- * done): gated, act, the sizes, whether x is held as a checkpoint (and dw is
- * wanted), whether db is wanted.                                             */
-dbs_status dbs_backward_work(const dbs_layer *L, int gated, dbs_act act, int32_t tokens, int32_t n_in, int32_t n_out,
-                             int x_codes, int want_db, size_t *bytes);
+                     void *d_h, int64_t ldh, const dbs_keep *gate, const dbs_keep *up, void *d_work, size_t work_bytes);
 
 /* Gradients of dbs_linear, with dz = dy * act'(pre):  dx = dz w, dw = dz^T x,
  * db = the sum of dz over the tokens (the residual's gradient is dy itself).

@@ -31,7 +31,7 @@ EXPORTED = [
     "dbs_ctx_read_timing", "dbs_last_error", "dbs_version", "dbs_basic_build", "dbs_basic_destroy",
     "dbs_basic_spmspv", "dbs_matrix_build_dense", "dbs_matrix_layout_get", "dbs_matrix_download",
     "dbs_spmspv_noalloc", "dbs_ctx_set_single_launch",
-    "dbs_layer_create", "dbs_layer_set_stream", "dbs_layer_destroy", "dbs_linear", "dbs_gated", "dbs_backward_work",
+    "dbs_layer_create", "dbs_layer_set_stream", "dbs_layer_destroy", "dbs_linear", "dbs_gated", "dbs_forward_work", "dbs_backward_work",
     "dbs_linear_backward", "dbs_gated_backward", "dbs_pack", "dbs_unpack",
 ]
 DBS_NOALLOC_MAX_DIM = 1 << 20
@@ -155,11 +155,12 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "dbs_layer_set_stream": (ctypes.c_int, [vp, vp]),
         "dbs_layer_destroy": (None, [vp]),
         "dbs_linear": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, vp, i64, vp, i64, vp, ctypes.c_int, vp, i64, vp, i64,
-                                      P(Held)]),
+                                      P(Held), vp, ctypes.c_size_t]),
         "dbs_gated": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, vp, i64, vp, i64, vp, i64, ctypes.c_int, vp, i64,
-                                     P(Held), P(Held)]),
+                                     P(Held), P(Held), vp, ctypes.c_size_t]),
+        "dbs_forward_work": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, P(ctypes.c_size_t)]),
         "dbs_backward_work": (ctypes.c_int, [vp, ctypes.c_int, ctypes.c_int, i32, i32, i32, ctypes.c_int, ctypes.c_int,
-                                             P(ctypes.c_size_t)]),
+                                             ctypes.c_int, P(ctypes.c_size_t)]),
         "dbs_linear_backward": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, vp, i64, P(Held), vp, i64, P(Held),
                                                ctypes.c_int, vp, i64, vp, i64, vp, vp, ctypes.c_size_t]),
         "dbs_gated_backward": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, vp, i64, P(Held), vp, i64, vp, i64, P(Held),

@@ -130,6 +130,32 @@ __global__ __launch_bounds__(CK_TPB) void k_unpack(const int8_t *__restrict__ co
     }
 }
 
+// (bits only: one kernel for both types)
+__global__ __launch_bounds__(CK_TPB) void k_align(const _Float16 *__restrict__ src, int64_t ld, int32_t rows, int32_t cols,
+                                                  uint4 *__restrict__ dst, int64_t ldd)
+{
+    const uint32_t per = (uint32_t)((cols + 7) / 8);
+    const uint64_t total = (uint64_t)rows * per, stride = (uint64_t)gridDim.x * CK_TPB;
+    for (uint64_t i0 = (uint64_t)blockIdx.x * CK_TPB + threadIdx.x; i0 < total; i0 += CK_U * stride) {
+        Fp16::V8 v[CK_U];
+        int64_t at[CK_U];
+#pragma unroll
+        for (int u = 0; u < CK_U; ++u) {
+            const uint64_t i = i0 + u * stride < total ? i0 + u * stride : total - 1;
+            const int32_t row = (int32_t)(i / per), col = 8 * (int32_t)(i - (uint64_t)row * per);
+            const _Float16 *p = src + (int64_t)row * ld;
+            if (cols >= 8) v[u] = load_end<Fp16>(p, col, cols);
+            else
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[u][k] = k < cols ? p[min(k, cols - 1)] : (_Float16)0.f;
+            at[u] = ((int64_t)row * ldd + col) / 8;
+        }
+#pragma unroll
+        for (int u = 0; u < CK_U; ++u)
+            if (i0 + u * stride < total) dst[at[u]] = __builtin_bit_cast(uint4, v[u]);
+    }
+}
+
 constexpr int SL_WAVES = 4;                // waves of a workgroup, each a row at a time
 constexpr int SL_COLS = 64 * 8;            // columns of a workgroup
 
@@ -236,6 +262,16 @@ hipError_t launch_unpack(bool bf16, const int8_t *codes, const uint8_t *exps, in
 {
     if (rows == 0 || cols == 0) return hipSuccess;
     return bf16 ? unpack_t<Bf16>(codes, exps, rows, cols, y, ldy, cus, s) : unpack_t<Fp16>(codes, exps, rows, cols, y, ldy, cus, s);
+}
+
+hipError_t launch_align(const void *src, int64_t ld, int32_t rows, int32_t cols, void *dst, int64_t ldd, int32_t cus,
+                        hipStream_t s)
+{
+    if (rows == 0 || cols == 0) return hipSuccess;
+    const uint64_t chunks = (uint64_t)rows * ((cols + 7) / 8);
+    hipLaunchKernelGGL(k_align, dim3(chunk_grid(chunks, cus)), dim3(CK_TPB), 0, s, (const _Float16 *)src, ld, rows, cols,
+                       (uint4 *)dst, ldd);
+    return hipGetLastError();
 }
 
 // Workgroups along the rows: enough to fill the device, none with less than

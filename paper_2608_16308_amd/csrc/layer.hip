@@ -70,23 +70,28 @@ dbs_status check_call(const char *fn, const dbs_layer *L, dbs_dtype dt, int64_t 
     return DBS_OK;
 }
 
+dbs_status check_work(const char *fn, const void *d_work)
+{
+    if ((uintptr_t)d_work % 256) return dbs_fail(DBS_ERR_ARG, "%s: the workspace is not aligned to 256 bytes", fn);
+    return DBS_OK;
+}
+
+dbs_status check_room(const char *fn, size_t need, const void *d_work, size_t work_bytes)
+{
+    if (need > work_bytes || (need && !d_work) || (uintptr_t)d_work % 256)
+        return dbs_fail(DBS_ERR_ARG, "%s: needs %zu bytes of workspace at a multiple of 256, got %zu", fn, need, work_bytes);
+    return DBS_OK;
+}
+
 #define CHECK(expr)                                    \
     do {                                               \
         const dbs_status st_ = (expr);                 \
         if (st_ != DBS_OK) return st_;                 \
     } while (0)
 
-bool aligned(const void *p, int64_t ld, int bytes) { return (uintptr_t)p % bytes == 0 && ld * 2 % bytes == 0; }
-
 HeldIn held_in(const dbs_held *h) { return h ? HeldIn{h->d_values, h->ld, h->d_codes, h->d_exps} : HeldIn{}; }
 
-SaveTo save_to(const dbs_keep *k, int64_t cols)
-{
-    if (!k) return SaveTo{};
-    SaveTo s{k->d_values, k->ld, k->d_codes, k->d_exps, 0};
-    s.vec = k->d_values ? aligned(k->d_values, k->ld, 16) : (uintptr_t)k->d_codes % 16 == 0 && cols % 16 == 0;
-    return s;
-}
+SaveTo save_to(const dbs_keep *k) { return k ? SaveTo{k->d_values, k->ld, k->d_codes, k->d_exps} : SaveTo{}; }
 
 int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -102,25 +107,64 @@ struct Carve {
         return p;
     }
 };
+// Whether a product gains from copies of its operands in whole 16-byte chunks
+// (`bytes` of them): the tiles that load straight into LDS reach 900 TFLOP/s and
+// more where those through registers reach 400, and a copy is read and written at
+// 4.5 TB/s, after 3 us of launch.
+bool copies_pay(double flops, double bytes, int copies)
+{
+    return flops * (1 / 400e6 - 1 / 900e6) > 2 * bytes / 4.5e6 + 3.0 * copies;  // (us)
+}
+size_t rows_bytes(int64_t rows, int64_t cols) { return up256((size_t)rows * up8(cols) * 2); }
+
+// An operand, or its copy in whole chunks.
+struct Operand {
+    const void *p;
+    int64_t ld;
+    int32_t rows, cols;
+    bool whole() const { return whole_chunks(p, ld, cols); }
+};
+// Copies the operands that are not in whole chunks into the workspace, if that
+// pays and they fit; true if they all are then.
+hipError_t make_whole(const LayerWork &w, Operand *const *ops, int n, double flops, Carve &c, size_t room, hipStream_t s, bool *padded)
+{
+    size_t bytes = 0;
+    int copies = 0;
+    *padded = false;
+    for (int i = 0; i < n; ++i)
+        if (!ops[i]->whole()) bytes += rows_bytes(ops[i]->rows, ops[i]->cols), ++copies;
+    if (!copies || !c.base || c.used + bytes > room || !copies_pay(flops, (double)bytes, copies)) return hipSuccess;
+    for (int i = 0; i < n; ++i) {
+        Operand &o = *ops[i];
+        if (o.whole()) continue;
+        void *to = c.take(rows_bytes(o.rows, o.cols));
+        const hipError_t e = launch_align(o.p, o.ld, o.rows, o.cols, to, up8(o.cols), w.cus, s);
+        if (e != hipSuccess) return e;
+        o.p = to, o.ld = up8(o.cols);
+    }
+    *padded = true;
+    return hipSuccess;
+}
+
+// What a backward pass cannot do without: dz (and du) where an activation has a
+// slope or dy is not in whole chunks, the values of an x held in 8 bits, the
+// partial sums of db.
 struct BackwardWork {
     void *dz, *du, *x;
     float *sums;
     int64_t ldz, ldx;
-    size_t bytes;
+    Carve c;
 };
-// dz (and du) where an activation has a slope, the values of an x held in 8
-// bits, the partial sums of db.
 BackwardWork carve(void *mem, bool gated, bool slope, bool x_codes, bool db, int64_t t, int64_t n_in, int64_t n_out, int32_t cus)
 {
-    Carve c{(uint8_t *)mem};
     BackwardWork b{};
+    b.c.base = (uint8_t *)mem;
     b.ldz = up8(n_out);
     b.ldx = up8(n_in);
-    if (slope) b.dz = c.take((size_t)t * b.ldz * 2);
-    if (gated) b.du = c.take((size_t)t * b.ldz * 2);
-    if (x_codes) b.x = c.take((size_t)t * b.ldx * 2);
-    if (db) b.sums = (float *)c.take((size_t)slope_row_blocks((int32_t)t, (int32_t)n_out, cus) * n_out * 4);
-    b.bytes = c.used;
+    if (slope) b.dz = b.c.take((size_t)t * b.ldz * 2);
+    if (gated) b.du = b.c.take((size_t)t * b.ldz * 2);
+    if (x_codes) b.x = b.c.take((size_t)t * b.ldx * 2);
+    if (db) b.sums = (float *)b.c.take((size_t)slope_row_blocks((int32_t)t, (int32_t)n_out, cus) * n_out * 4);
     return b;
 }
 
@@ -171,9 +215,34 @@ void dbs_layer_destroy(dbs_layer *L)
     delete L;
 }
 
+// x and the one or two weights of a forward product, few tokens as they are.
+static dbs_status forward_operands(dbs_layer *L, const char *fn, Operand *const *ops, int n, GemmArgs &a, void *d_work,
+                                   size_t work_bytes)
+{
+    a.pn = ops[1]->rows, a.qn = ops[0]->rows, a.kn = ops[0]->cols, a.segs = 1, a.batch = 1;
+    bool padded = false;
+    Carve c{(uint8_t *)d_work};
+    if (a.qn > ROWS_TOKENS)
+        LAYER_TRY(make_whole(L->w, ops, n, 2.0 * (n - 1) * a.qn * a.kn * a.pn, c, work_bytes, L->stream, &padded), fn);
+    a.p_padded = a.q_padded = padded;
+    a.q[0] = ops[0]->p, a.ldq[0] = ops[0]->ld;
+    for (int i = 1; i < n; ++i) a.p[i - 1] = ops[i]->p, a.ldp[i - 1] = ops[i]->ld;
+    return DBS_OK;
+}
+
+dbs_status dbs_forward_work(const dbs_layer *L, int gated, int32_t t, int32_t n_in, int32_t n_out, size_t *bytes)
+{
+    CHECK(check_call("dbs_forward_work", L, DBS_F16, t, n_in, n_out));
+    if (!bytes) return dbs_fail(DBS_ERR_ARG, "dbs_forward_work: bytes is NULL");
+    const int n = gated ? 2 : 1;
+    const size_t x = rows_bytes(t, n_in), w = n * rows_bytes(n_out, n_in);
+    *bytes = t > ROWS_TOKENS && copies_pay(2.0 * n * t * n_in * n_out, (double)std::min(x, w), 1) ? x + w : 0;
+    return DBS_OK;
+}
+
 dbs_status dbs_linear(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_in, int32_t n_out, const void *d_x, int64_t ldx,
                       const void *d_w, int64_t ldw, const void *d_bias, dbs_act act, const void *d_res, int64_t ldr,
-                      void *d_y, int64_t ldy, const dbs_keep *pre)
+                      void *d_y, int64_t ldy, const dbs_keep *pre, void *d_work, size_t work_bytes)
 {
     const char *fn = "dbs_linear";
     CHECK(check_call(fn, L, dt, t, n_in, n_out));
@@ -184,19 +253,19 @@ dbs_status dbs_linear(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_in, int32
     if (d_res) CHECK(check_operand(fn, "residual", d_res, t, n_out, ldr));
     CHECK(check_operand(fn, "y", d_y, t, n_out, ldy));
     CHECK(check_keep(fn, "pre", pre, t, n_out));
+    CHECK(check_work(fn, d_work));
     GemmArgs a{};
-    a.p[0] = d_w, a.ldp[0] = ldw, a.q[0] = d_x, a.ldq[0] = ldx;
-    a.pn = n_out, a.qn = t, a.kn = n_in, a.segs = 1, a.batch = 1;
+    Operand x{d_x, ldx, t, n_in}, w{d_w, ldw, n_out, n_in}, *const ops[] = {&x, &w};
+    CHECK(forward_operands(L, fn, ops, 2, a, d_work, work_bytes));
     a.y[0] = d_y, a.ldy[0] = ldy, a.bias = d_bias, a.res = d_res, a.ldr = ldr, a.act = Act::of(act);
-    a.save[0] = save_to(pre, n_out);
-    a.vec = aligned(d_y, ldy, 16) && (!d_res || aligned(d_res, ldr, 16));
+    a.save[0] = save_to(pre);
     LAYER_TRY(launch_gemm(L->w, dt == DBS_BF16, G_LINEAR, a, L->stream), fn);
     return DBS_OK;
 }
 
 dbs_status dbs_gated(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_in, int32_t n_out, const void *d_x, int64_t ldx,
                      const void *d_wg, int64_t ldwg, const void *d_wu, int64_t ldwu, dbs_act act, void *d_h, int64_t ldh,
-                     const dbs_keep *gate, const dbs_keep *up)
+                     const dbs_keep *gate, const dbs_keep *up, void *d_work, size_t work_bytes)
 {
     const char *fn = "dbs_gated";
     CHECK(check_call(fn, L, dt, t, n_in, n_out));
@@ -210,54 +279,59 @@ dbs_status dbs_gated(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_in, int32_
     CHECK(check_keep(fn, "up", up, t, n_out));
     if (gate && t > 0 && n_out > 0 && (gate->d_codes == nullptr) != (up->d_codes == nullptr))
         return dbs_fail(DBS_ERR_ARG, "%s: gate and up are kept in one form", fn);
+    CHECK(check_work(fn, d_work));
     GemmArgs a{};
-    a.p[0] = d_wg, a.ldp[0] = ldwg, a.p[1] = d_wu, a.ldp[1] = ldwu, a.q[0] = d_x, a.ldq[0] = ldx;
-    a.pn = n_out, a.qn = t, a.kn = n_in, a.segs = 1, a.batch = 1;
+    Operand x{d_x, ldx, t, n_in}, g{d_wg, ldwg, n_out, n_in}, u{d_wu, ldwu, n_out, n_in}, *const ops[] = {&x, &g, &u};
+    CHECK(forward_operands(L, fn, ops, 3, a, d_work, work_bytes));
     a.y[0] = d_h, a.ldy[0] = ldh, a.act = Act::of(act);
-    a.save[0] = save_to(gate, n_out), a.save[1] = save_to(up, n_out);
-    a.vec = aligned(d_h, ldh, 16);
+    a.save[0] = save_to(gate), a.save[1] = save_to(up);
     LAYER_TRY(launch_gemm(L->w, dt == DBS_BF16, G_GATED, a, L->stream), fn);
     return DBS_OK;
 }
 
 dbs_status dbs_backward_work(const dbs_layer *L, int gated, dbs_act act, int32_t t, int32_t n_in, int32_t n_out, int x_codes,
-                             int want_db, size_t *bytes)
+                             int want_db, int whole, size_t *bytes)
 {
     CHECK(check_call("dbs_backward_work", L, DBS_F16, t, n_in, n_out));
     if (!bytes) return dbs_fail(DBS_ERR_ARG, "dbs_backward_work: bytes is NULL");
-    *bytes = carve(nullptr, gated != 0, gated || act != DBS_ACT_NONE, x_codes != 0, !gated && want_db, t, n_in, n_out, L->w.cus).bytes;
+    const int n = gated ? 2 : 1;
+    *bytes = carve(nullptr, gated != 0, gated || act != DBS_ACT_NONE || !whole, x_codes != 0, !gated && want_db, t, n_in, n_out, L->w.cus).c.used;
+    if (whole) return DBS_OK;
+    const double flops = 2.0 * n * t * n_in * n_out;
+    const size_t x = rows_bytes(t, n_in), w = rows_bytes(n_out, n_in);
+    if (copies_pay(flops, (double)w, 1)) *bytes += n * w;
+    if (!x_codes && copies_pay(flops, (double)x, 1)) *bytes += x;
     return DBS_OK;
 }
 
-// The products that both backward passes end in, dz (and du) given.
+// The products that both backward passes end in, dz (and du) given in whole
+// chunks.
 static dbs_status gradients(dbs_layer *L, const char *fn, dbs_dtype dt, int32_t t, int32_t n_in, int32_t n_out, int n,
-                            const void *const dz[2], int64_t ldz, const dbs_held *x, const BackwardWork &b,
-                            bool own_dz, const void *const w[2], const int64_t ldw[2], void *d_dx, int64_t lddx, void *const dw[2],
-                            const int64_t lddw[2])
+                            const void *const dz[2], int64_t ldz, bool own_dz, const dbs_held *x, BackwardWork &b,
+                            size_t room, Operand *const *w, void *d_dx, int64_t lddx, void *const dw[2], const int64_t lddw[2])
 {
     const bool bf = dt == DBS_BF16;
+    const double flops = 2.0 * n * t * n_in * n_out;
+    bool padded = false;
     if (d_dx) {
+        LAYER_TRY(make_whole(L->w, w, n, flops, b.c, room, L->stream, &padded), fn);
         GemmArgs a{};
-        for (int i = 0; i < n; ++i) a.p[i] = w[i], a.ldp[i] = ldw[i], a.q[i] = dz[i], a.ldq[i] = ldz;
+        for (int i = 0; i < n; ++i) a.p[i] = w[i]->p, a.ldp[i] = w[i]->ld, a.q[i] = dz[i], a.ldq[i] = ldz;
         a.pn = n_in, a.qn = t, a.kn = n_out, a.segs = n, a.batch = 1;
         a.y[0] = d_dx, a.ldy[0] = lddx;
-        a.vec = aligned(d_dx, lddx, 8), a.q_padded = own_dz;
+        a.p_padded = padded, a.q_padded = own_dz;
         LAYER_TRY(launch_gemm(L->w, bf, G_DX, a, L->stream), fn);
     }
     if (dw[0]) {
-        const void *xv = x ? x->d_values : nullptr;
-        int64_t ldx = x ? x->ld : 0;
+        Operand xv{x ? x->d_values : nullptr, x ? x->ld : 0, t, n_in}, *const ops[] = {&xv};
         if (b.x) {
             LAYER_TRY(launch_unpack(bf, x->d_codes, x->d_exps, t, n_in, b.x, b.ldx, L->w.cus, L->stream), fn);
-            xv = b.x, ldx = b.ldx;
-        }
+            xv.p = b.x, xv.ld = b.ldx;
+            padded = true;
+        } else LAYER_TRY(make_whole(L->w, ops, 1, flops, b.c, room, L->stream, &padded), fn);
         GemmArgs a{};
-        a.vec = 1;
-        for (int i = 0; i < n; ++i) {
-            a.q[i] = dz[i], a.ldq[i] = ldz, a.y[i] = dw[i], a.ldy[i] = lddw[i];
-            a.vec = a.vec && aligned(dw[i], lddw[i], 8);
-        }
-        a.p[0] = xv, a.ldp[0] = ldx, a.p_padded = b.x != nullptr, a.q_padded = own_dz;
+        for (int i = 0; i < n; ++i) a.q[i] = dz[i], a.ldq[i] = ldz, a.y[i] = dw[i], a.ldy[i] = lddw[i];
+        a.p[0] = xv.p, a.ldp[0] = xv.ld, a.p_padded = padded, a.q_padded = own_dz;
         a.pn = n_in, a.qn = n_out, a.kn = t, a.segs = 1, a.batch = n;
         LAYER_TRY(launch_gemm(L->w, bf, G_DW, a, L->stream), fn);
     }
@@ -282,21 +356,23 @@ dbs_status dbs_linear_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_
         CHECK(check_operand(fn, "dw", d_dw, n_out, n_in, lddw));
     }
     if (d_db) CHECK(check_operand(fn, "db", d_db, 1, n_out, n_out));
-    const bool slope = act != DBS_ACT_NONE, x_codes = d_dw && x && x->d_codes;
-    const BackwardWork b = carve(d_work, false, slope, x_codes, d_db != nullptr, t, n_in, n_out, L->w.cus);
-    if (b.bytes > work_bytes || (b.bytes && (!d_work || (uintptr_t)d_work % 256)))
-        return dbs_fail(DBS_ERR_ARG, "%s: needs %zu bytes of workspace at a multiple of 256, got %zu", fn, b.bytes, work_bytes);
+    // (a dy that is not in whole chunks becomes a dz that is, also without a slope)
+    const bool slope = act != DBS_ACT_NONE || !whole_chunks(d_dy, lddy, n_out), x_codes = d_dw && x && x->d_codes;
+    BackwardWork b = carve(d_work, false, slope, x_codes, d_db != nullptr, t, n_in, n_out, L->w.cus);
+    CHECK(check_room(fn, b.c.used, d_work, work_bytes));
     if (slope || d_db) {
         SlopeArgs s{};
         s.dy = d_dy, s.lddy = lddy, s.rows = t, s.cols = n_out, s.act = Act::of(act);
-        if (slope) s.pre = held_in(pre), s.dz = b.dz, s.ldz = b.ldz;
+        if (act != DBS_ACT_NONE) s.pre = held_in(pre);
+        s.dz = b.dz, s.ldz = b.ldz;
         s.sums = d_db ? b.sums : nullptr, s.db = d_db, s.row_blocks = slope_row_blocks(t, n_out, L->w.cus);
         LAYER_TRY(launch_slope(dt == DBS_BF16, false, s, L->stream), fn);
     }
-    const void *dz[2] = {slope ? b.dz : d_dy, nullptr}, *w[2] = {d_w, nullptr};
+    const void *dz[2] = {slope ? b.dz : d_dy, nullptr};
+    Operand w{d_w, ldw, n_out, n_in}, *const ws[] = {&w};
     void *dw[2] = {d_dw, nullptr};
-    const int64_t ldws[2] = {ldw, 0}, lddws[2] = {lddw, 0};
-    return gradients(L, fn, dt, t, n_in, n_out, 1, dz, slope ? b.ldz : lddy, x, b, slope, w, ldws, d_dx, lddx, dw, lddws);
+    const int64_t lddws[2] = {lddw, 0};
+    return gradients(L, fn, dt, t, n_in, n_out, 1, dz, slope ? b.ldz : lddy, slope, x, b, work_bytes, ws, d_dx, lddx, dw, lddws);
 }
 
 dbs_status dbs_gated_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_in, int32_t n_out, const void *d_dh,
@@ -322,19 +398,19 @@ dbs_status dbs_gated_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_i
         CHECK(check_operand(fn, "dw_up", d_dwu, n_out, n_in, lddwu));
     }
     const bool x_codes = d_dwg && x && x->d_codes;
-    const BackwardWork b = carve(d_work, true, true, x_codes, false, t, n_in, n_out, L->w.cus);
-    if (b.bytes > work_bytes || (b.bytes && (!d_work || (uintptr_t)d_work % 256)))
-        return dbs_fail(DBS_ERR_ARG, "%s: needs %zu bytes of workspace at a multiple of 256, got %zu", fn, b.bytes, work_bytes);
+    BackwardWork b = carve(d_work, true, true, x_codes, false, t, n_in, n_out, L->w.cus);
+    CHECK(check_room(fn, b.c.used, d_work, work_bytes));
     if (t > 0) {
         SlopeArgs s{};
         s.dy = d_dh, s.lddy = lddh, s.pre = held_in(gate), s.up = held_in(up), s.rows = t, s.cols = n_out, s.act = Act::of(act);
         s.dz = b.dz, s.du = b.du, s.ldz = b.ldz, s.row_blocks = slope_row_blocks(t, n_out, L->w.cus);
         LAYER_TRY(launch_slope(dt == DBS_BF16, true, s, L->stream), fn);
     }
-    const void *dz[2] = {b.dz, b.du}, *w[2] = {d_wg, d_wu};
+    const void *dz[2] = {b.dz, b.du};
+    Operand g{d_wg, ldwg, n_out, n_in}, u{d_wu, ldwu, n_out, n_in}, *const ws[] = {&g, &u};
     void *dw[2] = {d_dwg, d_dwu};
-    const int64_t ldw[2] = {ldwg, ldwu}, lddw[2] = {lddwg, lddwu};
-    return gradients(L, fn, dt, t, n_in, n_out, 2, dz, b.ldz, x, b, true, w, ldw, d_dx, lddx, dw, lddw);
+    const int64_t lddw[2] = {lddwg, lddwu};
+    return gradients(L, fn, dt, t, n_in, n_out, 2, dz, b.ldz, true, x, b, work_bytes, ws, d_dx, lddx, dw, lddw);
 }
 
 dbs_status dbs_pack(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t cols, const void *d_x, int64_t ldx, int8_t *d_codes,

@@ -39,6 +39,30 @@ struct Fp16 {
     }
 };
 
+// Eight elements at any alignment.
+template <class X> struct __attribute__((packed, aligned(2))) Eight {
+    typename X::V8 v;
+};
+template <class X> __device__ __forceinline__ typename X::V8 load_eight(const typename X::T *p)
+{
+    return ((const Eight<X> *)p)->v;
+}
+// Elements k .. k + 7 of a row of n >= 8, zeros past its end: what stands at
+// its last eight, moved down.
+template <class X> __device__ __forceinline__ typename X::V8 load_end(const typename X::T *row, int k, int n)
+{
+    const int at = min(k, n - 8), by = k - at;
+    struct Two {
+        uint64_t lo, hi;
+    } v = __builtin_bit_cast(Two, load_eight<X>(row + at));
+    if (by >= 4) v.lo = v.hi, v.hi = 0;
+    const int bits = 16 * (by & 3);
+    v.lo = v.lo >> bits | (v.hi << 1) << (63 - bits);
+    v.hi >>= bits;
+    if (by >= 8) v.lo = v.hi = 0;
+    return __builtin_bit_cast(typename X::V8, v);
+}
+
 // ---------------------------------------------------------------------------
 // activations
 // ---------------------------------------------------------------------------
@@ -145,7 +169,6 @@ struct SaveTo {
     int64_t ld;
     int8_t *codes;
     uint8_t *exps;
-    int32_t vec;  // 16-byte stores are aligned
 };
 // What a backward pass reads: 16-bit values, or a checkpoint.
 struct HeldIn {
@@ -174,7 +197,6 @@ struct GemmArgs {
     int64_t ldr;
     Act act;
     SaveTo save[2];
-    int32_t vec;             // y and res take 16-byte (G_DX, G_DW: 8-byte) accesses
     int32_t p_padded, q_padded;  // rows of P, Q go on to a whole 16 bytes (Q of G_DX: with zeros)
     // filled by the launcher
     int32_t chunks;          // P and Q are made of whole 16-byte chunks
@@ -193,6 +215,13 @@ struct LayerWork {
 };
 
 hipError_t launch_gemm(const LayerWork &w, bool bf16, GemmKind kind, GemmArgs a, hipStream_t s);
+// Whether an operand is made of whole 16-byte chunks (`contiguous` of its
+// elements in a row), as loads straight into LDS need it, near enough to each
+// other for 32-bit offsets within a tile.
+bool whole_chunks(const void *p, int64_t ld, int64_t contiguous);
+// A copy of an operand in rows of ldd elements, zeros behind the last column.
+hipError_t launch_align(const void *src, int64_t ld, int32_t rows, int32_t cols, void *dst, int64_t ldd, int32_t cus,
+                        hipStream_t s);
 
 // G_LINEAR and G_GATED for few tokens; whether these kernels take a call: up to
 // ROWS_TOKENS tokens, rows of at least a load, 16 of them within 32-bit offsets.

@@ -11,23 +11,9 @@ namespace dbs {
 constexpr int BK = 64;    // elements of the sum per step
 constexpr int GROUP = 4;  // rows of tiles that are worked on together
 constexpr int64_t MAX_TILES = 1 << 30;
-constexpr double JOIN_STEPS = 1.5;  // steps that a tile's sums take to memory or back
+constexpr double JOIN_STEPS = 2;  // steps that a tile's sums take to memory or back
 
 typedef short s4_t __attribute__((ext_vector_type(4)));
-
-template <class X> struct __attribute__((packed, aligned(2))) Chunk {
-    typename X::V8 v;
-};
-
-// Eight elements from p, of which the first `left` exist.
-template <class X> __device__ __forceinline__ typename X::V8 load_chunk(const typename X::T *p, int64_t left)
-{
-    if (left >= 8) return ((const Chunk<X> *)p)->v;
-    typename X::V8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (typename X::T)0.f;
-    return v;
-}
 
 // LDS tiles hold 16-byte chunks of eight elements in rows, chunk c of row r at
 // place c ^ swz(r), so that the lanes of one read fall into different banks.
@@ -53,6 +39,8 @@ struct Tile {
     static constexpr bool PKS = KIND == G_DX || KIND == G_DW, QKS = KIND == G_DW;
     static constexpr int PB = TP * BK * 2, QB = TQ * BK * 2;
     static constexpr int LP = PB / 16 / NT, LQ = QB / 16 / NT;  // chunks per thread and step
+    // workgroups that fit the LDS of a compute unit
+    static constexpr int per_cu(int stages) { return 160 * 1024 / (stages * (PB + QB)); }
     static_assert(PB % (16 * NT) == 0 && QB % (16 * NT) == 0, "whole chunks per thread");
 };
 
@@ -66,6 +54,12 @@ template <int KIND> __device__ __forceinline__ int p_row(int r, int &mat)
     mat = 0;
     return r;
 }
+
+// A store at any alignment.
+template <class V> struct __attribute__((packed, aligned(1))) Any {
+    V v;
+};
+template <class V> __device__ __forceinline__ void store_any(void *p, V v) { ((Any<V> *)p)->v = v; }
 
 // Rounds and stores a wave's 16 MT x 64 sums (gated: 32 columns of each
 // projection): q0 and p0 are its first row and column, z the product of a batch.
@@ -90,7 +84,7 @@ __device__ __forceinline__ void epilogue(const GemmArgs &a, const f4_t (&acc)[MT
                 V4 v;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] = (T)acc[m][j][i];
-                if (a.vec && col + 4 <= a.pn) *(V4 *)dst = v;
+                if (col + 4 <= a.pn) store_any(dst, v);
                 else
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -109,9 +103,14 @@ __device__ __forceinline__ void epilogue(const GemmArgs &a, const f4_t (&acc)[MT
             if (to.full) {
                 if (row >= a.qn) return;
                 T *dst = (T *)to.full + (int64_t)row * to.ld + col;
-                if (to.vec && col + NC <= a.pn) {
+                if (col + NC <= a.pn) {
 #pragma unroll
-                    for (int i = 0; i < NC; i += 8) *(V8 *)(dst + i) = *(const V8 *)(t + i);
+                    for (int i = 0; i < NC; i += 8) {
+                        V8 o;
+#pragma unroll
+                        for (int h = 0; h < 8; ++h) o[h] = t[i + h];
+                        store_any(dst + i, o);
+                    }
                 } else
 #pragma unroll
                     for (int i = 0; i < NC; ++i)
@@ -131,14 +130,14 @@ __device__ __forceinline__ void epilogue(const GemmArgs &a, const f4_t (&acc)[MT
             int8_t code[NC];
 #pragma unroll
             for (int i = 0; i < NC; ++i) code[i] = (int8_t)ck_code((float)t[i], e);
-            if (to.vec && col + NC <= a.pn) {
+            if (col + NC <= a.pn) {
                 uint32_t w[NC / 4];
 #pragma unroll
                 for (int i = 0; i < NC / 4; ++i)
                     w[i] = (uint32_t)(uint8_t)code[4 * i] | (uint32_t)(uint8_t)code[4 * i + 1] << 8 |
                            (uint32_t)(uint8_t)code[4 * i + 2] << 16 | (uint32_t)(uint8_t)code[4 * i + 3] << 24;
-                if (NC == 16) *(uint4 *)dst = make_uint4(w[0], w[1], w[NC / 4 - 2], w[NC / 4 - 1]);
-                else *(uint2 *)dst = make_uint2(w[0], w[1]);
+                if (NC == 16) store_any(dst, make_uint4(w[0], w[1], w[NC / 4 - 2], w[NC / 4 - 1]));
+                else store_any(dst, make_uint2(w[0], w[1]));
             } else
 #pragma unroll
                 for (int i = 0; i < NC; ++i)
@@ -176,18 +175,18 @@ __device__ __forceinline__ void epilogue(const GemmArgs &a, const f4_t (&acc)[MT
             if (row >= a.qn || col >= a.pn) continue;
             T *dst = (T *)a.y[0] + (int64_t)row * a.ldy[0] + col;
             const T *res = KIND == G_LINEAR && a.res ? (const T *)a.res + (int64_t)row * a.ldr + col : nullptr;
-            if (a.vec && col + NC <= a.pn) {
+            if (col + NC <= a.pn) {
 #pragma unroll
                 for (int h = 0; h < NC; h += 8) {
                     V8 o;
                     if (res) {
-                        const V8 add = *(const V8 *)(res + h);
+                        const V8 add = load_eight<X>(res + h);
 #pragma unroll
                         for (int i = 0; i < 8; ++i) v[h + i] += (float)add[i];
                     }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) o[i] = (T)v[h + i];
-                    *(V8 *)(dst + h) = o;
+                    store_any(dst + h, o);
                 }
             } else
 #pragma unroll
@@ -262,7 +261,7 @@ template <class X, int KIND, int NWQ, int NWP, int MT> __global__ __launch_bound
     epilogue<X, KIND, 1>(a, acc, u.q0 + 16 * (MT * wq + m), u.p0 + (KIND == G_GATED ? 32 : 64) * wp, u.z);
 }
 
-template <class X, int KIND, int NWQ, int NWP, int MT>
+template <class X, int KIND, int NWQ, int NWP, int MT, int PF>
 __global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_tile(GemmArgs a)
 {
     using C = Tile<X, KIND, NWQ, NWP, MT>;
@@ -277,41 +276,61 @@ __global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_tile(GemmArgs a)
     const int q0 = u.q0, p0 = u.p0, z = u.z, s0 = u.s0, s1 = u.s1;
     const int ksteps = (a.kn + BK - 1) / BK;
 
-    V8 rp[C::LP], rq[C::LQ];
-    auto fetch = [&](int step) {
-        const int seg = a.segs > 1 && step >= ksteps ? 1 : 0;
-        const int k0 = (step - seg * ksteps) * BK;
+    V8 rp[PF][C::LP], rq[PF][C::LQ];
+    // A chunk: elements `at` .. + 7 of row `row` of a matrix of `rows` rows of n
+    // elements.  EDGE: it may pass a row's end, and reads as zeros there; else
+    // only the rows may be past the last, and are read as the last.
+    auto chunk = [&](auto edge, const T *m, int64_t ld, int row, int rows, int at, int n) {
+        const T *p = m + (int64_t)min(row, rows - 1) * ld;
+        if (!decltype(edge)::value) return load_eight<X>(p + at);
+        if (n >= 8) return load_end<X>(p, at, n);
+        V8 v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = at + i < n ? p[min(at + i, n - 1)] : (T)0.f;
+        return v;
+    };
+    auto fetch_p = [&](auto edge, int seg, int k0, V8(&v)[C::LP]) {
 #pragma unroll
         for (int i = 0; i < C::LP; ++i) {
             const int c = i * C::NT + tid;
             if constexpr (C::PKS) {
                 const int k = c / (C::TP / 8), col = p0 + 8 * ((c % (C::TP / 8)) ^ swz_k<C::TP>(k));
-                const int left = k0 + k < a.kn ? a.pn - col : 0;
-                rp[i] = load_chunk<X>((const T *)a.p[seg] + (int64_t)(k0 + k) * a.ldp[seg] + col, left);
+                v[i] = chunk(edge, (const T *)a.p[seg], a.ldp[seg], k0 + k, a.kn, col, a.pn);
+                if (k0 + k >= a.kn) v[i] = V8{};
             } else {
                 int mat;
                 const int row = p0 + p_row<KIND>(c >> 3, mat), k = k0 + 8 * ((c & 7) ^ swz_p<KIND>(c >> 3));
-                rp[i] = load_chunk<X>((const T *)a.p[mat] + (int64_t)row * a.ldp[mat] + k, row < a.pn ? a.kn - k : 0);
+                v[i] = chunk(edge, (const T *)a.p[mat], a.ldp[mat], row, a.pn, k, a.kn);
             }
         }
+    };
+    auto fetch_q = [&](auto edge, int seg, int k0, V8(&v)[C::LQ]) {
 #pragma unroll
         for (int i = 0; i < C::LQ; ++i) {
             const int c = i * C::NT + tid;
             if constexpr (C::QKS) {
                 const int k = c / (C::TQ / 8), col = q0 + 8 * ((c % (C::TQ / 8)) ^ swz_k<C::TQ>(k));
-                rq[i] = load_chunk<X>((const T *)a.q[z] + (int64_t)(k0 + k) * a.ldq[z] + col,
-                                      k0 + k < a.kn ? a.qn - col : 0);
+                v[i] = chunk(edge, (const T *)a.q[z], a.ldq[z], k0 + k, a.kn, col, a.qn);
+                if (k0 + k >= a.kn) v[i] = V8{};
             } else {
                 const int row = q0 + (c >> 3), k = k0 + 8 * ((c & 7) ^ swz_q(c >> 3));
-                rq[i] = load_chunk<X>((const T *)a.q[seg] + (int64_t)row * a.ldq[seg] + k, row < a.qn ? a.kn - k : 0);
+                v[i] = chunk(edge, (const T *)a.q[seg], a.ldq[seg], row, a.qn, k, a.kn);
             }
         }
     };
-    auto stage = [&](int buf) {
+    auto fetch = [&](int step, int f) {
+        const int seg = a.segs > 1 && step >= ksteps ? 1 : 0;
+        const int k0 = (step - seg * ksteps) * BK;
+        if (C::PKS ? p0 + C::TP > a.pn : k0 + BK > a.kn) fetch_p(std::true_type{}, seg, k0, rp[f]);
+        else fetch_p(std::false_type{}, seg, k0, rp[f]);
+        if (C::QKS ? q0 + C::TQ > a.qn : k0 + BK > a.kn) fetch_q(std::true_type{}, seg, k0, rq[f]);
+        else fetch_q(std::false_type{}, seg, k0, rq[f]);
+    };
+    auto stage = [&](int f, int buf) {
 #pragma unroll
-        for (int i = 0; i < C::LP; ++i) *(V8 *)(lds[buf] + (i * C::NT + tid) * 16) = rp[i];
+        for (int i = 0; i < C::LP; ++i) *(V8 *)(lds[buf] + (i * C::NT + tid) * 16) = rp[f][i];
 #pragma unroll
-        for (int i = 0; i < C::LQ; ++i) *(V8 *)(lds[buf] + C::PB + (i * C::NT + tid) * 16) = rq[i];
+        for (int i = 0; i < C::LQ; ++i) *(V8 *)(lds[buf] + C::PB + (i * C::NT + tid) * 16) = rq[f][i];
     };
 
     f4_t acc[MT][4];
@@ -360,16 +379,20 @@ __global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_tile(GemmArgs a)
         }
     };
 
-    if (s0 < s1) {
-        fetch(s0);
-        stage(0);
-    }
-    for (int t = s0; t < s1; ++t) {
-        const int buf = (t - s0) & 1;
-        __syncthreads();
-        if (t + 1 < s1) fetch(t + 1);
-        compute(buf);
-        if (t + 1 < s1) stage(buf ^ 1);
+    // PF steps are on their way in registers while one is multiplied
+#pragma unroll
+    for (int f = 0; f < PF; ++f)
+        if (s0 + f < s1) fetch(s0 + f, f);
+    for (int t = s0; t < s1;) {
+#pragma unroll
+        for (int f = 0; f < PF; ++f, ++t) {
+            if (t >= s1) break;
+            const int buf = (t - s0) & 1;
+            stage(f, buf);
+            __syncthreads();
+            if (t + PF < s1) fetch(t + PF, f);
+            compute(buf);
+        }
     }
 
     if (u.tile >= 0) leave_part<C::NT, MT>(a, u, acc);
@@ -380,13 +403,13 @@ __global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_tile(GemmArgs a)
 #define LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
 #define GLB_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
 
-template <class X, int KIND, int NWQ, int NWP, int MT>
+template <class X, int KIND, int NWQ, int NWP, int MT, int NS>
 __global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_block(GemmArgs a)
 {
     using C = Tile<X, KIND, NWQ, NWP, MT>;
     typedef typename X::V8 V8;
     typedef typename X::V4 V4;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][C::PB + C::QB];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[NS][C::PB + C::QB];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = wave_id();
     const int wq = wave / NWP, wp = wave % NWP, r = lane & 15, g = lane >> 4;
 
@@ -516,67 +539,114 @@ __global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_block(GemmArgs a)
         __builtin_amdgcn_sched_barrier(0);
     };
 
+    // At most `steps` steps of loads are still on their way, and every wave's
+    // part of the others has arrived.
+    auto arrived = [&](auto steps) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(steps)::value * (C::LP + C::LQ)) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
     if (s0 < s1) {
-        fetch(s0, 0);
-        __syncthreads();
-        if (s0 + 1 < s1) fetch(s0 + 1, 1);
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+            if (s0 + i < s1) fetch(s0 + i, i);
+        if (s0 + NS <= s1) arrived(std::integral_constant<int, NS - 1>{});
+        else arrived(std::integral_constant<int, 0>{});
         fragments(0, 0);
+        int buf = 0;
         for (int t = s0; t < s1; ++t) {
-            const int buf = (t - s0) & 1;
+            const int next = buf + 1 < NS ? buf + 1 : 0;
             fragments(buf, 1);
             multiply(0);
             // the next step has arrived, and every wave has read this one
-            __syncthreads();
-            __builtin_amdgcn_sched_barrier(0);
-            if (t + 2 < s1) fetch(t + 2, buf);
+            if (NS > 2 && t + NS - 1 < s1) arrived(std::integral_constant<int, NS - 2>{});
+            else arrived(std::integral_constant<int, 0>{});
+            if (t + NS < s1) fetch(t + NS, buf);
             __builtin_amdgcn_s_setprio(1);
-            fragments(buf ^ 1, 0);  // (after the last step: not used)
+            fragments(next, 0);  // (after the last step: not used)
             multiply(1);
             __builtin_amdgcn_s_setprio(0);
+            buf = next;
         }
     }
     if (u.tile >= 0) leave_part<C::NT, MT>(a, u, acc);
     else epilogue<X, KIND, MT>(a, acc, q0 + 16 * MT * wq, p0 + (KIND == G_GATED ? 32 : 64) * wp, z);
 }
 
-// How many tiles are taken whole and in how many parts the others: the time of
-// the last round in steps, and what joining costs (a tile's sums written, and
-// those of all its parts read by one workgroup).
-static void plan_parts(GemmArgs &a, const LayerWork &w, int64_t ntile, int per_cu, int64_t tile_bytes)
+// How many tiles are taken whole and in how many parts the others; the steps
+// that a compute unit does in sequence, joining included (a tile's sums are
+// written, and those of all its parts read).
+static double plan_parts(GemmArgs &a, const LayerWork &w, int64_t ntile, int per_cu, int64_t tile_bytes)
 {
     const int64_t slots = (int64_t)w.cus * per_cu, steps = (int64_t)((a.kn + BK - 1) / BK) * a.segs;
     const int64_t rest = ntile % slots;
     a.full = (int32_t)(ntile - rest), a.splits = 1;
-    if (rest == 0) return;
+    const double whole = (double)(ntile / slots) * (double)steps;
+    if (rest == 0) return whole;
     double best = (double)steps;
     for (int64_t s = 2; s <= 16 && s * 2 <= steps && rest * s * tile_bytes <= (int64_t)w.part_bytes; ++s) {
         const double cost = (double)((rest * s + slots - 1) / slots) * (double)((steps + s - 1) / s) + JOIN_STEPS * (1.0 + s);
         if (cost < best) best = cost, a.splits = (int32_t)s;
     }
+    return whole + best;
 }
 
-template <class X, int KIND, int NWQ, int NWP, int MT, bool BLOCK>
-hipError_t launch_tile(const LayerWork &w, GemmArgs a, hipStream_t s)
+// The tiles of a call with a given kernel, `per_cu` workgroups of which fit a
+// compute unit; false: too many.
+template <class C, int KIND> static bool lay_out(const LayerWork &w, GemmArgs &a, int per_cu, double *steps)
 {
-    using C = Tile<X, KIND, NWQ, NWP, MT>;
     constexpr int DP = KIND == G_GATED ? C::TP / 2 : C::TP;
     const int64_t tq = ((int64_t)a.qn + C::TQ - 1) / C::TQ, tp = ((int64_t)a.pn + DP - 1) / DP, ntile = tq * tp * a.batch;
-    if (ntile == 0) return hipSuccess;
-    if (ntile > MAX_TILES) return hipErrorInvalidConfiguration;
+    if (ntile > MAX_TILES) return false;
     a.tq = (int32_t)tq, a.tp = (int32_t)tp;
-    plan_parts(a, w, ntile, 160 * 1024 / (2 * (C::PB + C::QB)), (int64_t)C::TP * C::TQ * 4);
+    *steps = plan_parts(a, w, ntile, per_cu, (int64_t)C::TP * C::TQ * 4);
+    return true;
+}
+
+// NS: stages in LDS, or 0: through registers, PF steps ahead.
+template <class X, int KIND, int NWQ, int NWP, int MT, int NS, int PF = 1>
+static hipError_t launch_tile(const LayerWork &w, GemmArgs a, hipStream_t s)
+{
+    using C = Tile<X, KIND, NWQ, NWP, MT>;
+    double steps;
+    if (!lay_out<C, KIND>(w, a, C::per_cu(NS ? NS : 2), &steps)) return hipErrorInvalidConfiguration;
+    const int ntile = a.tp * a.tq * a.batch;
+    if (ntile == 0) return hipSuccess;
     const unsigned grid = (unsigned)(a.full + (ntile - a.full) * a.splits);
-    if constexpr (BLOCK) hipLaunchKernelGGL((k_block<X, KIND, NWQ, NWP, MT>), dim3(grid), dim3(C::NT), 0, s, a);
-    else hipLaunchKernelGGL((k_tile<X, KIND, NWQ, NWP, MT>), dim3(grid), dim3(C::NT), 0, s, a);
+    if constexpr (NS != 0) hipLaunchKernelGGL((k_block<X, KIND, NWQ, NWP, MT, NS>), dim3(grid), dim3(C::NT), 0, s, a);
+    else hipLaunchKernelGGL((k_tile<X, KIND, NWQ, NWP, MT, PF>), dim3(grid), dim3(C::NT), 0, s, a);
     if (a.splits > 1)
         hipLaunchKernelGGL((k_join<X, KIND, NWQ, NWP, MT>), dim3((unsigned)((ntile - a.full) * MT)), dim3(C::NT), 0, s, a);
     return hipGetLastError();
 }
 
-template <class X, int KIND> hipError_t launch_kind(const LayerWork &w, const GemmArgs &a, hipStream_t s)
+// Microseconds that a call takes with each of the tiles: its steps, at what a
+// step of each costs with all compute units at it (256x256: 1250 TFLOP/s;
+// 128x128 with four stages: 830; 64x128 with three, two workgroups to a compute
+// unit: 700; the 128x128 through registers: 550).
+template <class X, int KIND> static double estimate(const LayerWork &w, GemmArgs a, int tile)
 {
-    if (a.chunks) return launch_tile<X, KIND, 2, 4, 8, true>(w, a, s);
-    return launch_tile<X, KIND, 2, 2, 4, false>(w, a, s);
+    double steps = 0;
+    bool ok;
+    if (tile == 0) ok = lay_out<Tile<X, KIND, 2, 4, 8>, KIND>(w, a, 1, &steps), steps *= 1.75;
+    else if (tile == 1) ok = lay_out<Tile<X, KIND, 4, 2, 2>, KIND>(w, a, 1, &steps), steps *= 0.66;
+    else ok = lay_out<Tile<X, KIND, 2, 2, 2>, KIND>(w, a, 2, &steps), steps *= 0.76;
+    return ok ? steps : 1e30;
+}
+
+template <class X, int KIND> static hipError_t launch_kind(const LayerWork &w, const GemmArgs &a, hipStream_t s)
+{
+    if (!a.chunks) {
+        // (gated 50x4097->5001 bf16: 37 us with 64 rows and two steps ahead, 48 with
+        // 128 and one; 100 tokens: 56 and 47)
+        if (a.qn <= 64) return launch_tile<X, KIND, 2, 2, 2, 0, 2>(w, a, s);
+        return launch_tile<X, KIND, 2, 2, 4, 0, 1>(w, a, s);
+    }
+    int tile = 0;
+    for (int i = 1; i < 3; ++i)
+        if (estimate<X, KIND>(w, a, i) < estimate<X, KIND>(w, a, tile)) tile = i;
+    if (tile == 0) return launch_tile<X, KIND, 2, 4, 8, 2>(w, a, s);
+    if (tile == 1) return launch_tile<X, KIND, 4, 2, 2, 4>(w, a, s);
+    return launch_tile<X, KIND, 2, 2, 2, 3>(w, a, s);
 }
 
 template <class X> hipError_t launch_type(const LayerWork &w, GemmKind kind, const GemmArgs &a, hipStream_t s)
@@ -589,11 +659,9 @@ template <class X> hipError_t launch_type(const LayerWork &w, GemmKind kind, con
     }
 }
 
-// Whether an operand is made of whole 16-byte chunks, as loads straight into
-// LDS need it, near enough to each other for 32-bit offsets within a tile.
-static bool whole_chunks(const void *p, int64_t ld, int64_t contiguous, bool padded)
+bool whole_chunks(const void *p, int64_t ld, int64_t contiguous)
 {
-    return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld <= (1 << 21) && (padded || contiguous % 8 == 0);
+    return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld <= (1 << 21) && contiguous % 8 == 0;
 }
 
 hipError_t launch_gemm(const LayerWork &w, bool bf16, GemmKind kind, GemmArgs a, hipStream_t s)
@@ -606,9 +674,9 @@ hipError_t launch_gemm(const LayerWork &w, bool bf16, GemmKind kind, GemmArgs a,
     const int nq = kind == G_DX ? a.segs : a.batch;
     a.chunks = 1;
     for (int i = 0; i < np; ++i)
-        a.chunks &= whole_chunks(a.p[i], a.ldp[i], pks ? a.pn : a.kn, a.p_padded) && (kind != G_DX || a.ldp[i] == a.ldp[0]);
+        a.chunks &= whole_chunks(a.p[i], a.ldp[i], a.p_padded ? 0 : pks ? a.pn : a.kn) && (kind != G_DX || a.ldp[i] == a.ldp[0]);
     for (int i = 0; i < nq; ++i)
-        a.chunks &= whole_chunks(a.q[i], a.ldq[i], qks ? a.qn : a.kn, a.q_padded) && a.ldq[i] == a.ldq[0];
+        a.chunks &= whole_chunks(a.q[i], a.ldq[i], a.q_padded ? 0 : qks ? a.qn : a.kn) && a.ldq[i] == a.ldq[0];
     return bf16 ? launch_type<Bf16>(w, kind, a, s) : launch_type<Fp16>(w, kind, a, s);
 }
 

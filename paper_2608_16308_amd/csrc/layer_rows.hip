@@ -7,35 +7,12 @@
 
 namespace dbs {
 
-template <class X> struct __attribute__((packed, aligned(2))) Eight {
-    typename X::V8 v;
-};
-template <class X> __device__ __forceinline__ typename X::V8 load_eight(const typename X::T *p)
-{
-    return ((const Eight<X> *)p)->v;
-}
 // (weights pass once: they need not stay in the caches)
 template <class X> __device__ __forceinline__ typename X::V8 load_once(const typename X::T *p)
 {
     typedef typename X::V8 V8u __attribute__((aligned(2)));
     return __builtin_nontemporal_load((const V8u *)p);
 }
-// Elements k .. k + 7 of a row of n >= 8, zeros past its end: what stands at
-// its last eight, moved down.
-template <class X> __device__ __forceinline__ typename X::V8 load_end(const typename X::T *row, int k, int n)
-{
-    const int at = min(k, n - 8), by = k - at;
-    struct Two {
-        uint64_t lo, hi;
-    } v = __builtin_bit_cast(Two, load_eight<X>(row + at));
-    if (by >= 4) v.lo = v.hi, v.hi = 0;
-    const int bits = 16 * (by & 3);
-    v.lo = v.lo >> bits | (v.hi << 1) << (63 - bits);
-    v.hi >>= bits;
-    if (by >= 8) v.lo = v.hi = 0;
-    return __builtin_bit_cast(typename X::V8, v);
-}
-
 // Keeps a projection of token t, a column a lane: in 16 bits, or in 8, where 32
 // neighbouring lanes hold the columns of a group (`in`: one that exists).
 template <class X>

@@ -107,6 +107,11 @@ def check_checkpoint(torch, c, name, dtype, device, rows, cols):
                              f"{t.dtype} {tuple(t.shape)} on {t.device}")
 
 
+def _whole(t, ld):
+    """Whether the rows of a 16-bit tensor start and end at multiples of 16 bytes."""
+    return t.data_ptr() % 16 == 0 and ld % 8 == 0 and t.shape[1] % 8 == 0
+
+
 def _check_apart(out, name, inputs):
     """A caller's output buffer must not overlap an input."""
     def span(t):
@@ -188,6 +193,18 @@ class LayerContext:
                           torch.empty((rows, -(-cols // CK_GROUP)), dtype=torch.uint8, device=self.device), dtype)
 
     # -- forward
+    def _forward_work(self, gated, t, n_in, n_out, *inputs):
+        """(workspace or None, its bytes, its address) for inputs (tensor, ld)
+        that are not in whole 16-byte chunks."""
+        if t <= 1 or all(_whole(v, ld) for v, ld in inputs):
+            return None, 0, None
+        n = ctypes.c_size_t()
+        check(self._fn.dbs_forward_work(self._h, gated, t, n_in, n_out, ctypes.byref(n)))
+        if not n.value:
+            return None, 0, None
+        work = self._torch.empty(n.value, dtype=self._torch.uint8, device=self.device)
+        return work, n.value, work.data_ptr()
+
     def linear(self, x, w, bias=None, act="none", residual=None, save="none", y=None):
         """y = act(x w^T + bias) + residual for x [tokens, n_in] (or one token
         [n_in]), w [n_out, n_in]; y may be preallocated, also as the residual.
@@ -216,10 +233,11 @@ class LayerContext:
         def body():
             out = given if given is not None else self._torch.empty((t, n_out), dtype=x.dtype, device=dev)
             kept, keep = self._keep(save, t, n_out, x.dtype)
+            work, size, at = self._forward_work(0, t, n_in, n_out, (x, ldx), (w, ldw))
             check(self._fn.dbs_linear(
                 self._h, dt, t, n_in, n_out, x.data_ptr(), ldx, w.data_ptr(), ldw,
                 None if bias is None else bias.data_ptr(), act_code, None if residual is None else residual.data_ptr(),
-                ldr, out.data_ptr(), n_out if given is None else ldy, None if keep is None else ctypes.byref(keep)))
+                ldr, out.data_ptr(), n_out if given is None else ldy, None if keep is None else ctypes.byref(keep), at, size))
             return out, kept
         out, kept = self._call(body, (x, w, bias, residual, given))
         out = out[0] if one else out
@@ -250,19 +268,21 @@ class LayerContext:
             out = given if given is not None else self._torch.empty((t, n_out), dtype=x.dtype, device=dev)
             gate, kg = self._keep(save, t, n_out, x.dtype)
             up, ku = self._keep(save, t, n_out, x.dtype)
+            work, size, at = self._forward_work(1, t, n_in, n_out, (x, ldx), (w_gate, ldg), (w_up, ldu))
             check(self._fn.dbs_gated(
                 self._h, dt, t, n_in, n_out, x.data_ptr(), ldx, w_gate.data_ptr(), ldg, w_up.data_ptr(), ldu, act_code,
                 out.data_ptr(), n_out if given is None else ldh, None if kg is None else ctypes.byref(kg),
-                None if ku is None else ctypes.byref(ku)))
+                None if ku is None else ctypes.byref(ku), at, size))
             return out, gate, up
         out, gate, up = self._call(body, (x, w_gate, w_up, given))
         out = out[0] if one else out
         return out if save == "none" else (out, gate, up)
 
     # -- backward
-    def _work(self, gated, act, t, n_in, n_out, x_codes, want_db):
+    def _work(self, gated, act, t, n_in, n_out, x_codes, want_db, *inputs):
         n = ctypes.c_size_t()
-        check(self._fn.dbs_backward_work(self._h, gated, act, t, n_in, n_out, x_codes, want_db, ctypes.byref(n)))
+        whole = n_in % 8 == 0 and all(_whole(v, ld) for v, ld in inputs)
+        check(self._fn.dbs_backward_work(self._h, gated, act, t, n_in, n_out, x_codes, want_db, whole, ctypes.byref(n)))
         return self._torch.empty(n.value, dtype=self._torch.uint8, device=self.device) if n.value else None, n.value
 
     def linear_backward(self, dy, x, w, pre=None, act="none", bias=False, need_dx=True, need_dw=True):
@@ -284,7 +304,8 @@ class LayerContext:
             dx = torch.empty((t, n_in), dtype=dy.dtype, device=dev) if need_dx else None
             dw = torch.empty((n_out, n_in), dtype=dy.dtype, device=dev) if need_dw else None
             db = torch.empty((n_out,), dtype=dy.dtype, device=dev) if bias else None
-            work, size = self._work(0, act_code, t, n_in, n_out, x_codes, 1 if bias else 0)
+            work, size = self._work(0, act_code, t, n_in, n_out, x_codes, 1 if bias else 0, (dy, ldy), (w, ldw),
+                                    *(((x, hx.ld),) if need_dw and not x_codes else ()))
             check(self._fn.dbs_linear_backward(
                 self._h, dt, t, n_in, n_out, dy.data_ptr(), ldy, None if hx is None else ctypes.byref(hx), w.data_ptr(),
                 ldw, None if hp is None else ctypes.byref(hp), act_code, None if dx is None else dx.data_ptr(), n_in,
@@ -311,7 +332,8 @@ class LayerContext:
             dx = torch.empty((t, n_in), dtype=dh.dtype, device=dev) if need_dx else None
             dwg = torch.empty((n_out, n_in), dtype=dh.dtype, device=dev) if need_dw else None
             dwu = torch.empty((n_out, n_in), dtype=dh.dtype, device=dev) if need_dw else None
-            work, size = self._work(1, act_code, t, n_in, n_out, x_codes, 0)
+            work, size = self._work(1, act_code, t, n_in, n_out, x_codes, 0, (w_gate, ldg), (w_up, ldu),
+                                    *(((x, hx.ld),) if need_dw and not x_codes else ()))
             check(self._fn.dbs_gated_backward(
                 self._h, dt, t, n_in, n_out, dh.data_ptr(), ldh, None if hx is None else ctypes.byref(hx),
                 w_gate.data_ptr(), ldg, w_up.data_ptr(), ldu, ctypes.byref(hg), ctypes.byref(hu), act_code,

@@ -84,10 +84,12 @@ H = lambda *v: ctypes.byref(_lib.Held(*v))
 full, held = H(p, 16, None, None), H(None, 0, p, p)
 BF, NONE, SILU = 3, 0, 2
 
-def linear(L=L, dt=BF, t=4, n=16, m=8, x=p, ldx=16, w=p, ldw=16, b=p, act=SILU, r=p, ldr=8, y=p, ldy=8, pre=None):
-    return lib.dbs_linear(L, dt, t, n, m, x, ldx, w, ldw, b, act, r, ldr, y, ldy, pre)
-def gated(L=L, dt=BF, t=4, n=16, m=8, x=p, ldx=16, g=p, ldg=16, u=p, ldu=16, act=SILU, h=p, ldh=8, kg=None, ku=None):
-    return lib.dbs_gated(L, dt, t, n, m, x, ldx, g, ldg, u, ldu, act, h, ldh, kg, ku)
+def linear(L=L, dt=BF, t=4, n=16, m=8, x=p, ldx=16, w=p, ldw=16, b=p, act=SILU, r=p, ldr=8, y=p, ldy=8, pre=None,
+           work=None, size=0):
+    return lib.dbs_linear(L, dt, t, n, m, x, ldx, w, ldw, b, act, r, ldr, y, ldy, pre, work, size)
+def gated(L=L, dt=BF, t=4, n=16, m=8, x=p, ldx=16, g=p, ldg=16, u=p, ldu=16, act=SILU, h=p, ldh=8, kg=None, ku=None,
+          work=None, size=0):
+    return lib.dbs_gated(L, dt, t, n, m, x, ldx, g, ldg, u, ldu, act, h, ldh, kg, ku, work, size)
 def lback(L=L, dt=BF, t=4, n=16, m=8, dy=p, lddy=8, x=full, w=p, ldw=16, pre=H(p, 8, None, None), act=SILU, dx=p, lddx=16, dw=p,
           lddw=16, db=p, work=4096, size=1 << 20):
     return lib.dbs_linear_backward(L, dt, t, n, m, dy, lddy, x, w, ldw, pre, act, dx, lddx, dw, lddw, db, work, size)
@@ -102,7 +104,7 @@ odd = p + 1
 bad = [(linear, d) for d in (dict(L=None), dict(dt=0), dict(dt=2), dict(dt=7), dict(t=-1), dict(n=-1), dict(m=-1), dict(x=None),
        dict(x=odd), dict(ldx=15), dict(w=None), dict(ldw=15), dict(b=odd), dict(act=5), dict(act=-1), dict(ldr=7), dict(y=None),
        dict(ldy=7), dict(pre=H(p, 8, p, p)), dict(pre=H(None, 0, p, None)), dict(pre=H(None, 0, None, None)),
-       dict(pre=H(p, 7, None, None)))]
+       dict(pre=H(p, 7, None, None)), dict(work=4097, size=64))]
 bad += [(gated, d) for d in (dict(L=None), dict(dt=1 << 8), dict(g=None), dict(u=None), dict(ldu=3), dict(h=None), dict(ldh=1),
         dict(kg=full), dict(ku=full), dict(kg=H(p, 8, None, None), ku=held), dict(act=9), dict(t=-5))]
 bad += [(lback, d) for d in (dict(L=None), dict(dt=0), dict(dy=None), dict(lddy=7), dict(x=None), dict(x=H(p, 15, None, None)),
@@ -116,8 +118,10 @@ for f, d in bad:
     assert lib.dbs_last_error()
 assert linear(n=(1 << 30) + 1, ldx=1 << 31, ldw=1 << 31) == 4
 size = ctypes.c_size_t()
-assert lib.dbs_backward_work(L, 0, SILU, -1, 1, 1, 0, 0, ctypes.byref(size)) == 1
-assert lib.dbs_backward_work(L, 0, SILU, 1, 1, 1, 0, 0, None) == 1
+assert lib.dbs_backward_work(L, 0, SILU, -1, 1, 1, 0, 0, 0, ctypes.byref(size)) == 1
+assert lib.dbs_backward_work(L, 0, SILU, 1, 1, 1, 0, 0, 0, None) == 1
+assert lib.dbs_forward_work(None, 0, 1, 1, 1, ctypes.byref(size)) == 1
+assert lib.dbs_forward_work(L, 0, 1, 1, 1, None) == 1
 for name, args in (("dbs_pack", (p, 16, p, p)), ("dbs_unpack", (p, p, p, 16))):
     f = getattr(lib, name)
     assert f(L, BF, 4, 16, *args) == 0
