@@ -530,12 +530,14 @@ __global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_block(GemmArgs a)
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[m][j] = X::mma(fp[s][j], fq[s][m], acc[m][j]);
+        if constexpr (!C::PKS) {
 #pragma unroll
         for (int i = 0; i < READS; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an LDS read
             __builtin_amdgcn_sched_group_barrier(0x8, EACH, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x8, MMAS - READS * EACH, 0);
+        }
         __builtin_amdgcn_sched_barrier(0);
     };
 
