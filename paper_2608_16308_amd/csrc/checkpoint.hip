@@ -12,9 +12,6 @@ namespace dbs {
 template <class X> struct __attribute__((packed, aligned(2))) Vals8 {
     typename X::V8 v;
 };
-struct __attribute__((packed, aligned(1))) Codes8 {
-    uint32_t w[2];
-};
 
 template <class X>
 __device__ __forceinline__ void load_vals(const typename X::T *p, int left, float (&v)[8])
@@ -49,115 +46,129 @@ __device__ __forceinline__ Codes8 load_codes(const int8_t *p, int left)
         if (i < left) c.w[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
     return c;
 }
-template <class X> __device__ __forceinline__ void decode8(Codes8 c, int e, float (&v)[8])
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = ck_value<X>((int)(int8_t)(c.w[i >> 2] >> (8 * (i & 3))), e);
-}
-
 constexpr int CK_TPB = 256;
-constexpr int CK_U = 4;  // chunks in flight per thread
+constexpr int CK_U = 2;      // chunks in flight per thread
+constexpr int CK_CHUNK = 16; // columns of a chunk
 
-// A thread takes chunks of eight columns, the four of a group in neighbouring
+// The chunks of a thread: from row to row in steps of the whole grid, with one
+// division at the start.
+struct Walk {
+    int32_t row, chunk;
+    __device__ Walk(uint32_t per, uint32_t first) : row((int32_t)(first / per)), chunk((int32_t)(first % per)) {}
+    __device__ void step(const int32_t rows_on, const int32_t chunks_on, const int32_t per)
+    {
+        row += rows_on;
+        chunk += chunks_on;
+        if (chunk >= per) chunk -= per, ++row;
+    }
+};
+// per: chunks of a row; rows_on, chunks_on: the grid's threads in rows and chunks
+struct Grid {
+    int32_t rows, cols, per, rows_on, chunks_on;
+};
+
+struct __attribute__((packed, aligned(1))) Codes16 {
+    uint32_t w[4];
+};
+// A thread takes chunks of 16 columns, the two of a group in neighbouring
 // lanes; a row's chunks are counted up to a whole group.
+//
+// Bound: by the bytes (2 in, 33/32 out per value).
 template <class X>
-__global__ __launch_bounds__(CK_TPB) void k_pack(const typename X::T *__restrict__ x, int64_t ldx, int32_t rows,
-                                                 int32_t cols, int8_t *__restrict__ codes, uint8_t *__restrict__ exps)
+__global__ __launch_bounds__(CK_TPB) void k_pack(const typename X::T *__restrict__ x, int64_t ldx, Grid g,
+                                                 int8_t *__restrict__ codes, uint8_t *__restrict__ exps)
 {
-    const uint32_t groups = (uint32_t)((cols + CK_GROUP - 1) / CK_GROUP), per = 4 * groups;
-    const uint64_t total = (uint64_t)rows * per, stride = (uint64_t)gridDim.x * CK_TPB;
-    for (uint64_t i0 = (uint64_t)blockIdx.x * CK_TPB + threadIdx.x; i0 < total; i0 += CK_U * stride) {
-        float v[CK_U][8];
+    const int64_t groups = g.per / 2;
+    for (Walk at((uint32_t)g.per, blockIdx.x * CK_TPB + threadIdx.x); at.row < g.rows;) {
+        float v[CK_U][16];
         int32_t row[CK_U], col[CK_U];
 #pragma unroll
-        for (int u = 0; u < CK_U; ++u) {
-            const uint64_t i = i0 + u * stride;
-            row[u] = i < total ? (int32_t)(i / per) : -1;
-            col[u] = 8 * (int32_t)(i - (uint64_t)(uint32_t)row[u] * per);
-            load_vals<X>(x + (int64_t)row[u] * ldx + col[u], row[u] < 0 ? 0 : cols - col[u], v[u]);
+        for (int u = 0; u < CK_U; ++u, at.step(g.rows_on, g.chunks_on, g.per)) {
+            row[u] = at.row, col[u] = CK_CHUNK * at.chunk;
+            const int left = row[u] < g.rows ? g.cols - col[u] : 0;
+            const typename X::T *p = x + (int64_t)row[u] * ldx + col[u];
+            float lo[8], hi[8];
+            load_vals<X>(p, left, lo);
+            load_vals<X>(p + 8, left - 8, hi);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[u][k] = lo[k], v[u][8 + k] = hi[k];
         }
 #pragma unroll
         for (int u = 0; u < CK_U; ++u) {
             float big = 0.f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) big = fmaxf(big, ck_mag(v[u][k]));
+            for (int k = 0; k < 16; ++k) big = fmaxf(big, ck_mag(v[u][k]));
             big = fmaxf(big, __shfl_xor(big, 1, 64));
-            big = fmaxf(big, __shfl_xor(big, 2, 64));
-            if (row[u] < 0 || col[u] >= cols) continue;
+            const int left = g.cols - col[u];
+            if (row[u] >= g.rows || left <= 0) continue;
             const int e = ck_exp<X>(big);
-            if (col[u] % CK_GROUP == 0) exps[(int64_t)row[u] * groups + col[u] / CK_GROUP] = (uint8_t)(e + CK_BIAS);
-            int8_t *dst = codes + (int64_t)row[u] * cols + col[u];
-            Codes8 c = {{0u, 0u}};
+            if (col[u] % CK_GROUP == 0) exps[row[u] * groups + col[u] / CK_GROUP] = (uint8_t)(e + CK_BIAS);
+            int8_t *dst = codes + (int64_t)row[u] * g.cols + col[u];
+            Codes16 c = {{0u, 0u, 0u, 0u}};
 #pragma unroll
-            for (int k = 0; k < 8; ++k) c.w[k >> 2] |= (uint32_t)(ck_code(v[u][k], e) & 255) << (8 * (k & 3));
-            const int left = cols - col[u];
-            if (left >= 8) *(Codes8 *)dst = c;
+            for (int k = 0; k < 16; ++k) c.w[k >> 2] |= (uint32_t)(ck_code(v[u][k], e) & 255) << (8 * (k & 3));
+            if (left >= 16) *(Codes16 *)dst = c;
             else
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int k = 0; k < 16; ++k)
                     if (k < left) dst[k] = (int8_t)(c.w[k >> 2] >> (8 * (k & 3)));
         }
     }
 }
 
+// Chunks of eight columns here: a lane's 16 bytes lie beside its neighbours'.
 template <class X>
-__global__ __launch_bounds__(CK_TPB) void k_unpack(const int8_t *__restrict__ codes, const uint8_t *__restrict__ exps,
-                                                   int32_t rows, int32_t cols, typename X::T *__restrict__ y,
-                                                   int64_t ldy)
+__global__ __launch_bounds__(CK_TPB) void k_unpack(const int8_t *__restrict__ codes, const uint8_t *__restrict__ exps, Grid g,
+                                                   typename X::T *__restrict__ y, int64_t ldy)
 {
-    const uint32_t groups = (uint32_t)((cols + CK_GROUP - 1) / CK_GROUP), per = (uint32_t)((cols + 7) / 8);
-    const uint64_t total = (uint64_t)rows * per, stride = (uint64_t)gridDim.x * CK_TPB;
-    for (uint64_t i0 = (uint64_t)blockIdx.x * CK_TPB + threadIdx.x; i0 < total; i0 += CK_U * stride) {
-        Codes8 c[CK_U];
-        int e[CK_U];
-        int32_t row[CK_U], col[CK_U];
+    constexpr int U = 2 * CK_U;
+    const int64_t groups = (g.cols + CK_GROUP - 1) / CK_GROUP;
+    for (Walk at((uint32_t)g.per, blockIdx.x * CK_TPB + threadIdx.x); at.row < g.rows;) {
+        Codes8 c[U];
+        int e[U];
+        int32_t row[U], col[U];
 #pragma unroll
-        for (int u = 0; u < CK_U; ++u) {
-            const uint64_t i = i0 + u * stride;
-            row[u] = i < total ? (int32_t)(i / per) : -1;
-            col[u] = 8 * (int32_t)(i - (uint64_t)(uint32_t)row[u] * per);
-            if (row[u] < 0) continue;
-            c[u] = load_codes(codes + (int64_t)row[u] * cols + col[u], cols - col[u]);
-            e[u] = (int)exps[(int64_t)row[u] * groups + col[u] / CK_GROUP] - CK_BIAS;
+        for (int u = 0; u < U; ++u, at.step(g.rows_on, g.chunks_on, g.per)) {
+            row[u] = at.row, col[u] = 8 * at.chunk;
+            if (row[u] >= g.rows) continue;
+            c[u] = load_codes(codes + (int64_t)row[u] * g.cols + col[u], g.cols - col[u]);
+            e[u] = (int)exps[row[u] * groups + col[u] / CK_GROUP] - CK_BIAS;
         }
 #pragma unroll
-        for (int u = 0; u < CK_U; ++u) {
-            if (row[u] < 0) continue;
+        for (int u = 0; u < U; ++u) {
+            if (row[u] >= g.rows) continue;
             float v[8];
-            decode8<X>(c[u], e[u], v);
-            store_vals<X>(y + (int64_t)row[u] * ldy + col[u], cols - col[u], v);
+            ck_values<X>(c[u], e[u], v);
+            store_vals<X>(y + (int64_t)row[u] * ldy + col[u], g.cols - col[u], v);
         }
     }
 }
 
 // (bits only: one kernel for both types)
-__global__ __launch_bounds__(CK_TPB) void k_align(const _Float16 *__restrict__ src, int64_t ld, int32_t rows, int32_t cols,
-                                                  uint4 *__restrict__ dst, int64_t ldd)
+__global__ __launch_bounds__(CK_TPB) void k_align(const _Float16 *__restrict__ src, int64_t ld, Grid g, uint4 *__restrict__ dst,
+                                                  int64_t ldd)
 {
-    const uint32_t per = (uint32_t)((cols + 7) / 8);
-    const uint64_t total = (uint64_t)rows * per, stride = (uint64_t)gridDim.x * CK_TPB;
-    for (uint64_t i0 = (uint64_t)blockIdx.x * CK_TPB + threadIdx.x; i0 < total; i0 += CK_U * stride) {
-        Fp16::V8 v[CK_U];
-        int64_t at[CK_U];
+    for (Walk at((uint32_t)g.per, blockIdx.x * CK_TPB + threadIdx.x); at.row < g.rows;) {
+        Fp16::V8 v[2 * CK_U];
+        int32_t row[2 * CK_U], chunk[2 * CK_U];
 #pragma unroll
-        for (int u = 0; u < CK_U; ++u) {
-            const uint64_t i = i0 + u * stride < total ? i0 + u * stride : total - 1;
-            const int32_t row = (int32_t)(i / per), col = 8 * (int32_t)(i - (uint64_t)row * per);
-            const _Float16 *p = src + (int64_t)row * ld;
-            if (cols >= 8) v[u] = load_end<Fp16>(p, col, cols);
+        for (int u = 0; u < 2 * CK_U; ++u, at.step(g.rows_on, g.chunks_on, g.per)) {
+            row[u] = at.row, chunk[u] = at.chunk;
+            const _Float16 *p = src + (int64_t)min(row[u], g.rows - 1) * ld;
+            if (g.cols >= 8) v[u] = load_end<Fp16>(p, 8 * chunk[u], g.cols);
             else
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[u][k] = k < cols ? p[min(k, cols - 1)] : (_Float16)0.f;
-            at[u] = ((int64_t)row * ldd + col) / 8;
+                for (int k = 0; k < 8; ++k) v[u][k] = k < g.cols ? p[min(k, g.cols - 1)] : (_Float16)0.f;
         }
 #pragma unroll
-        for (int u = 0; u < CK_U; ++u)
-            if (i0 + u * stride < total) dst[at[u]] = __builtin_bit_cast(uint4, v[u]);
+        for (int u = 0; u < 2 * CK_U; ++u)
+            if (row[u] < g.rows) dst[(int64_t)row[u] * (ldd / 8) + chunk[u]] = __builtin_bit_cast(uint4, v[u]);
     }
 }
 
 constexpr int SL_WAVES = 4;                // waves of a workgroup, each a row at a time
 constexpr int SL_COLS = 64 * 8;            // columns of a workgroup
+constexpr int SUM_WAVES = 16;
 
 // The sums of the columns are added in a fixed order: a lane's rows, the
 // waves, then the workgroups along the rows (k_slope_sum).
@@ -172,32 +183,30 @@ __global__ __launch_bounds__(64 * SL_WAVES) void k_slope(SlopeArgs a)
     const int r1 = (int)((int64_t)a.rows * (blockIdx.y + 1) / a.row_blocks);
     const int64_t groups = (a.cols + CK_GROUP - 1) / CK_GROUP;
     auto held = [&](const HeldIn &h, int row, float (&v)[8]) {
-        if (h.codes) decode8<X>(load_codes(h.codes + (int64_t)row * a.cols + col, left),
+        if (h.codes) ck_values<X>(load_codes(h.codes + (int64_t)row * a.cols + col, left),
                                 (int)h.exps[row * groups + col / CK_GROUP] - CK_BIAS, v);
         else load_vals<X>((const T *)h.full + (int64_t)row * h.ld + col, left, v);
     };
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (left > 0)
         for (int row = r0 + wave; row < r1; row += SL_WAVES) {
-            float dy[8], z[8], up[8], du[8];
+            float dy[8], z[8], up[8], f[8], d[8], dz[8], du[8];
             load_vals<X>((const T *)a.dy + (int64_t)row * a.lddy + col, left, dy);
             if (a.pre.codes || a.pre.full) held(a.pre, row, z);
             else
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = 0.f;
             if (GATED) held(a.up, row, up);
+            act_slopes(a.act, z, f, d);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                float f;
-                const float d = act_slope(a.act, z[i], f);
-                if (GATED) du[i] = dy[i] * f;
                 // (columns past the last: the zeros that fill the row)
-                z[i] = i < left ? (GATED ? dy[i] * up[i] * d : dy[i] * d) : 0.f;
-                if (GATED && i >= left) du[i] = 0.f;
-                sum[i] += z[i];
+                if (GATED) du[i] = i < left ? dy[i] * f[i] : 0.f;
+                dz[i] = i < left ? (GATED ? dy[i] * up[i] : dy[i]) * d[i] : 0.f;
+                sum[i] += dz[i];
             }
             if (a.dz) {
-                store_vals<X>((T *)a.dz + (int64_t)row * a.ldz + col, 8, z);
+                store_vals<X>((T *)a.dz + (int64_t)row * a.ldz + col, 8, dz);
                 if (GATED) store_vals<X>((T *)a.du + (int64_t)row * a.ldz + col, 8, du);
             }
         }
@@ -216,61 +225,64 @@ __global__ __launch_bounds__(64 * SL_WAVES) void k_slope(SlopeArgs a)
     }
 }
 
+// The workgroups' sums, a column a lane, the rows shared out to the waves.
 template <class X>
-__global__ __launch_bounds__(256) void k_slope_sum(const float *__restrict__ sums, int32_t n, int32_t cols,
-                                                   typename X::T *__restrict__ db)
+__global__ __launch_bounds__(64 * SUM_WAVES) void k_slope_sum(const float *__restrict__ sums, int32_t n, int32_t cols,
+                                                              typename X::T *__restrict__ db)
 {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= cols) return;
+    __shared__ float part[SUM_WAVES][64];
+    const int lane = lane_id(), wave = wave_id(), c = (int)blockIdx.x * 64 + lane;
     float s = 0.f;
-    for (int i = 0; i < n; ++i) s += sums[i * (int64_t)cols + c];
+    if (c < cols)
+#pragma unroll 4
+        for (int i = wave; i < n; i += SUM_WAVES) s += sums[i * (int64_t)cols + c];
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || c >= cols) return;
+#pragma unroll
+    for (int w = 1; w < SUM_WAVES; ++w) s += part[w][lane];
     db[c] = (typename X::T)s;
 }
 
-static unsigned chunk_grid(uint64_t chunks, int32_t cus)
+// A grid over rows of `per` chunks: a thread per chunk, or as many as are
+// resident at once.
+static Grid chunk_grid(int32_t rows, int32_t cols, int32_t per, int32_t cus, unsigned *blocks)
 {
-    return (unsigned)std::min<uint64_t>((chunks + CK_TPB - 1) / CK_TPB, (uint64_t)cus * 8);
+    const uint64_t chunks = (uint64_t)rows * per;
+    *blocks = (unsigned)std::max<uint64_t>(1, std::min<uint64_t>((chunks + CK_TPB - 1) / CK_TPB, (uint64_t)cus * 8));
+    const uint32_t threads = *blocks * CK_TPB;
+    return Grid{rows, cols, per, (int32_t)(threads / (uint32_t)per), (int32_t)(threads % (uint32_t)per)};
 }
 
-template <class X>
-static hipError_t pack_t(const void *x, int64_t ldx, int32_t rows, int32_t cols, int8_t *codes, uint8_t *exps, int32_t cus,
-                         hipStream_t s)
-{
-    const uint64_t chunks = (uint64_t)rows * 4 * ((cols + CK_GROUP - 1) / CK_GROUP);
-    hipLaunchKernelGGL(k_pack<X>, dim3(chunk_grid(chunks, cus)), dim3(CK_TPB), 0, s, (const typename X::T *)x, ldx, rows,
-                       cols, codes, exps);
-    return hipGetLastError();
-}
 hipError_t launch_pack(bool bf16, const void *x, int64_t ldx, int32_t rows, int32_t cols, int8_t *codes, uint8_t *exps,
                        int32_t cus, hipStream_t s)
 {
     if (rows == 0 || cols == 0) return hipSuccess;
-    return bf16 ? pack_t<Bf16>(x, ldx, rows, cols, codes, exps, cus, s) : pack_t<Fp16>(x, ldx, rows, cols, codes, exps, cus, s);
-}
-
-template <class X>
-static hipError_t unpack_t(const int8_t *codes, const uint8_t *exps, int32_t rows, int32_t cols, void *y, int64_t ldy,
-                           int32_t cus, hipStream_t s)
-{
-    const uint64_t chunks = (uint64_t)rows * ((cols + 7) / 8);
-    hipLaunchKernelGGL(k_unpack<X>, dim3(chunk_grid(chunks, cus)), dim3(CK_TPB), 0, s, codes, exps, rows, cols,
-                       (typename X::T *)y, ldy);
+    unsigned n;
+    const Grid g = chunk_grid(rows, cols, 2 * ((cols + CK_GROUP - 1) / CK_GROUP), cus, &n);
+    if (bf16) hipLaunchKernelGGL(k_pack<Bf16>, dim3(n), dim3(CK_TPB), 0, s, (const Bf16::T *)x, ldx, g, codes, exps);
+    else hipLaunchKernelGGL(k_pack<Fp16>, dim3(n), dim3(CK_TPB), 0, s, (const Fp16::T *)x, ldx, g, codes, exps);
     return hipGetLastError();
 }
+
 hipError_t launch_unpack(bool bf16, const int8_t *codes, const uint8_t *exps, int32_t rows, int32_t cols, void *y,
                          int64_t ldy, int32_t cus, hipStream_t s)
 {
     if (rows == 0 || cols == 0) return hipSuccess;
-    return bf16 ? unpack_t<Bf16>(codes, exps, rows, cols, y, ldy, cus, s) : unpack_t<Fp16>(codes, exps, rows, cols, y, ldy, cus, s);
+    unsigned n;
+    const Grid g = chunk_grid(rows, cols, (cols + 7) / 8, cus, &n);
+    if (bf16) hipLaunchKernelGGL(k_unpack<Bf16>, dim3(n), dim3(CK_TPB), 0, s, codes, exps, g, (Bf16::T *)y, ldy);
+    else hipLaunchKernelGGL(k_unpack<Fp16>, dim3(n), dim3(CK_TPB), 0, s, codes, exps, g, (Fp16::T *)y, ldy);
+    return hipGetLastError();
 }
 
 hipError_t launch_align(const void *src, int64_t ld, int32_t rows, int32_t cols, void *dst, int64_t ldd, int32_t cus,
                         hipStream_t s)
 {
     if (rows == 0 || cols == 0) return hipSuccess;
-    const uint64_t chunks = (uint64_t)rows * ((cols + 7) / 8);
-    hipLaunchKernelGGL(k_align, dim3(chunk_grid(chunks, cus)), dim3(CK_TPB), 0, s, (const _Float16 *)src, ld, rows, cols,
-                       (uint4 *)dst, ldd);
+    unsigned n;
+    const Grid g = chunk_grid(rows, cols, (cols + 7) / 8, cus, &n);
+    hipLaunchKernelGGL(k_align, dim3(n), dim3(CK_TPB), 0, s, (const _Float16 *)src, ld, g, (uint4 *)dst, ldd);
     return hipGetLastError();
 }
 
@@ -290,7 +302,7 @@ template <class X> static hipError_t slope_t(bool gated, const SlopeArgs &a, hip
     else hipLaunchKernelGGL((k_slope<X, false>), grid, block, 0, s, a);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.sums) {
-        hipLaunchKernelGGL(k_slope_sum<X>, dim3((unsigned)((a.cols + 255) / 256)), dim3(256), 0, s, a.sums, a.row_blocks,
+        hipLaunchKernelGGL(k_slope_sum<X>, dim3((unsigned)((a.cols + 63) / 64)), dim3(64 * SUM_WAVES), 0, s, a.sums, a.row_blocks,
                            a.cols, (typename X::T *)a.db);
         e = hipGetLastError();
     }

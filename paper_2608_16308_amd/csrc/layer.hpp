@@ -95,27 +95,32 @@ template <int N> __device__ __forceinline__ void act_values(Act f, float (&v)[N]
         for (int i = 0; i < N; ++i) v[i] = v[i] * logistic(v[i] * (f.a + f.b * v[i] * v[i]));
     }
 }
-// act(z) and act'(z).
-__device__ __forceinline__ float act_slope(Act f, float z, float &value)
+// act(z) and act'(z) of N values.
+template <int N> __device__ __forceinline__ void act_slopes(Act f, const float (&z)[N], float (&value)[N], float (&slope)[N])
 {
     if (f.kind == DBS_ACT_NONE) {
-        value = z;
-        return 1.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) value[i] = z[i], slope[i] = 1.f;
+    } else if (f.kind == DBS_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) value[i] = z[i] < 0.f ? 0.f : z[i], slope[i] = z[i] > 0.f ? 1.f : 0.f;
+    } else if (f.kind == DBS_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float c = 0.5f * (1.f + erff(z[i] * 0.70710678118654752f));
+            value[i] = z[i] * c;
+            slope[i] = c + z[i] * __expf(-0.5f * z[i] * z[i]) * 0.39894228040143268f;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float zz = z[i] * z[i], s = logistic(z[i] * (f.a + f.b * zz));
+            value[i] = z[i] * s;
+            // (where s is 0 or 1 the second term is 0, also where z^3 overflows)
+            const float d = s * (1.f - s), t = z[i] * d * (f.a + 3.f * f.b * zz);
+            slope[i] = s + (d == 0.f ? 0.f : t);
+        }
     }
-    if (f.kind == DBS_ACT_RELU) {
-        value = z < 0.f ? 0.f : z;
-        return z > 0.f ? 1.f : 0.f;
-    }
-    if (f.kind == DBS_ACT_GELU) {
-        const float c = 0.5f * (1.f + erff(z * 0.70710678118654752f));
-        value = z * c;
-        return c + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
-    }
-    const float s = logistic(z * (f.a + f.b * z * z));
-    value = z * s;
-    // (where s is 0 or 1 the second term is 0, also where z^3 overflows)
-    const float d = s * (1.f - s);
-    return s + (d == 0.f ? 0.f : z * d * (f.a + 3.f * f.b * z * z));
 }
 
 // ---------------------------------------------------------------------------
@@ -150,13 +155,28 @@ __device__ __forceinline__ int ck_code(float v, int e)
     const float c = __builtin_rintf(__builtin_amdgcn_ldexpf(v, -e));
     return __builtin_fabsf(v) <= 3.402823466e38f ? (int)c : -128;
 }
-// The largest group magnitudes reach 64 * 2^e = 2^(e + 6) beyond the type's
-// largest number: such values come back as that number.
-template <class X> __device__ __forceinline__ float ck_value(int code, int e)
+// The values of eight codes of a group.  The largest magnitudes reach 64 * 2^e =
+// 2^(e + 6) beyond the type's largest number: such values come back as that
+// number.
+struct __attribute__((packed, aligned(1))) Codes8 {
+    uint32_t w[2];
+};
+template <class X> __device__ __forceinline__ void ck_values(Codes8 c, int e, float (&v)[8])
 {
-    const float v = __builtin_amdgcn_ldexpf((float)code, e);
-    const float w = __builtin_fminf(__builtin_fmaxf(v, -X::MAX), X::MAX);
-    return code == -128 ? __builtin_nanf("") : w;
+    const float scale = __builtin_amdgcn_ldexpf(1.f, e);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t w = c.w[h] ^ 0x80808080u;  // code + 128
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float code = (float)((w >> (8 * i)) & 255u) - 128.f;
+            v[4 * h + i] = __builtin_amdgcn_fmed3f(code * scale, -X::MAX, X::MAX);
+        }
+        if ((w - 0x01010101u) & ~w & 0x80808080u)  // a code of -128
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (((w >> (8 * i)) & 255u) == 0u) v[4 * h + i] = __builtin_nanf("");
+    }
 }
 
 // ---------------------------------------------------------------------------
