@@ -22,6 +22,7 @@ ACTS = {"none": _lib.DBS_ACT_NONE, "relu": _lib.DBS_ACT_RELU, "silu": _lib.DBS_A
         "gelu_tanh": _lib.DBS_ACT_GELU_TANH}
 SAVES = ("none", "full", "8bit")
 CK_GROUP = _lib.DBS_CK_GROUP
+ROWS_TOKENS = 16  # forward calls of so few tokens use no workspace
 
 
 class Checkpoint:
@@ -112,16 +113,30 @@ def _whole(t, ld):
     return t.data_ptr() % 16 == 0 and ld % 8 == 0 and t.shape[1] % 8 == 0
 
 
+def _span(t):
+    n = 0 if t.numel() == 0 else 1 + sum((s - 1) * st for s, st in zip(t.shape, t.stride()))
+    return t.data_ptr(), t.data_ptr() + n * t.element_size()
+
+
+def _side_by_side(a, b):
+    """Whether two tensors are columns of one buffer that do not meet."""
+    if a.dim() != 2 or b.dim() != 2 or a.stride(0) != b.stride(0) or a.element_size() != b.element_size():
+        return False
+    row, size = a.stride(0), a.element_size()
+    far = b.data_ptr() - a.data_ptr()
+    if row <= 0 or far % size:
+        return False
+    at = far // size % row  # where b's rows begin in a's
+    return at >= a.shape[1] and at + b.shape[1] <= row
+
+
 def _check_apart(out, name, inputs):
     """A caller's output buffer must not overlap an input."""
-    def span(t):
-        n = 0 if t.numel() == 0 else 1 + sum((s - 1) * st for s, st in zip(t.shape, t.stride()))
-        return t.data_ptr(), t.data_ptr() + n * t.element_size()
-    a, b = span(out)
+    a, b = _span(out)
     for t, what in inputs:
         if t is not None:
-            c, d = span(t)
-            if a < d and c < b:
+            c, d = _span(t)
+            if a < d and c < b and not _side_by_side(out, t):
                 raise _arg_error(f"{name} overlaps {what}")
 
 
@@ -196,7 +211,7 @@ class LayerContext:
     def _forward_work(self, gated, t, n_in, n_out, *inputs):
         """(workspace or None, its bytes, its address) for inputs (tensor, ld)
         that are not in whole 16-byte chunks."""
-        if t <= 1 or all(_whole(v, ld) for v, ld in inputs):
+        if t <= ROWS_TOKENS or all(_whole(v, ld) for v, ld in inputs):
             return None, 0, None
         n = ctypes.c_size_t()
         check(self._fn.dbs_forward_work(self._h, gated, t, n_in, n_out, ctypes.byref(n)))
@@ -367,6 +382,8 @@ class LayerContext:
         rows, cols = c.codes.shape
         check_checkpoint(torch, c, "c", c.dtype, self.device, rows, cols)
         ld = cols if y is None else check_rows(y, "y", c.dtype, self.device, rows, cols)
+        if y is not None:
+            _check_apart(y, "y", ((c.codes, "the codes of c"), (c.exponents, "the exponents of c")))
 
         def body():
             out = torch.empty((rows, cols), dtype=c.dtype, device=self.device) if y is None else y

@@ -158,6 +158,80 @@ def test_strides_and_alignment(ctx, size, pad, offset, dt):
         ref.check(v, *want[name], name)
 
 
+# tokens on either side of each kernel's range, sums of a turn, of several and
+# of a ragged one, rows that are shorter than a load
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("n", [7, 8, 9, 255, 256, 264, 2049, 4100])
+@pytest.mark.parametrize("t", [1, 2, 5, 15, 16, 17, 33, 64, 65])
+def test_few_tokens(ctx, t, n, dt):
+    m = 70
+    g = gen(t * 31 + n)
+    log(f"few tokens {t} {n} {dt}")
+    x, w, wu = rnd(g, (t, n), dt), rnd(g, (m, n), dt, n ** -0.5), rnd(g, (m, n), dt, n ** -0.5)
+    bias, res = rnd(g, (1, m), dt)[0], rnd(g, (t, m), dt)
+    y, ey, z, ez = ref.linear(x, w, bias, "silu", res)
+    got, pre = ctx.linear(x, w, bias=bias, act="silu", residual=res, save="full")
+    ref.check(got, y, ey, "linear")
+    ref.check(pre, z, ez, "pre")
+    got8, pre8 = ctx.linear(x, w, bias=bias, act="silu", residual=res, save="8bit")
+    assert torch.equal(got8, got) and torch.equal(pre8.codes.cpu(), ref.pack(pre.cpu())[0])
+    h, eh = ref.gated(x, w, wu, "gelu")[:2]
+    got, gate, up = ctx.gated(x, w, wu, act="gelu", save="full")
+    ref.check(got, h, eh, "gated")
+    got8, g8, u8 = ctx.gated(x, w, wu, act="gelu", save="8bit")
+    assert torch.equal(got8, got)
+    for full, held in ((gate, g8), (up, u8)):
+        codes, exps = ref.pack(full.cpu())
+        assert torch.equal(held.codes.cpu(), codes) and torch.equal(held.exponents.cpu(), exps)
+    if t == 1:
+        assert torch.equal(ctx.linear(x[0], w, bias=bias, act="silu", residual=res[0]), ctx.linear(x, w, bias=bias, act="silu", residual=res)[0])
+        assert torch.equal(ctx.gated(x[0], w, wu, act="gelu"), got[0])
+
+
+# rounds of whole tiles with a rest in parts, several rows and columns of tiles,
+# operands in whole chunks, in odd places and copied from there
+@pytest.mark.parametrize("size", [(1024, 4096, 1032), (520, 2056, 4104), (300, 4099, 1500), (700, 3001, 2003), (90, 8200, 600)], ids=str)
+def test_larger_products(ctx, size):
+    t, n, m = size
+    dt = torch.bfloat16
+    g = gen(sum(size))
+    log(f"larger {size}")
+    x, w, wu, dy = rnd(g, (t, n), dt), rnd(g, (m, n), dt, n ** -0.5), rnd(g, (m, n), dt, n ** -0.5), rnd(g, (t, m), dt)
+    res = rnd(g, (t, m), dt)
+    y, ey, _, _ = ref.linear(x, w, None, "gelu_tanh", res)
+    ref.check(ctx.linear(x, w, act="gelu_tanh", residual=res), y, ey, "linear")
+    h, eh, gate, eg, up, eu = ref.gated(x, w, wu, "silu")
+    got, kg, ku = ctx.gated(x, w, wu, save="full")
+    ref.check(got, h, eh, "gated")
+    ref.check(kg, gate, eg, "gate")
+    ref.check(ku, up, eu, "up")
+    want = ref.gated_backward(dy, x.double(), w, wu, kg.double(), ku.double(), "silu")
+    for name, v in zip(("dx", "dw_gate", "dw_up"), ctx.gated_backward(dy, x, w, wu, kg, ku)):
+        ref.check(v, *want[name], name)
+    want = ref.linear_backward(dy, x.double(), w, None, "none")
+    for name, v in zip(("dx", "dw", "db"), ctx.linear_backward(dy, x, w, bias=True)):
+        ref.check(v, *want[name], name)
+
+
+def test_without_workspace(ctx):
+    """Operands in odd places, with the copies that a workspace allows and without."""
+    import ctypes
+    from paper_2608_16308_amd import _lib
+    dt, (t, n, m) = torch.float16, (2000, 3001, 2003)
+    g = gen(6)
+    x, w, y = rnd(g, (t, n), dt), rnd(g, (m, n), dt, n ** -0.5), torch.empty((t, m), dtype=dt, device="cuda")
+    want, bound, _, _ = ref.linear(x, w, None, "none", None)
+    size = ctypes.c_size_t()
+    _lib.check(dbs.lib().dbs_forward_work(ctx._h, 0, t, n, m, ctypes.byref(size)))
+    assert size.value >= 2 * (t * n + m * n)
+    work = torch.empty(size.value, dtype=torch.uint8, device="cuda")
+    for at, room in ((work.data_ptr(), size.value), (work.data_ptr(), 1024), (None, 0)):
+        y.fill_(float("nan"))
+        _lib.check(dbs.lib().dbs_linear(ctx._h, _lib.DBS_F16, t, n, m, x.data_ptr(), n, w.data_ptr(), n, None, 0, None, 0,
+                                        y.data_ptr(), m, None, at, room))
+        ref.check(y, want, bound, f"{room} bytes")
+
+
 @pytest.mark.parametrize("dt", TYPES, ids=str)
 def test_empty_sizes(ctx, dt):
     z = lambda *s: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731

@@ -69,6 +69,11 @@ def test_output_apart_from_inputs():
     a, b = z[:40].view(4, 10), z[40:80].view(4, 10)
     layer._check_apart(a, "y", ((b, "x"), (None, "bias")))
     rejects(layer._check_apart, a, "y", ((z[30:70].view(4, 10), "x"),))
+    # columns of one buffer
+    w = torch.zeros((6, 40), dtype=BF)
+    layer._check_apart(w[:, 10:20], "y", ((w[:, :10], "x"), (w[:, 20:], "residual"), (w[1:5, 30:], "w")))
+    for bad in (w[:, :11], w[:, 19:], w[2:4, 12:14], w[:, :]):
+        rejects(layer._check_apart, w[:, 10:20], "y", ((bad, "x"),))
 
 
 def test_c_abi_refusals():
