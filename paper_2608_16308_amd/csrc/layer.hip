@@ -2,6 +2,7 @@
 // order of the launches.
 #include <algorithm>
 #include <climits>
+#include <cstring>
 #include <new>
 
 #include "layer.hpp"
@@ -180,14 +181,14 @@ dbs_status dbs_layer_create(void *stream, dbs_layer **out)
     hipDeviceProp_t prop;
     LAYER_TRY(hipGetDevice(&dev), "hipGetDevice");
     LAYER_TRY(hipGetDeviceProperties(&prop, dev), "hipGetDeviceProperties");
-    const std::string arch(prop.gcnArchName);
-    if (arch.compare(0, 6, "gfx950") != 0)
+    if (std::strncmp(prop.gcnArchName, "gfx950", 6) != 0)
         return dbs_fail(DBS_ERR_DEVICE, "dbs_layer_create: this build runs on gfx950, the device is %s", prop.gcnArchName);
     dbs_layer *L = new (std::nothrow) dbs_layer();
     if (!L) return dbs_fail(DBS_ERR_ALLOC, "dbs_layer_create: host allocation");
     const size_t zeros = 256;
     hipError_t e = hipMalloc(&L->mem, zeros + PART_BYTES);
     if (e == hipSuccess) e = hipMemset(L->mem, 0, zeros);
+    if (e == hipSuccess) e = hipStreamSynchronize(nullptr);  // (calls may run on streams that do not wait for this one)
     if (e == hipSuccess) e = hipDeviceGetAttribute(&L->w.cus, hipDeviceAttributeMultiprocessorCount, dev);
     if (e != hipSuccess) {
         dbs_layer_destroy(L);
