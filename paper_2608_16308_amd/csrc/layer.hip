@@ -357,8 +357,10 @@ dbs_status dbs_linear_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_
         CHECK(check_operand(fn, "dw", d_dw, n_out, n_in, lddw));
     }
     if (d_db) CHECK(check_operand(fn, "db", d_db, 1, n_out, n_out));
-    // (a dy that is not in whole chunks becomes a dz that is, also without a slope)
-    const bool slope = act != DBS_ACT_NONE || !whole_chunks(d_dy, lddy, n_out), x_codes = d_dw && x && x->d_codes;
+    // (a dy that is not in whole chunks becomes a dz that is, also without a slope;
+    // one with rows too far apart for the tiles that load them is read as it is)
+    const bool chunks = (uintptr_t)d_dy % 16 == 0 && (t <= 1 || lddy % 8 == 0) && n_out % 8 == 0;
+    const bool slope = act != DBS_ACT_NONE || !chunks, x_codes = d_dw && x && x->d_codes;
     BackwardWork b = carve(d_work, false, slope, x_codes, d_db != nullptr, t, n_in, n_out, L->w.cus);
     CHECK(check_room(fn, b.c.used, d_work, work_bytes));
     if (slope || d_db) {

@@ -467,3 +467,17 @@ def test_rows_past_32_bits(ctx):
     ref.check(ctx.linear_backward(dy, x, w)[1], *want["dw"], "dw of far rows")
     c = ctx.pack(x)
     assert torch.equal(c.codes.cpu(), ref.pack(x.cpu().contiguous())[0])
+
+
+def test_gradients_of_rows_far_apart(ctx):
+    """Without an activation dy is multiplied as it is, whatever its rows' distance."""
+    dt = torch.bfloat16
+    g = gen(23)
+    for t, m, ld in ((1, (1 << 21) + 8, None), (2, 80, (1 << 21) + 8)):
+        x, w = rnd(g, (t, 8), dt), rnd(g, (m, 8), dt)
+        buf = torch.zeros((t, ld or m), dtype=dt, device="cuda")
+        dy = buf[:, :m]
+        dy.copy_(torch.randn((t, m), generator=g, device="cuda"))
+        want = ref.linear_backward(dy, x.double(), w, None, "none")
+        for name, v in zip(("dx", "dw"), ctx.linear_backward(dy, x, w)):
+            ref.check(v, *want[name], f"{t}x{m} rows of {ld or m} {name}")
