@@ -1,6 +1,7 @@
 // 8-bit activation checkpoints and the elementwise part of the backward
 // passes that reads them.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "layer.hpp"
@@ -169,6 +170,43 @@ __global__ __launch_bounds__(CK_TPB) void k_align(const _Float16 *__restrict__ s
 constexpr int SL_WAVES = 4;                // waves of a workgroup, each a row at a time
 constexpr int SL_COLS = 64 * 8;            // columns of a workgroup
 constexpr int SUM_WAVES = 16;
+static_assert(SL_WAVES == 4, "the maxima of four waves");
+
+__device__ __forceinline__ float wave_max(float v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, WAVE));
+    return v;
+}
+
+// Eight columns of a row of the activation gradients in 32 bits, the chunk `col`
+// (`left` columns up to the row's end, zeros behind it).
+template <class X, bool GATED>
+__device__ __forceinline__ void slope_chunk(const SlopeArgs &a, int row, int col, int left, float (&dz)[8], float (&du)[8])
+{
+    typedef typename X::T T;
+    const int64_t groups = (a.cols + CK_GROUP - 1) / CK_GROUP;
+    auto held = [&](const HeldIn &h, float (&v)[8]) {
+        if (h.codes) ck_values<X>(load_codes(h.codes + (int64_t)row * a.cols + col, left),
+                                (int)h.exps[row * groups + col / CK_GROUP] - CK_BIAS, v);
+        else load_vals<X>((const T *)h.full + (int64_t)row * h.ld + col, left, v);
+    };
+    float dy[8], z[8], up[8], f[8], d[8];
+    load_vals<X>((const T *)a.dy + (int64_t)row * a.lddy + col, left, dy);
+    if (a.pre.codes || a.pre.full) held(a.pre, z);
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = 0.f;
+    if (GATED) held(a.up, up);
+    act_slopes(a.act, z, f, d);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (GATED) du[i] = i < left ? dy[i] * f[i] : 0.f;
+        dz[i] = i < left ? (GATED ? dy[i] * up[i] : dy[i]) * d[i] : 0.f;
+    }
+}
+// The rows of workgroups along the rows.
+__device__ __forceinline__ int slope_row(const SlopeArgs &a, int block) { return (int)((int64_t)a.rows * block / a.row_blocks); }
 
 // The sums of the columns are added in a fixed order: a lane's rows, the
 // waves, then the workgroups along the rows (k_slope_sum).
@@ -176,35 +214,21 @@ template <class X, bool GATED>
 __global__ __launch_bounds__(64 * SL_WAVES) void k_slope(SlopeArgs a)
 {
     typedef typename X::T T;
+    constexpr bool RANGE = std::is_same<X, Fp16>::value;
     __shared__ float part[SL_WAVES][SL_COLS];
     const int lane = lane_id(), wave = wave_id();
     const int col = (int)blockIdx.x * SL_COLS + 8 * lane, left = a.cols - col;
-    const int r0 = (int)((int64_t)a.rows * blockIdx.y / a.row_blocks);
-    const int r1 = (int)((int64_t)a.rows * (blockIdx.y + 1) / a.row_blocks);
-    const int64_t groups = (a.cols + CK_GROUP - 1) / CK_GROUP;
-    auto held = [&](const HeldIn &h, int row, float (&v)[8]) {
-        if (h.codes) ck_values<X>(load_codes(h.codes + (int64_t)row * a.cols + col, left),
-                                (int)h.exps[row * groups + col / CK_GROUP] - CK_BIAS, v);
-        else load_vals<X>((const T *)h.full + (int64_t)row * h.ld + col, left, v);
-    };
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int r1 = slope_row(a, (int)blockIdx.y + 1);
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, most = 0.f;
     if (left > 0)
-        for (int row = r0 + wave; row < r1; row += SL_WAVES) {
-            float dy[8], z[8], up[8], f[8], d[8], dz[8], du[8];
-            load_vals<X>((const T *)a.dy + (int64_t)row * a.lddy + col, left, dy);
-            if (a.pre.codes || a.pre.full) held(a.pre, row, z);
-            else
+        for (int row = slope_row(a, (int)blockIdx.y) + wave; row < r1; row += SL_WAVES) {
+            float dz[8], du[8];
+            slope_chunk<X, GATED>(a, row, col, left, dz, du);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) z[i] = 0.f;
-            if (GATED) held(a.up, row, up);
-            act_slopes(a.act, z, f, d);
+            for (int i = 0; i < 8; ++i) sum[i] += dz[i];
+            if (RANGE && a.most)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                // (columns past the last: the zeros that fill the row)
-                if (GATED) du[i] = i < left ? dy[i] * f[i] : 0.f;
-                dz[i] = i < left ? (GATED ? dy[i] * up[i] : dy[i]) * d[i] : 0.f;
-                sum[i] += dz[i];
-            }
+                for (int i = 0; i < 8; ++i) most = fmaxf(most, GATED ? fmaxf(ck_mag(dz[i]), ck_mag(du[i])) : ck_mag(dz[i]));
             if (a.dz) {
                 store_vals<X>((T *)a.dz + (int64_t)row * a.ldz + col, 8, dz);
                 if (GATED) store_vals<X>((T *)a.du + (int64_t)row * a.ldz + col, 8, du);
@@ -221,6 +245,50 @@ __global__ __launch_bounds__(64 * SL_WAVES) void k_slope(SlopeArgs a)
 #pragma unroll
             for (int w = 0; w < SL_WAVES; ++w) s += part[w][c];
             a.sums[blockIdx.y * (int64_t)a.cols + at] = s;
+        }
+        __syncthreads();
+    }
+    if (RANGE && a.most) {
+        most = wave_max(most);
+        if (lane == 0) part[wave][0] = most;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            a.most[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = fmaxf(fmaxf(part[0][0], part[1][0]), fmaxf(part[2][0], part[3][0]));
+    }
+}
+
+// fp16: where the largest dz or du has left the type's range, all of them again,
+// times 2^-s.  Nearly always there is nothing to do beside reading the workgroups'
+// maxima (4 us of a call; no atomics and no answer on the host, so that a captured
+// call follows its inputs).
+template <bool GATED> __global__ __launch_bounds__(64 * SL_WAVES) void k_slope_range(SlopeArgs a, int32_t strips)
+{
+    __shared__ float part[SL_WAVES];
+    const int lane = lane_id(), wave = wave_id();
+    const int64_t n = (int64_t)strips * a.row_blocks;
+    float most = 0.f;
+    for (int64_t i = threadIdx.x; i < n; i += 64 * SL_WAVES) most = fmaxf(most, a.most[i]);
+    most = wave_max(most);
+    if (lane == 0) part[wave] = most;
+    __syncthreads();
+    const int s = slope_exp(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])));
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.most[n] = __builtin_amdgcn_ldexpf(1.f, s);
+    if (s == 0) return;
+    const float by = __builtin_amdgcn_ldexpf(1.f, -s);
+    for (int64_t at = blockIdx.x; at < n; at += gridDim.x) {
+        const int block = (int)(at / strips), col = (int)(at % strips) * SL_COLS + 8 * lane, left = a.cols - col;
+        const int r1 = slope_row(a, block + 1);
+        if (left <= 0) continue;
+        for (int row = slope_row(a, block) + wave; row < r1; row += SL_WAVES) {
+            float dz[8], du[8];
+            slope_chunk<Fp16, GATED>(a, row, col, left, dz, du);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dz[i] *= by;
+                if (GATED) du[i] *= by;
+            }
+            store_vals<Fp16>((_Float16 *)a.dz + (int64_t)row * a.ldz + col, 8, dz);
+            if (GATED) store_vals<Fp16>((_Float16 *)a.du + (int64_t)row * a.ldz + col, 8, du);
         }
     }
 }
@@ -295,12 +363,23 @@ int32_t slope_row_blocks(int32_t rows, int32_t cols, int32_t cus)
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, (rows + SL_WAVES - 1) / SL_WAVES, 65535}));
 }
 
+int64_t slope_blocks(int32_t rows, int32_t cols, int32_t cus)
+{
+    return (((int64_t)cols + SL_COLS - 1) / SL_COLS) * slope_row_blocks(rows, cols, cus);
+}
+
 template <class X> static hipError_t slope_t(bool gated, const SlopeArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)((a.cols + SL_COLS - 1) / SL_COLS), (unsigned)a.row_blocks), block(64 * SL_WAVES);
     if (gated) hipLaunchKernelGGL((k_slope<X, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_slope<X, false>), grid, block, 0, s, a);
     hipError_t e = hipGetLastError();
+    if (e == hipSuccess && a.most) {
+        const unsigned n = std::min(grid.x * grid.y, 1024u);
+        if (gated) hipLaunchKernelGGL(k_slope_range<true>, dim3(n), block, 0, s, a, (int32_t)grid.x);
+        else hipLaunchKernelGGL(k_slope_range<false>, dim3(n), block, 0, s, a, (int32_t)grid.x);
+        e = hipGetLastError();
+    }
     if (e == hipSuccess && a.sums) {
         hipLaunchKernelGGL(k_slope_sum<X>, dim3((unsigned)((a.cols + 63) / 64)), dim3(64 * SUM_WAVES), 0, s, a.sums, a.row_blocks,
                            a.cols, (typename X::T *)a.db);

@@ -148,11 +148,12 @@ hipError_t make_whole(const LayerWork &w, Operand *const *ops, int n, double flo
 }
 
 // What a backward pass cannot do without: dz (and du) where an activation has a
-// slope or dy is not in whole chunks, the values of an x held in 8 bits, the
-// partial sums of db.
+// slope or dy is not in whole chunks, with the largest of them, the values of an x
+// held in 8 bits, the partial sums of db.
 struct BackwardWork {
     void *dz, *du, *x;
-    float *sums;
+    float *most, *sums;
+    int64_t blocks;
     int64_t ldz, ldx;
     Carve c;
 };
@@ -162,7 +163,8 @@ BackwardWork carve(void *mem, bool gated, bool slope, bool x_codes, bool db, int
     b.c.base = (uint8_t *)mem;
     b.ldz = up8(n_out);
     b.ldx = up8(n_in);
-    if (slope) b.dz = b.c.take((size_t)t * b.ldz * 2);
+    b.blocks = slope_blocks(t, n_out, cus);
+    if (slope) b.dz = b.c.take((size_t)t * b.ldz * 2), b.most = (float *)b.c.take((size_t)(b.blocks + 1) * 4);
     if (gated) b.du = b.c.take((size_t)t * b.ldz * 2);
     if (x_codes) b.x = b.c.take((size_t)t * b.ldx * 2);
     if (db) b.sums = (float *)b.c.take((size_t)slope_row_blocks((int32_t)t, (int32_t)n_out, cus) * n_out * 4);
@@ -306,9 +308,9 @@ dbs_status dbs_backward_work(const dbs_layer *L, int gated, dbs_act act, int32_t
 }
 
 // The products that both backward passes end in, dz (and du) given in whole
-// chunks.
+// chunks, times 1 / *scale where that is given.
 static dbs_status gradients(dbs_layer *L, const char *fn, dbs_dtype dt, int32_t t, int32_t n_in, int32_t n_out, int n,
-                            const void *const dz[2], int64_t ldz, bool own_dz, const dbs_held *x, BackwardWork &b,
+                            const void *const dz[2], int64_t ldz, bool own_dz, const float *scale, const dbs_held *x, BackwardWork &b,
                             size_t room, Operand *const *w, void *d_dx, int64_t lddx, void *const dw[2], const int64_t lddw[2])
 {
     const bool bf = dt == DBS_BF16;
@@ -320,7 +322,7 @@ static dbs_status gradients(dbs_layer *L, const char *fn, dbs_dtype dt, int32_t 
         for (int i = 0; i < n; ++i) a.p[i] = w[i]->p, a.ldp[i] = w[i]->ld, a.q[i] = dz[i], a.ldq[i] = ldz;
         a.pn = n_in, a.qn = t, a.kn = n_out, a.segs = n, a.batch = 1;
         a.y[0] = d_dx, a.ldy[0] = lddx;
-        a.p_padded = padded, a.q_padded = own_dz;
+        a.p_padded = padded, a.q_padded = own_dz, a.scale = scale;
         LAYER_TRY(launch_gemm(L->w, bf, G_DX, a, L->stream), fn);
     }
     if (dw[0]) {
@@ -332,7 +334,7 @@ static dbs_status gradients(dbs_layer *L, const char *fn, dbs_dtype dt, int32_t 
         } else LAYER_TRY(make_whole(L->w, ops, 1, flops, b.c, room, L->stream, &padded), fn);
         GemmArgs a{};
         for (int i = 0; i < n; ++i) a.q[i] = dz[i], a.ldq[i] = ldz, a.y[i] = dw[i], a.ldy[i] = lddw[i];
-        a.p[0] = xv.p, a.ldp[0] = xv.ld, a.p_padded = padded, a.q_padded = own_dz;
+        a.p[0] = xv.p, a.ldp[0] = xv.ld, a.p_padded = padded, a.q_padded = own_dz, a.scale = scale;
         a.pn = n_in, a.qn = n_out, a.kn = t, a.segs = 1, a.batch = n;
         LAYER_TRY(launch_gemm(L->w, bf, G_DW, a, L->stream), fn);
     }
@@ -363,11 +365,13 @@ dbs_status dbs_linear_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_
     const bool slope = act != DBS_ACT_NONE || !chunks, x_codes = d_dw && x && x->d_codes;
     BackwardWork b = carve(d_work, false, slope, x_codes, d_db != nullptr, t, n_in, n_out, L->w.cus);
     CHECK(check_room(fn, b.c.used, d_work, work_bytes));
+    // (ReLU passes or drops dy as it is)
+    const bool range = dt == DBS_F16 && act != DBS_ACT_NONE && act != DBS_ACT_RELU && t > 0 && n_out > 0 && (d_dx || d_dw);
     if (slope || d_db) {
         SlopeArgs s{};
         s.dy = d_dy, s.lddy = lddy, s.rows = t, s.cols = n_out, s.act = Act::of(act);
         if (act != DBS_ACT_NONE) s.pre = held_in(pre);
-        s.dz = b.dz, s.ldz = b.ldz;
+        s.dz = b.dz, s.ldz = b.ldz, s.most = range ? b.most : nullptr;
         s.sums = d_db ? b.sums : nullptr, s.db = d_db, s.row_blocks = slope_row_blocks(t, n_out, L->w.cus);
         LAYER_TRY(launch_slope(dt == DBS_BF16, false, s, L->stream), fn);
     }
@@ -375,7 +379,7 @@ dbs_status dbs_linear_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_
     Operand w{d_w, ldw, n_out, n_in}, *const ws[] = {&w};
     void *dw[2] = {d_dw, nullptr};
     const int64_t lddws[2] = {lddw, 0};
-    return gradients(L, fn, dt, t, n_in, n_out, 1, dz, slope ? b.ldz : lddy, slope, x, b, work_bytes, ws, d_dx, lddx, dw, lddws);
+    return gradients(L, fn, dt, t, n_in, n_out, 1, dz, slope ? b.ldz : lddy, slope, range ? b.most + b.blocks : nullptr, x, b, work_bytes, ws, d_dx, lddx, dw, lddws);
 }
 
 dbs_status dbs_gated_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_in, int32_t n_out, const void *d_dh,
@@ -403,17 +407,19 @@ dbs_status dbs_gated_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_i
     const bool x_codes = d_dwg && x && x->d_codes;
     BackwardWork b = carve(d_work, true, true, x_codes, false, t, n_in, n_out, L->w.cus);
     CHECK(check_room(fn, b.c.used, d_work, work_bytes));
+    const bool range = dt == DBS_F16 && t > 0 && n_out > 0;
     if (t > 0) {
         SlopeArgs s{};
         s.dy = d_dh, s.lddy = lddh, s.pre = held_in(gate), s.up = held_in(up), s.rows = t, s.cols = n_out, s.act = Act::of(act);
         s.dz = b.dz, s.du = b.du, s.ldz = b.ldz, s.row_blocks = slope_row_blocks(t, n_out, L->w.cus);
+        s.most = range ? b.most : nullptr;
         LAYER_TRY(launch_slope(dt == DBS_BF16, true, s, L->stream), fn);
     }
     const void *dz[2] = {b.dz, b.du};
     Operand g{d_wg, ldwg, n_out, n_in}, u{d_wu, ldwu, n_out, n_in}, *const ws[] = {&g, &u};
     void *dw[2] = {d_dwg, d_dwu};
     const int64_t lddw[2] = {lddwg, lddwu};
-    return gradients(L, fn, dt, t, n_in, n_out, 2, dz, b.ldz, true, x, b, work_bytes, ws, d_dx, lddx, dw, lddw);
+    return gradients(L, fn, dt, t, n_in, n_out, 2, dz, b.ldz, true, range ? b.most + b.blocks : nullptr, x, b, work_bytes, ws, d_dx, lddx, dw, lddw);
 }
 
 dbs_status dbs_pack(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t cols, const void *d_x, int64_t ldx, int8_t *d_codes,

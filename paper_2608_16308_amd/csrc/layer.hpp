@@ -222,6 +222,7 @@ struct GemmArgs {
     int32_t chunks;          // P and Q are made of whole 16-byte chunks
     int32_t tp, tq;          // tiles along p and q
     int32_t full, splits;    // tiles taken whole; parts of each of the others along k
+    const float *scale;      // G_DX, G_DW: what the sums are multiplied by (NULL: 1)
     float *part;             // the parts' sums
     const void *zeros;       // 16 bytes of zeros
 };
@@ -252,6 +253,14 @@ hipError_t launch_rows(const LayerWork &w, bool bf16, bool gated, const GemmArgs
 // Activation gradients: dz = dy * act'(pre) or, gated, dz = dy * up * act'(gate)
 // and du = dy * act(gate), rounded to the element type, rows of `ldz` elements
 // with zeros behind the last column; sums of the columns of the unrounded dz.
+//
+// Why 16 bits: dz and du are operands of the matrix cores.  That costs a rounding
+// of u of each of them (in bf16 the gradients are then 2.3e-3 from 64 bits, where
+// the final rounding alone is 1.7e-3; in fp16 2.9e-4 and 2.1e-4); two 16-bit parts
+// for each would double the products.  In fp16 such a product of 16-bit numbers may
+// leave the type's range where the gradients do not, so there all dz and du of a
+// call are held times a power of two 2^-s, and the sums over them are multiplied by
+// 2^s in 32 bits: see slope_exp.
 struct SlopeArgs {
     const void *dy;
     int64_t lddy;
@@ -263,8 +272,19 @@ struct SlopeArgs {
     float *sums;        // NULL, or row_blocks x cols
     void *db;
     int32_t row_blocks; // workgroups along the rows
+    float *most;        // NULL, or for each workgroup its largest |dz|, |du|, and then 2^s
 };
+// s for the largest finite magnitude m of dz and du: 0 while they keep to the
+// range (from 2^-8 on, what is lost below the least fp16 number is under 2^-17 of
+// m), else m 2^-s is in [2^14, 2^15); s >= -60 keeps 2^s a normal number.
+__device__ __forceinline__ int slope_exp(float m)
+{
+    if (m == 0.f || (m >= 0.00390625f && m <= Fp16::MAX)) return 0;
+    return max((int)__builtin_amdgcn_frexp_expf(m) - 15, -60);
+}
 int32_t slope_row_blocks(int32_t rows, int32_t cols, int32_t cus);
+// Workgroups of a call (the elements of `most` before 2^s).
+int64_t slope_blocks(int32_t rows, int32_t cols, int32_t cus);
 hipError_t launch_slope(bool bf16, bool gated, const SlopeArgs &a, hipStream_t s);
 
 hipError_t launch_pack(bool bf16, const void *x, int64_t ldx, int32_t rows, int32_t cols, int8_t *codes, uint8_t *exps,

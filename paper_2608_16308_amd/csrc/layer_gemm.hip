@@ -73,6 +73,7 @@ __device__ __forceinline__ void epilogue(const GemmArgs &a, const f4_t (&acc)[MT
     if constexpr ((KIND == G_DX || KIND == G_DW)) {
         T *y = (T *)a.y[z];
         const int64_t ld = a.ldy[z];
+        const float scale = a.scale ? *a.scale : 1.f;
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             const int row = q0 + 16 * m + r;
@@ -83,7 +84,7 @@ __device__ __forceinline__ void epilogue(const GemmArgs &a, const f4_t (&acc)[MT
                 T *dst = y + (int64_t)row * ld + col;
                 V4 v;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = (T)acc[m][j][i];
+                for (int i = 0; i < 4; ++i) v[i] = (T)(acc[m][j][i] * scale);
                 if (col + 4 <= a.pn) store_any(dst, v);
                 else
 #pragma unroll
