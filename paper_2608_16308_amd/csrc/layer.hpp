@@ -66,18 +66,14 @@ template <class X> __device__ __forceinline__ typename X::V8 load_end(const type
 // ---------------------------------------------------------------------------
 // activations
 // ---------------------------------------------------------------------------
-// act(z).  SiLU and the tanh form of GELU are both z times a logistic of
+// act(z).  SiLU is z times a logistic of z, and so is the tanh form of GELU, of
 // a z + b z^3 (1 + tanh(q) = 2 logistic(2 q)), which also keeps the relative
 // precision of the small values left of zero; GELU itself takes erf.
 struct Act {
     int32_t kind;
-    float a, b;  // of the logistic
-    static Act of(dbs_act k)
-    {
-        const float c = 1.5957691216057308f;  // 2 sqrt(2 / pi)
-        return Act{(int32_t)k, k == DBS_ACT_GELU_TANH ? c : 1.f, k == DBS_ACT_GELU_TANH ? c * 0.044715f : 0.f};
-    }
+    static Act of(dbs_act k) { return Act{(int32_t)k}; }
 };
+constexpr float GELU_A = 1.5957691216057308f, GELU_B = GELU_A * 0.044715f;  // a = 2 sqrt(2 / pi)
 __device__ __forceinline__ float logistic(float q) { return __builtin_amdgcn_rcpf(1.f + __expf(-q)); }
 
 // v = act(v) for N values
@@ -90,10 +86,21 @@ template <int N> __device__ __forceinline__ void act_values(Act f, float (&v)[N]
     } else if (f.kind == DBS_ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * (1.f + erff(v[i] * 0.70710678118654752f));
+    } else if (f.kind == DBS_ACT_SILU) {  // (not the form below with b = 0: an infinite square times zero is NaN)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] * logistic(v[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = v[i] * logistic(v[i] * (f.a + f.b * v[i] * v[i]));
+        for (int i = 0; i < N; ++i) v[i] = v[i] * logistic(v[i] * (GELU_A + GELU_B * v[i] * v[i]));
     }
+}
+// Value and slope of z logistic(q), `g` the slope of q.  Where the logistic is 0
+// or 1 the second term of the slope is 0, also where g has overflowed.
+__device__ __forceinline__ void logistic_slope(float z, float q, float g, float &value, float &slope)
+{
+    const float s = logistic(q), d = s * (1.f - s);
+    value = z * s;
+    slope = s + (d == 0.f ? 0.f : z * d * g);
 }
 // act(z) and act'(z) of N values.
 template <int N> __device__ __forceinline__ void act_slopes(Act f, const float (&z)[N], float (&value)[N], float (&slope)[N])
@@ -111,14 +118,14 @@ template <int N> __device__ __forceinline__ void act_slopes(Act f, const float (
             value[i] = z[i] * c;
             slope[i] = c + z[i] * __expf(-0.5f * z[i] * z[i]) * 0.39894228040143268f;
         }
+    } else if (f.kind == DBS_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) logistic_slope(z[i], z[i], 1.f, value[i], slope[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float zz = z[i] * z[i], s = logistic(z[i] * (f.a + f.b * zz));
-            value[i] = z[i] * s;
-            // (where s is 0 or 1 the second term is 0, also where z^3 overflows)
-            const float d = s * (1.f - s), t = z[i] * d * (f.a + 3.f * f.b * zz);
-            slope[i] = s + (d == 0.f ? 0.f : t);
+            const float zz = z[i] * z[i];
+            logistic_slope(z[i], z[i] * (GELU_A + GELU_B * zz), GELU_A + 3.f * GELU_B * zz, value[i], slope[i]);
         }
     }
 }
