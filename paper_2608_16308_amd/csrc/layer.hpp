@@ -68,7 +68,8 @@ template <class X> __device__ __forceinline__ typename X::V8 load_end(const type
 // ---------------------------------------------------------------------------
 // act(z).  SiLU is z times a logistic of z, and so is the tanh form of GELU, of
 // a z + b z^3 (1 + tanh(q) = 2 logistic(2 q)), which also keeps the relative
-// precision of the small values left of zero; GELU itself takes erf.
+// precision of the small values left of zero; GELU itself takes the complement
+// of erf, 1 + erf(x) = erfc(-x): the sum would cancel there (4% off at -5).
 struct Act {
     int32_t kind;
     static Act of(dbs_act k) { return Act{(int32_t)k}; }
@@ -85,7 +86,7 @@ template <int N> __device__ __forceinline__ void act_values(Act f, float (&v)[N]
         for (int i = 0; i < N; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
     } else if (f.kind == DBS_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * (1.f + erff(v[i] * 0.70710678118654752f));
+        for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * erfcf(v[i] * -0.70710678118654752f);
     } else if (f.kind == DBS_ACT_SILU) {  // (not the form below with b = 0: an infinite square times zero is NaN)
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = v[i] * logistic(v[i]);
@@ -114,7 +115,7 @@ template <int N> __device__ __forceinline__ void act_slopes(Act f, const float (
     } else if (f.kind == DBS_ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float c = 0.5f * (1.f + erff(z[i] * 0.70710678118654752f));
+            const float c = 0.5f * erfcf(z[i] * -0.70710678118654752f);
             value[i] = z[i] * c;
             slope[i] = c + z[i] * __expf(-0.5f * z[i] * z[i]) * 0.39894228040143268f;
         }
