@@ -513,12 +513,12 @@ dbs_status dbs_basic_spmspv(dbs_basic_matrix *B, dbs_path path, int32_t x_nnz, c
  * Sizes are at most 2^30.  Outputs must not overlap inputs, except that y may
  * be the residual itself.  NaN and infinities propagate as in the formulas. */
 
-/* A layer context holds the workspace of one stream: calls on it run in
- * stream order and are asynchronous; it is used by one host thread at a time.
- * Calls allocate nothing and may be captured into a graph.                  */
+/* A layer context holds the workspace of one stream, the one that it is created
+ * for: calls on it run in stream order and are asynchronous; it is used by one
+ * host thread at a time.  Calls allocate nothing and may be captured into a
+ * graph, which needs the context as long as it is replayed.                  */
 typedef struct dbs_layer dbs_layer;
 dbs_status dbs_layer_create(void *stream, dbs_layer **out);
-dbs_status dbs_layer_set_stream(dbs_layer *L, void *stream);
 void dbs_layer_destroy(dbs_layer *L);
 
 /* act(z): z; max(z, 0); z / (1 + e^-z); z (1 + erf(z / sqrt 2)) / 2;

@@ -31,7 +31,7 @@ EXPORTED = [
     "dbs_ctx_read_timing", "dbs_last_error", "dbs_version", "dbs_basic_build", "dbs_basic_destroy",
     "dbs_basic_spmspv", "dbs_matrix_build_dense", "dbs_matrix_layout_get", "dbs_matrix_download",
     "dbs_spmspv_noalloc", "dbs_ctx_set_single_launch",
-    "dbs_layer_create", "dbs_layer_set_stream", "dbs_layer_destroy", "dbs_linear", "dbs_gated", "dbs_forward_work", "dbs_backward_work",
+    "dbs_layer_create", "dbs_layer_destroy", "dbs_linear", "dbs_gated", "dbs_forward_work", "dbs_backward_work",
     "dbs_linear_backward", "dbs_gated_backward", "dbs_pack", "dbs_unpack",
 ]
 DBS_NOALLOC_MAX_DIM = 1 << 20
@@ -152,7 +152,6 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "dbs_basic_destroy": (None, [vp]),
         "dbs_basic_spmspv": (ctypes.c_int, [vp, ctypes.c_int, i32, vp, vp, vp, vp]),
         "dbs_layer_create": (ctypes.c_int, [vp, P(vp)]),
-        "dbs_layer_set_stream": (ctypes.c_int, [vp, vp]),
         "dbs_layer_destroy": (None, [vp]),
         "dbs_linear": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, vp, i64, vp, i64, vp, ctypes.c_int, vp, i64, vp, i64,
                                       P(Held), vp, ctypes.c_size_t]),

@@ -204,13 +204,6 @@ dbs_status dbs_layer_create(void *stream, dbs_layer **out)
     return DBS_OK;
 }
 
-dbs_status dbs_layer_set_stream(dbs_layer *L, void *stream)
-{
-    if (!L) return dbs_fail(DBS_ERR_ARG, "dbs_layer_set_stream: layer context is NULL");
-    L->stream = (hipStream_t)stream;
-    return DBS_OK;
-}
-
 void dbs_layer_destroy(dbs_layer *L)
 {
     if (!L) return;
