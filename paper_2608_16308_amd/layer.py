@@ -16,12 +16,13 @@ from __future__ import annotations
 import ctypes
 
 from . import _lib
-from ._lib import DBS_BF16, DBS_ERR_ARG, DBS_F16, DbsError, check
+from ._lib import DBS_BF16, DBS_ERR_ARG, DBS_ERR_UNSUPPORTED, DBS_F16, DbsError, check
 
 ACTS = {"none": _lib.DBS_ACT_NONE, "relu": _lib.DBS_ACT_RELU, "silu": _lib.DBS_ACT_SILU, "gelu": _lib.DBS_ACT_GELU,
         "gelu_tanh": _lib.DBS_ACT_GELU_TANH}
 SAVES = ("none", "full", "8bit")
 CK_GROUP = _lib.DBS_CK_GROUP
+MAX_DIM = 1 << 30  # of each size
 ROWS_TOKENS = 16  # forward calls of so few tokens use no workspace
 
 
@@ -67,6 +68,12 @@ def _dtype_code(torch, t, name):
     raise _arg_error(f"{name} has dtype {t.dtype}, expected torch.float16 or torch.bfloat16")
 
 
+def _check_dims(shape, name):
+    """Sizes are handed on as 32-bit numbers, which would drop the upper bits."""
+    if max(shape) > MAX_DIM:
+        raise DbsError(DBS_ERR_UNSUPPORTED, f"{name} has shape {tuple(shape)}: size above 2^30")
+
+
 def check_rows(t, name, dtype, device, rows, cols):
     """One 2-D tensor argument of rows x cols (None: any) of `dtype` on `device`
     with unit column stride; the elements from row to row."""
@@ -79,6 +86,7 @@ def check_rows(t, name, dtype, device, rows, cols):
     if t.dim() != 2:
         raise _arg_error(f"{name} must have 2 dimensions, not {t.dim()}")
     r, c = t.shape
+    _check_dims(t.shape, name)
     if (rows is not None and r != rows) or (cols is not None and c != cols):
         raise _arg_error(f"{name} has shape {tuple(t.shape)}, expected ({'any' if rows is None else rows}, "
                          f"{'any' if cols is None else cols})")
@@ -99,6 +107,7 @@ def check_vector(t, name, dtype, device, n):
 
 
 def check_checkpoint(torch, c, name, dtype, device, rows, cols):
+    _check_dims((rows, cols), name)
     if c.dtype != dtype:
         raise _arg_error(f"{name} holds values of {c.dtype}, expected {dtype}")
     for t, part, dt, shape in ((c.codes, "codes", torch.int8, (rows, cols)),
