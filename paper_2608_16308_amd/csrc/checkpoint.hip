@@ -296,10 +296,10 @@ template <bool GATED> __global__ __launch_bounds__(64 * SL_WAVES) void k_slope_r
 // The workgroups' sums, a column a lane, the rows shared out to the waves.
 template <class X>
 __global__ __launch_bounds__(64 * SUM_WAVES) void k_slope_sum(const float *__restrict__ sums, int32_t n, int32_t cols,
-                                                              typename X::T *__restrict__ db)
+                                                              typename X::T *__restrict__ db, int32_t first)
 {
     __shared__ float part[SUM_WAVES][64];
-    const int lane = lane_id(), wave = wave_id(), c = (int)blockIdx.x * 64 + lane;
+    const int lane = lane_id(), wave = wave_id(), c = ((int)blockIdx.x + first) * 64 + lane;
     float s = 0.f;
     if (c < cols)
 #pragma unroll 4
@@ -381,9 +381,10 @@ template <class X> static hipError_t slope_t(bool gated, const SlopeArgs &a, hip
         e = hipGetLastError();
     }
     if (e == hipSuccess && a.sums) {
-        hipLaunchKernelGGL(k_slope_sum<X>, dim3((unsigned)((a.cols + 63) / 64)), dim3(64 * SUM_WAVES), 0, s, a.sums, a.row_blocks,
-                           a.cols, (typename X::T *)a.db);
-        e = hipGetLastError();
+        e = launch_parts(((int64_t)a.cols + 63) / 64, 64 * SUM_WAVES, [&](int32_t first, dim3 n) {
+            hipLaunchKernelGGL(k_slope_sum<X>, n, dim3(64 * SUM_WAVES), 0, s, a.sums, a.row_blocks, a.cols,
+                               (typename X::T *)a.db, first);
+        });
     }
     return e;
 }

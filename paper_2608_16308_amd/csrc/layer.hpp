@@ -227,6 +227,7 @@ struct GemmArgs {
     SaveTo save[2];
     int32_t p_padded, q_padded;  // rows of P, Q go on to a whole 16 bytes (Q of G_DX: with zeros)
     // filled by the launcher
+    int32_t first;           // number of the launch's first workgroup
     int32_t chunks;          // P and Q are made of whole 16-byte chunks
     int32_t tp, tq;          // tiles along p and q
     int32_t full, splits;    // tiles taken whole; parts of each of the others along k
@@ -234,6 +235,19 @@ struct GemmArgs {
     float *part;             // the parts' sums
     const void *zeros;       // 16 bytes of zeros
 };
+
+// Launches `n` workgroups in parts of fewer than 2^32 threads, which is what the
+// runtime takes: launch(first, number).
+template <class F> static hipError_t launch_parts(int64_t n, int threads, F &&launch)
+{
+    const int64_t most = (UINT32_MAX / threads) & ~(int64_t)7;  // (each XCD as in one launch)
+    for (int64_t first = 0; first < n; first += most) {
+        launch((int32_t)first, dim3((unsigned)(n - first < most ? n - first : most)));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 // Workspace of a layer context.
 struct LayerWork {

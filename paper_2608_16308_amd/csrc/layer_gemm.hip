@@ -220,7 +220,7 @@ template <int DQ, int DP> __device__ __forceinline__ Unit place_of(const GemmArg
 template <int DQ, int DP> __device__ __forceinline__ Unit unit_of(const GemmArgs &a)
 {
     const int ntile = a.tp * a.tq * a.batch, steps = (a.kn + BK - 1) / BK * a.segs;
-    const int id = (int)blockIdx.x, rest = id >= a.full;
+    const int id = (int)blockIdx.x + a.first, rest = id >= a.full;
     const int n = rest ? (ntile - a.full) * a.splits : a.full, i = rest ? id - a.full : id;
     const int x = i & 7, each = n >> 3, rem = n & 7;
     const int at = x * each + min(x, rem) + (i >> 3);
@@ -624,9 +624,12 @@ static hipError_t launch_tile(const LayerWork &w, GemmArgs a, hipStream_t s)
     if (!lay_out<C, KIND>(w, a, C::per_cu(NS ? NS : 2), &steps)) return hipErrorInvalidConfiguration;
     const int ntile = a.tp * a.tq * a.batch;
     if (ntile == 0) return hipSuccess;
-    const unsigned grid = (unsigned)(a.full + (ntile - a.full) * a.splits);
-    if constexpr (NS != 0) hipLaunchKernelGGL((k_block<X, KIND, NWQ, NWP, MT, NS>), dim3(grid), dim3(C::NT), 0, s, a);
-    else hipLaunchKernelGGL((k_tile<X, KIND, NWQ, NWP, MT, PF>), dim3(grid), dim3(C::NT), 0, s, a);
+    const hipError_t e = launch_parts(a.full + (ntile - a.full) * a.splits, C::NT, [&](int32_t first, dim3 grid) {
+        a.first = first;
+        if constexpr (NS != 0) hipLaunchKernelGGL((k_block<X, KIND, NWQ, NWP, MT, NS>), grid, dim3(C::NT), 0, s, a);
+        else hipLaunchKernelGGL((k_tile<X, KIND, NWQ, NWP, MT, PF>), grid, dim3(C::NT), 0, s, a);
+    });
+    if (e != hipSuccess) return e;
     if (a.splits > 1)
         hipLaunchKernelGGL((k_join<X, KIND, NWQ, NWP, MT>), dim3((unsigned)((ntile - a.full) * MT)), dim3(C::NT), 0, s, a);
     return hipGetLastError();

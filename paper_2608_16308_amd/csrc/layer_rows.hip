@@ -79,10 +79,11 @@ __global__ __launch_bounds__(64 * RW_MAX_WAVES, 3) void k_rows_dense(GemmArgs a,
 #pragma unroll
     for (int t = 0; t < 8; ++t) ox[t] = (uint32_t)min(2 * t + half, a.qn - 1) * (uint32_t)a.ldq[0] + at;
     const T *x = (const T *)a.q[0];
+    const int block = (int)blockIdx.x + a.first;
 
     for (int n = 0; n < groups; ++n) {
         // (a checkpoint's last group of columns may have no rows left)
-        const int p0 = min(((int)blockIdx.x * groups + n) * COLS, a.pn - 1);
+        const int p0 = min((block * groups + n) * COLS, a.pn - 1);
         // rows of w, from the first of their matrix
         const T *w[2];
         uint32_t ow[8];
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(64 * RW_MAX_WAVES, 3) void k_rows_dense(GemmArgs a,
     const int cols = COLS * groups;
     const int64_t ngroup = (a.pn + CK_GROUP - 1) / CK_GROUP;
     for (int c = (int)threadIdx.x; c < 16 * cols; c += (int)blockDim.x) {
-        const int token = c / cols, cc = c % cols, col = (int)blockIdx.x * cols + cc;
+        const int token = c / cols, cc = c % cols, col = block * cols + cc;
         const bool in = token < a.qn && col < a.pn;
         const float *of = total + ((cc / COLS) * 16 + token) * 16 + cc % COLS;
         finish_one<X, GATED>(a, of[0], GATED ? of[8] : 0.f, in, token, col, ngroup);
@@ -175,15 +176,16 @@ static int waves_of(const LayerWork &w, int64_t groups, int64_t kn)
     return (int)best;
 }
 
-template <class X, bool GATED> static hipError_t rows_t(const LayerWork &w, const GemmArgs &a, hipStream_t s)
+template <class X, bool GATED> static hipError_t rows_t(const LayerWork &w, GemmArgs a, hipStream_t s)
 {
     constexpr int COLS = GATED ? 8 : 16;
     const int64_t groups = ((int64_t)a.pn + COLS - 1) / COLS;
     const int waves = waves_of(w, groups, a.kn), each = a.save[0].codes ? CK_GROUP / COLS : 1;
     const size_t lds = (size_t)std::max(waves * 1024, waves * (16 + a.qn) * RW_ROW) + each * 1024;
-    hipLaunchKernelGGL((k_rows_dense<X, GATED>), dim3((unsigned)((groups + each - 1) / each)), dim3((unsigned)(64 * waves)), lds,
-                       s, a, each);
-    return hipGetLastError();
+    return launch_parts((groups + each - 1) / each, 64 * waves, [&](int32_t first, dim3 grid) {
+        a.first = first;
+        hipLaunchKernelGGL((k_rows_dense<X, GATED>), grid, dim3((unsigned)(64 * waves)), lds, s, a, each);
+    });
 }
 
 // ---------------------------------------------------------------------------
@@ -202,14 +204,14 @@ __global__ __launch_bounds__(64 * DT_WAVES) void k_rows_dot(GemmArgs a, int ks, 
     typedef typename X::T T;
     typedef typename X::V8 V8;
     __shared__ float sums[CK_GROUP * DT_WAVES][2];  // a row per pair and wave on it
-    const int lane = lane_id(), wave = wave_id(), at = 8 * lane;
+    const int lane = lane_id(), wave = wave_id(), at = 8 * lane, block = (int)blockIdx.x + a.first;
     const T *w[2], *x = (const T *)a.q[0];
     auto add = [&](V8 vw, V8 vx, float &s) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) s = __builtin_fmaf((float)vw[i], (float)vx[i], s);
     };
     for (int pair = wave / ks; pair < pairs; pair += DT_WAVES / ks) {
-        const int first = (int)blockIdx.x * pairs + pair;
+        const int first = block * pairs + pair;
 #pragma unroll
         for (int n = 0; n < 2; ++n)
             w[n] = (const T *)a.p[GATED ? n : 0] + (int64_t)min(GATED ? first : 2 * first + n, a.pn - 1) * a.ldp[GATED ? n : 0];
@@ -244,7 +246,7 @@ __global__ __launch_bounds__(64 * DT_WAVES) void k_rows_dot(GemmArgs a, int ks, 
     }
     __syncthreads();
     // a lane per column
-    const int cols = GATED ? pairs : 2 * pairs, c = (int)threadIdx.x, col = (int)blockIdx.x * cols + c;
+    const int cols = GATED ? pairs : 2 * pairs, c = (int)threadIdx.x, col = block * cols + c;
     if (c >= cols) return;
     auto value = [&](int n) {
         const float(*p)[2] = sums + (GATED ? c : c / 2) * ks;
@@ -256,15 +258,16 @@ __global__ __launch_bounds__(64 * DT_WAVES) void k_rows_dot(GemmArgs a, int ks, 
                          (a.pn + CK_GROUP - 1) / CK_GROUP);
 }
 
-template <class X, bool GATED> static hipError_t dot_t(const LayerWork &w, const GemmArgs &a, hipStream_t s)
+template <class X, bool GATED> static hipError_t dot_t(const LayerWork &w, GemmArgs a, hipStream_t s)
 {
     const int64_t pairs = GATED ? a.pn : ((int64_t)a.pn + 1) / 2, turns = ((int64_t)a.kn + DT_TURN - 1) / DT_TURN;
     int ks = 1;
     while (ks < DT_WAVES && 2 * ks <= turns && pairs * ks < 8 * (int64_t)w.cus) ks *= 2;
     const int per = a.save[0].codes ? CK_GROUP / (GATED ? 1 : 2) : DT_WAVES / ks;
-    hipLaunchKernelGGL((k_rows_dot<X, GATED>), dim3((unsigned)((pairs + per - 1) / per)), dim3(64 * DT_WAVES), 0, s, a, ks,
-                       per);
-    return hipGetLastError();
+    return launch_parts((pairs + per - 1) / per, 64 * DT_WAVES, [&](int32_t first, dim3 grid) {
+        a.first = first;
+        hipLaunchKernelGGL((k_rows_dot<X, GATED>), grid, dim3(64 * DT_WAVES), 0, s, a, ks, per);
+    });
 }
 
 template <class X, bool GATED> static hipError_t rows_g(const LayerWork &w, const GemmArgs &a, hipStream_t s)

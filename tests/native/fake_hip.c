@@ -15,6 +15,7 @@ typedef struct {
 
 long fake_allocs, fake_frees, fake_host_allocs, fake_fail_at = -1, fake_fail_from = -1, fake_occupancy_calls, fake_launches;
 int fake_device, fake_cus = 256, fake_per_cu = 1;
+unsigned long fake_most_threads; /* of a launch so far, along x */
 static __thread uint32_t last_grid; /* of this thread's last kernel with dynamic LDS: a traversal */
 static __thread err_t last_error; /* stays until it is read, as the runtime's */
 
@@ -190,6 +191,7 @@ err_t hipLaunchKernel(const void *f, dim_t g, dim_t b, void **args, size_t lds, 
     (void)args;
     (void)s;
     __sync_fetch_and_add(&fake_launches, 1);
+    if ((unsigned long)g.x * b.x > fake_most_threads) fake_most_threads = (unsigned long)g.x * b.x;
     if (lds) last_grid = g.x;
     return b.x && g.x ? 0 : done(1);
 }
