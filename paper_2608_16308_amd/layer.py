@@ -149,6 +149,38 @@ def _check_apart(out, name, inputs):
                 raise _arg_error(f"{name} overlaps {what}")
 
 
+_node = None
+
+
+def _no_graph(torch, call, inputs, outs):
+    """The outputs of a forward call.  Where autograd is asked for a gradient they
+    carry a node whose backward pass raises: without one the gradient would be
+    missing with no word."""
+    for t in inputs:
+        if t is not None and t.requires_grad:
+            break
+    else:
+        return outs
+    if not torch.is_grad_enabled():
+        return outs
+    global _node
+    if _node is None:
+        class NoGraph(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, call, outs, *inputs):
+                ctx.call = call
+                return tuple(t.detach() for t in outs)
+
+            @staticmethod
+            def backward(ctx, *grads):
+                raise DbsError(DBS_ERR_UNSUPPORTED, f"{ctx.call} builds no autograd graph; its gradients are those of "
+                                                    f"LayerContext.{ctx.call}_backward")
+        _node = NoGraph
+    tensors = tuple(t for t in outs if isinstance(t, torch.Tensor))
+    marked = iter(_node.apply(call, tensors, *(t for t in inputs if t is not None)))
+    return tuple(next(marked) if isinstance(t, torch.Tensor) else t for t in outs)
+
+
 class LayerContext:
     """Workspace of one stream (default: the current one); runs the dense layer
     operators on it.
@@ -156,7 +188,11 @@ class LayerContext:
     A call is asynchronous on the context's stream.  Where that is not torch's
     current stream, outputs belong to the context's stream and inputs are
     marked as used there; the caller orders the two streams, as for any work
-    on a stream of its own.  One host thread at a time may use a context."""
+    on a stream of its own.  One host thread at a time may use a context.
+
+    No call builds an autograd graph: the gradients are those of
+    ``linear_backward`` and ``gated_backward``, and a result that autograd
+    follows back to one of these calls raises."""
 
     def __init__(self, stream=None):
         import torch
@@ -263,7 +299,8 @@ class LayerContext:
                 None if bias is None else bias.data_ptr(), act_code, None if residual is None else residual.data_ptr(),
                 ldr, out.data_ptr(), n_out if given is None else ldy, None if keep is None else ctypes.byref(keep), at, size))
             return out, kept
-        out, kept = self._call(body, (x, w, bias, residual, given))
+        inputs = (x, w, bias, residual)
+        out, kept = _no_graph(self._torch, "linear", inputs, self._call(body, (*inputs, given)))
         out = out[0] if one else out
         return out if save == "none" else (out, kept)
 
@@ -298,7 +335,8 @@ class LayerContext:
                 out.data_ptr(), n_out if given is None else ldh, None if kg is None else ctypes.byref(kg),
                 None if ku is None else ctypes.byref(ku), at, size))
             return out, gate, up
-        out, gate, up = self._call(body, (x, w_gate, w_up, given))
+        inputs = (x, w_gate, w_up)
+        out, gate, up = _no_graph(self._torch, "gated", inputs, self._call(body, (*inputs, given)))
         out = out[0] if one else out
         return out if save == "none" else (out, gate, up)
 
