@@ -14,6 +14,8 @@ constexpr int64_t MAX_TILES = 1 << 30;
 constexpr double JOIN_STEPS = 2;  // steps that a tile's sums take to memory or back
 
 typedef short s4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u4_t __attribute__((ext_vector_type(4)));
 
 // LDS tiles hold 16-byte chunks of eight elements in rows, chunk c of row r at
 // place c ^ swz(r), so that the lanes of one read fall into different banks.
@@ -59,7 +61,11 @@ template <int KIND> __device__ __forceinline__ int p_row(int r, int &mat)
 template <class V> struct __attribute__((packed, aligned(1))) Any {
     V v;
 };
-template <class V> __device__ __forceinline__ void store_any(void *p, V v) { ((Any<V> *)p)->v = v; }
+template <class V> __device__ __forceinline__ void store_any(void *p, V v)
+{
+    static_assert(alignof(Any<V>) == 1, "a type that cannot be packed");
+    ((Any<V> *)p)->v = v;
+}
 
 // Rounds and stores a wave's 16 MT x 64 sums (gated: 32 columns of each
 // projection): q0 and p0 are its first row and column, z the product of a batch.
@@ -137,8 +143,8 @@ __device__ __forceinline__ void epilogue(const GemmArgs &a, const f4_t (&acc)[MT
                 for (int i = 0; i < NC / 4; ++i)
                     w[i] = (uint32_t)(uint8_t)code[4 * i] | (uint32_t)(uint8_t)code[4 * i + 1] << 8 |
                            (uint32_t)(uint8_t)code[4 * i + 2] << 16 | (uint32_t)(uint8_t)code[4 * i + 3] << 24;
-                if (NC == 16) store_any(dst, make_uint4(w[0], w[1], w[NC / 4 - 2], w[NC / 4 - 1]));
-                else store_any(dst, make_uint2(w[0], w[1]));
+                if (NC == 16) store_any(dst, u4_t{w[0], w[1], w[NC / 4 - 2], w[NC / 4 - 1]});
+                else store_any(dst, u2_t{w[0], w[1]});
             } else
 #pragma unroll
                 for (int i = 0; i < NC; ++i)
