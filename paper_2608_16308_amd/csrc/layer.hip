@@ -109,12 +109,21 @@ struct Carve {
     }
 };
 // Whether a product gains from copies of its operands in whole 16-byte chunks
-// (`bytes` of them): the tiles that load straight into LDS reach 900 TFLOP/s and
-// more where those through registers reach 400, and a copy is read and written at
-// 4.5 TB/s, after 3 us of launch.
-bool copies_pay(double flops, double bytes, int copies)
+// (`bytes` of them): a copy is read and written at 4.5 TB/s, after 3 us of launch,
+// and the tiles that load straight into LDS then save what the tiles through
+// registers are slower by.  Those lose most where operands are stored across k
+// (`across`: the backward products).  fp16, us through registers / with copies:
+//   linear 1531x1111->2003 27.5 / 31.6, 2000x2001->2003 39.8 / 44.8,
+//          2000x3001->2003 50.0 / 49.0, 4096x4097->4096 192 / 144
+//   dx     100x1111->2003 26.6 / 25.1, 777x1111->2003 38.1 / 30.0,
+//          2000x3001->2003 102 / 74, 4096x4097->4096 297 / 167
+//   dw     100x1111->2003 19.1 / 22.1, 777x1111->2003 42.8 / 27.6,
+//          2000x3001->2003 103 / 73, 4096x4097->4096 326 / 172
+// The rates are set to put the limit between them, 600 (300 across k) TFLOP/s
+// against 900.
+bool copies_pay(double flops, double bytes, int copies, bool across)
 {
-    return flops * (1 / 400e6 - 1 / 900e6) > 2 * bytes / 4.5e6 + 3.0 * copies;  // (us)
+    return flops * (1 / (across ? 300e6 : 600e6) - 1 / 900e6) > 2 * bytes / 4.5e6 + 3.0 * copies;  // (us)
 }
 size_t rows_bytes(int64_t rows, int64_t cols) { return up256((size_t)rows * up8(cols) * 2); }
 
@@ -127,14 +136,15 @@ struct Operand {
 };
 // Copies the operands that are not in whole chunks into the workspace, if that
 // pays and they fit; true if they all are then.
-hipError_t make_whole(const LayerWork &w, Operand *const *ops, int n, double flops, Carve &c, size_t room, hipStream_t s, bool *padded)
+hipError_t make_whole(const LayerWork &w, Operand *const *ops, int n, double flops, bool across, Carve &c, size_t room,
+                      hipStream_t s, bool *padded)
 {
     size_t bytes = 0;
     int copies = 0;
     *padded = false;
     for (int i = 0; i < n; ++i)
         if (!ops[i]->whole()) bytes += rows_bytes(ops[i]->rows, ops[i]->cols), ++copies;
-    if (!copies || !c.base || c.used + bytes > room || !copies_pay(flops, (double)bytes, copies)) return hipSuccess;
+    if (!copies || !c.base || c.used + bytes > room || !copies_pay(flops, (double)bytes, copies, across)) return hipSuccess;
     for (int i = 0; i < n; ++i) {
         Operand &o = *ops[i];
         if (o.whole()) continue;
@@ -219,7 +229,7 @@ static dbs_status forward_operands(dbs_layer *L, const char *fn, Operand *const 
     bool padded = false;
     Carve c{(uint8_t *)d_work};
     if (a.qn > ROWS_TOKENS)
-        LAYER_TRY(make_whole(L->w, ops, n, 2.0 * (n - 1) * a.qn * a.kn * a.pn, c, work_bytes, L->stream, &padded), fn);
+        LAYER_TRY(make_whole(L->w, ops, n, 2.0 * (n - 1) * a.qn * a.kn * a.pn, false, c, work_bytes, L->stream, &padded), fn);
     a.p_padded = a.q_padded = padded;
     a.q[0] = ops[0]->p, a.ldq[0] = ops[0]->ld;
     for (int i = 1; i < n; ++i) a.p[i - 1] = ops[i]->p, a.ldp[i - 1] = ops[i]->ld;
@@ -232,7 +242,7 @@ dbs_status dbs_forward_work(const dbs_layer *L, int gated, int32_t t, int32_t n_
     if (!bytes) return dbs_fail(DBS_ERR_ARG, "dbs_forward_work: bytes is NULL");
     const int n = gated ? 2 : 1;
     const size_t x = rows_bytes(t, n_in), w = n * rows_bytes(n_out, n_in);
-    *bytes = t > ROWS_TOKENS && copies_pay(2.0 * n * t * n_in * n_out, (double)std::min(x, w), 1) ? x + w : 0;
+    *bytes = t > ROWS_TOKENS && copies_pay(2.0 * n * t * n_in * n_out, (double)std::min(x, w), 1, false) ? x + w : 0;
     return DBS_OK;
 }
 
@@ -295,8 +305,8 @@ dbs_status dbs_backward_work(const dbs_layer *L, int gated, dbs_act act, int32_t
     if (whole) return DBS_OK;
     const double flops = 2.0 * n * t * n_in * n_out;
     const size_t x = rows_bytes(t, n_in), w = rows_bytes(n_out, n_in);
-    if (copies_pay(flops, (double)w, 1)) *bytes += n * w;
-    if (!x_codes && copies_pay(flops, (double)x, 1)) *bytes += x;
+    if (copies_pay(flops, (double)w, 1, true)) *bytes += n * w;
+    if (!x_codes && copies_pay(flops, (double)x, 1, true)) *bytes += x;
     return DBS_OK;
 }
 
@@ -310,7 +320,7 @@ static dbs_status gradients(dbs_layer *L, const char *fn, dbs_dtype dt, int32_t 
     const double flops = 2.0 * n * t * n_in * n_out;
     bool padded = false;
     if (d_dx) {
-        LAYER_TRY(make_whole(L->w, w, n, flops, b.c, room, L->stream, &padded), fn);
+        LAYER_TRY(make_whole(L->w, w, n, flops, true, b.c, room, L->stream, &padded), fn);
         GemmArgs a{};
         for (int i = 0; i < n; ++i) a.p[i] = w[i]->p, a.ldp[i] = w[i]->ld, a.q[i] = dz[i], a.ldq[i] = ldz;
         a.pn = n_in, a.qn = t, a.kn = n_out, a.segs = n, a.batch = 1;
@@ -324,7 +334,7 @@ static dbs_status gradients(dbs_layer *L, const char *fn, dbs_dtype dt, int32_t 
             LAYER_TRY(launch_unpack(bf, x->d_codes, x->d_exps, t, n_in, b.x, b.ldx, L->w.cus, L->stream), fn);
             xv.p = b.x, xv.ld = b.ldx;
             padded = true;
-        } else LAYER_TRY(make_whole(L->w, ops, 1, flops, b.c, room, L->stream, &padded), fn);
+        } else LAYER_TRY(make_whole(L->w, ops, 1, flops, true, b.c, room, L->stream, &padded), fn);
         GemmArgs a{};
         for (int i = 0; i < n; ++i) a.q[i] = dz[i], a.ldq[i] = ldz, a.y[i] = dw[i], a.ldy[i] = lddw[i];
         a.p[0] = xv.p, a.ldp[0] = xv.ld, a.p_padded = padded, a.q_padded = own_dz, a.scale = scale;

@@ -10,7 +10,6 @@
 namespace dbs {
 
 typedef float f4_t __attribute__((ext_vector_type(4)));
-typedef float f2_t __attribute__((ext_vector_type(2)));
 
 // The two element types.  V8 is a 16-byte chunk of them, and mma() one
 // 16x16x32 step on the matrix cores: lane l gives row l % 16 of a and column

@@ -642,9 +642,14 @@ static hipError_t launch_tile(const LayerWork &w, GemmArgs a, hipStream_t s)
 }
 
 // Microseconds that a call takes with each of the tiles: its steps, at what a
-// step of each costs with all compute units at it (256x256: 1250 TFLOP/s;
-// 128x128 with four stages: 830; 64x128 with three, two workgroups to a compute
-// unit: 700; the 128x128 through registers: 550).
+// step of each costs with all compute units at it.  bf16 products of 4096 and 8192
+// rows, TFLOP/s forward / backward: 256x256 1250 to 1380 / 1160 to 1320; 128x128
+// with four stages 790 to 920 / 570 to 640; 64x128 with three, two workgroups to a
+// compute unit, 750 to 840 / 650 to 690.  So the backward products, which read
+// operands stored across k, have no use for 128x128 (dx of 2048 columns, 320 tokens:
+// 19.1 us, 64x128 17.1; 4096x4096, 1024 tokens: 60.4, 56.5, 256x256 53.2).  Over
+// forward and backward products of 40 to 4096 tokens and 1024 to 11008 columns the
+// choice is 1 to 2% from the best of the tiles, at most 25%.
 template <class X, int KIND> static double estimate(const LayerWork &w, GemmArgs a, int tile)
 {
     double steps = 0;
@@ -663,11 +668,13 @@ template <class X, int KIND> static hipError_t launch_kind(const LayerWork &w, c
         if (a.qn <= 64) return launch_tile<X, KIND, 2, 2, 2, 0, 2>(w, a, s);
         return launch_tile<X, KIND, 2, 2, 4, 0, 1>(w, a, s);
     }
+    constexpr bool FORWARD = KIND == G_LINEAR || KIND == G_GATED;
     int tile = 0;
-    for (int i = 1; i < 3; ++i)
+    for (int i = FORWARD ? 1 : 2; i < 3; ++i)
         if (estimate<X, KIND>(w, a, i) < estimate<X, KIND>(w, a, tile)) tile = i;
     if (tile == 0) return launch_tile<X, KIND, 2, 4, 8, 2>(w, a, s);
-    if (tile == 1) return launch_tile<X, KIND, 4, 2, 2, 4>(w, a, s);
+    if constexpr (FORWARD)
+        if (tile == 1) return launch_tile<X, KIND, 4, 2, 2, 4>(w, a, s);
     return launch_tile<X, KIND, 2, 2, 2, 3>(w, a, s);
 }
 
