@@ -68,10 +68,9 @@ def _dtype_code(torch, t, name):
     raise _arg_error(f"{name} has dtype {t.dtype}, expected torch.float16 or torch.bfloat16")
 
 
-def _check_dims(shape, name):
-    """Sizes are handed on as 32-bit numbers, which would drop the upper bits."""
-    if max(shape) > MAX_DIM:
-        raise DbsError(DBS_ERR_UNSUPPORTED, f"{name} has shape {tuple(shape)}: size above 2^30")
+def _too_large(shape, name):
+    """(Sizes are handed on as 32-bit numbers, which would drop the upper bits.)"""
+    return DbsError(DBS_ERR_UNSUPPORTED, f"{name} has shape {tuple(shape)}: size above 2^30")
 
 
 def check_rows(t, name, dtype, device, rows, cols):
@@ -86,7 +85,8 @@ def check_rows(t, name, dtype, device, rows, cols):
     if t.dim() != 2:
         raise _arg_error(f"{name} must have 2 dimensions, not {t.dim()}")
     r, c = t.shape
-    _check_dims(t.shape, name)
+    if r > MAX_DIM or c > MAX_DIM:
+        raise _too_large(t.shape, name)
     if (rows is not None and r != rows) or (cols is not None and c != cols):
         raise _arg_error(f"{name} has shape {tuple(t.shape)}, expected ({'any' if rows is None else rows}, "
                          f"{'any' if cols is None else cols})")
@@ -107,7 +107,8 @@ def check_vector(t, name, dtype, device, n):
 
 
 def check_checkpoint(torch, c, name, dtype, device, rows, cols):
-    _check_dims((rows, cols), name)
+    if rows > MAX_DIM or cols > MAX_DIM:
+        raise _too_large((rows, cols), name)
     if c.dtype != dtype:
         raise _arg_error(f"{name} holds values of {c.dtype}, expected {dtype}")
     for t, part, dt, shape in ((c.codes, "codes", torch.int8, (rows, cols)),
@@ -153,14 +154,9 @@ _node = None
 
 
 def _no_graph(torch, call, inputs, outs):
-    """The outputs of a forward call.  Where autograd is asked for a gradient they
-    carry a node whose backward pass raises: without one the gradient would be
-    missing with no word."""
-    for t in inputs:
-        if t is not None and t.requires_grad:
-            break
-    else:
-        return outs
+    """The outputs of a forward call of which some input requires a gradient.  Where
+    autograd is on they carry a node whose backward pass raises: without one the
+    gradient would be missing with no word."""
     if not torch.is_grad_enabled():
         return outs
     global _node
@@ -299,8 +295,10 @@ class LayerContext:
                 None if bias is None else bias.data_ptr(), act_code, None if residual is None else residual.data_ptr(),
                 ldr, out.data_ptr(), n_out if given is None else ldy, None if keep is None else ctypes.byref(keep), at, size))
             return out, kept
-        inputs = (x, w, bias, residual)
-        out, kept = _no_graph(self._torch, "linear", inputs, self._call(body, (*inputs, given)))
+        out, kept = self._call(body, (x, w, bias, residual, given))
+        if x.requires_grad or w.requires_grad or bias is not None and bias.requires_grad or \
+                residual is not None and residual.requires_grad:
+            out, kept = _no_graph(self._torch, "linear", (x, w, bias, residual), (out, kept))
         out = out[0] if one else out
         return out if save == "none" else (out, kept)
 
@@ -335,8 +333,9 @@ class LayerContext:
                 out.data_ptr(), n_out if given is None else ldh, None if kg is None else ctypes.byref(kg),
                 None if ku is None else ctypes.byref(ku), at, size))
             return out, gate, up
-        inputs = (x, w_gate, w_up)
-        out, gate, up = _no_graph(self._torch, "gated", inputs, self._call(body, (*inputs, given)))
+        out, gate, up = self._call(body, (x, w_gate, w_up, given))
+        if x.requires_grad or w_gate.requires_grad or w_up.requires_grad:
+            out, gate, up = _no_graph(self._torch, "gated", (x, w_gate, w_up), (out, gate, up))
         out = out[0] if one else out
         return out if save == "none" else (out, gate, up)
 
