@@ -508,7 +508,7 @@ dbs_status dbs_basic_spmspv(dbs_basic_matrix *B, dbs_path path, int32_t x_nnz, c
  * below are rounded to the element type before they are multiplied again.  In
  * DBS_F16, where the largest finite magnitude of them in a call is above 65504 or
  * below 2^-8, they are rounded to that type times a power of two that all of them
- * share (the largest then between 2^14 and 2^15 of it), so that gradients within
+ * share (the largest then between 2^14 and 2^15 of it; no less than 2^-60), so that gradients within
  * the type's range are found where these products are not.
  * Sizes are at most 2^30.  Outputs must not overlap inputs, except that y may
  * be the residual itself.  NaN and infinities propagate as in the formulas. */

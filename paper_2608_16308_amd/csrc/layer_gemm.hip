@@ -270,8 +270,10 @@ template <class X, int KIND, int NWQ, int NWP, int MT> __global__ __launch_bound
 
 // A tile of the product whose operands may stand anywhere: chunks come through
 // registers, PF steps ahead, since loads straight into LDS need whole 16-byte
-// chunks.  Bound by the edge handling and the wait of one barrier a step: 550
-// TFLOP/s with 128x128 and all compute units at it.
+// chunks.  Bound by the edge handling and the wait of one barrier a step.  fp16
+// rows of odd length, all compute units at it: forward 650 to 730 TFLOP/s
+// (1531x7001->5003, 4096x4097->4096), across k 420 to 460; 777x1111->2003, which
+// has few steps, 137 and 90.
 template <class X, int KIND, int NWQ, int NWP, int MT, int PF>
 __global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_tile(GemmArgs a)
 {
@@ -416,10 +418,11 @@ __global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_tile(GemmArgs a)
 
 // A tile of the product whose operands are made of whole 16-byte chunks, which
 // go straight into LDS, NS steps deep.  The fragments of a half step are read
-// while the other half is multiplied, so that the matrix cores bound it: the
-// 256x256 tile gives each byte of LDS the most products (gated
-// 4096x4096->11008 bf16: 628 us, 1180 TFLOP/s), the smaller tiles with three
-// and four stages serve products with too few large ones.
+// while the other half is multiplied.  The 256x256 tile gives each byte of LDS the
+// most products; the smaller tiles with three and four stages serve products with
+// too few large ones.  Bound by the reads of LDS beside the products, and with two
+// stages by the wait for a whole step's loads: the matrix cores are busy 47 to 58%
+// of the time (gated 4096x4096->11008 bf16 keeping 8 bits: 694 us, 1060 TFLOP/s).
 template <class X, int KIND, int NWQ, int NWP, int MT, int NS>
 __global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_block(GemmArgs a)
 {
