@@ -612,6 +612,127 @@ dbs_status dbs_unpack(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t cols, co
                       const uint8_t *d_exps, void *d_y, int64_t ldy);
 
 /* ---------------------------------------------------------------------- */
+/* The edges of a feed-forward block: the norm before it, the join with the */
+/* residual stream after it, dropout, and their gradients.                  */
+/* ---------------------------------------------------------------------- */
+/* Tensors, types, sizes and contexts as above.  Statistics and sums are held in
+ * 32 bits and each output is rounded once.  Norms' weights and biases are
+ * vectors of n elements of the call's type.                                 */
+
+/* Blocks of 8-bit floating point (e4m3) of a matrix [rows, cols]: a block is
+ * DBS_BLOCK8 columns of a row (row blocks), or of DBS_BLOCK8 rows (tile
+ * blocks).  Codes: rows of ceil(cols / 128) * 128 bytes, zeros behind the last
+ * column, aligned to 16 bytes.  Exponents: for each row (128 rows) a byte e + 127
+ * for each block, rows of ceil(cols / 512) * 4 bytes, 127 behind the last,
+ * aligned to 4 bytes.  With a the largest finite magnitude of a block, e is the
+ * least integer with a <= 448 * 2^e and e >= -127; a code is the e4m3 number
+ * nearest to v * 2^-e (ties to even), NaN for a value that is not finite.     */
+#define DBS_BLOCK8 128
+typedef struct {
+    void *d_codes;
+    uint8_t *d_exps;
+} dbs_blocks8;
+
+/* norm(x) = xh * weight + bias, by rows:  DBS_NORM_RMS xh = x / sqrt(mean(x^2) +
+ * eps);  DBS_NORM_LAYER xh = (x - mean(x)) / sqrt(var(x) + eps), var the mean
+ * square around the mean.  weight, bias: NULL stands for ones and zeros.  A NULL
+ * descriptor or DBS_NORM_NONE: no norm.                                      */
+typedef enum { DBS_NORM_NONE = 0, DBS_NORM_RMS = 1, DBS_NORM_LAYER = 2 } dbs_norm_kind;
+typedef struct {
+    dbs_norm_kind kind;
+    float eps;
+    const void *d_weight, *d_bias;
+} dbs_norm_desc;
+
+/* Dropout, 0 <= p <= 1.  Chunk c = row * ceil(n / 8) + column / 8 of a matrix has
+ * the four words of Philox4x32-10 with counter (c mod 2^32, c / 2^32, offset mod
+ * 2^32, offset / 2^32) and key (seed mod 2^32, seed / 2^32); element j of the
+ * chunk the lower (j even) or upper 16 bits of word j / 2.  With T = p * 65536
+ * rounded to a whole number, an element is 0 where its bits are below T and
+ * multiplied by 65536 / (65536 - T) elsewhere.  d_rng: NULL, or seed and offset
+ * in device memory, read when the call runs (so that a captured call can be given
+ * others).                                                                   */
+typedef struct {
+    double p;
+    uint64_t seed, offset;
+    const uint64_t *d_rng;
+} dbs_drop_desc;
+
+/* y = norm(x), as 16-bit values (y may be x), or as row blocks of 8 bits of these
+ * values (y8; d_y NULL then).                                                */
+dbs_status dbs_norm(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t n, const void *d_x, int64_t ldx,
+                    const dbs_norm_desc *norm, void *d_y, int64_t ldy, const dbs_blocks8 *y8);
+
+/* stream = scale * residual + gate * dropout(after(branch));  h = before(stream),
+ * of the unrounded stream.  gate: NULL (ones), a vector [n] (ldg 0) or [rows, n].
+ * after, before, drop: NULL allowed; without before no h.  stream may be the
+ * residual or the branch, h the branch; h as 16-bit values, or as row blocks of
+ * 8 bits of these values (h8; d_h NULL then).                                */
+dbs_status dbs_join(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t n, const void *d_branch, int64_t ldb,
+                    const void *d_residual, int64_t ldr, const dbs_norm_desc *after, const dbs_norm_desc *before,
+                    const void *d_gate, int64_t ldg, float scale, const dbs_drop_desc *drop, void *d_stream, int64_t lds,
+                    void *d_h, int64_t ldh, const dbs_blocks8 *h8);
+
+/* Bytes of device memory (aligned to 256, free again when the call is done) that
+ * the gradients below need; sums: how many vectors they are asked for.        */
+dbs_status dbs_edge_work(const dbs_layer *L, int32_t rows, int32_t n, int sums, size_t *bytes);
+
+/* Gradients of dbs_norm at x:  dx (+ add [rows, n], NULL allowed), and the sums
+ * over the rows dweight, dbias [n].  Outputs may be NULL.                     */
+dbs_status dbs_norm_backward(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t n, const void *d_dy, int64_t lddy,
+                             const void *d_x, int64_t ldx, const dbs_norm_desc *norm, const void *d_add, int64_t ldadd,
+                             void *d_dx, int64_t lddx, void *d_dweight, void *d_dbias, void *d_work, size_t work_bytes);
+
+/* Gradients of dbs_join, with ds = dstream (NULL: zeros) + the gradient of h taken
+ * through before at the rounded stream:  dresidual = scale * ds; dgate = ds *
+ * dropout(after(branch)), [rows, n] or its sum over the rows; dbranch = gate * ds
+ * through dropout and after; the norms' weights and biases.  branch is read with
+ * a gate or a norm after, stream and dh with a norm before.  Outputs may be NULL. */
+dbs_status dbs_join_backward(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t n, const void *d_dstream, int64_t ldds,
+                             const void *d_dh, int64_t lddh, const void *d_branch, int64_t ldb, const void *d_stream,
+                             int64_t lds, const dbs_norm_desc *after, const dbs_norm_desc *before, const void *d_gate,
+                             int64_t ldg, float scale, const dbs_drop_desc *drop, void *d_dresidual, int64_t lddr,
+                             void *d_dbranch, int64_t lddb, void *d_dgate, int64_t lddg, void *d_dafter_weight,
+                             void *d_dafter_bias, void *d_dbefore_weight, void *d_dbefore_bias, void *d_work,
+                             size_t work_bytes);
+
+/* y = dropout(x) (y may be x); with the same drop it is its own gradient.      */
+dbs_status dbs_dropout(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t n, const void *d_x, int64_t ldx,
+                       const dbs_drop_desc *drop, void *d_y, int64_t ldy);
+
+/* Blocks of x [rows, cols], or (across) of its transpose [cols, rows]; tile: tile
+ * blocks, else row blocks.                                                    */
+dbs_status dbs_pack8(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t cols, const void *d_x, int64_t ldx, int tile,
+                     int across, const dbs_blocks8 *out);
+/* The values of blocks [rows, cols]: code * 2^e, limited to the type's largest
+ * finite number and rounded to it.                                            */
+dbs_status dbs_unpack8(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t cols, int tile, const dbs_blocks8 *x, void *d_y,
+                       int64_t ldy);
+
+/* y = x w^T + bias + residual with both factors in 8 bits: w [n_out, n_in] in tile
+ * blocks, x [tokens, n_in] in row blocks (x8), or 16-bit values (d_x; x8 NULL) that
+ * are brought into row blocks in the workspace (dbs_linear8_work bytes; none for
+ * x8).  Products of codes are exact; eight neighbouring ones are added in fixed
+ * point (each cut to a multiple of 2^-13 of the largest, rounded down to a power of
+ * two), the sums of eight in 32 bits.  n_in at most 2^24; y may be the residual.  */
+dbs_status dbs_linear8_work(const dbs_layer *L, int32_t tokens, int32_t n_in, int32_t n_out, size_t *bytes);
+dbs_status dbs_linear8(dbs_layer *L, dbs_dtype dt, int32_t tokens, int32_t n_in, int32_t n_out, const void *d_x, int64_t ldx,
+                       const dbs_blocks8 *x8, const dbs_blocks8 *w8, const void *d_bias, const void *d_residual, int64_t ldr,
+                       void *d_y, int64_t ldy, void *d_work, size_t work_bytes);
+
+/* Its gradients: dx = dy8 w with dy in row blocks; dw = dy8^T x8 with the
+ * transposes of dy and x in row blocks (blocks of 128 tokens); db = the sum of dy.
+ * x: 16-bit values, or the row blocks of the forward pass (x8), whose values are
+ * taken.  Outputs may be NULL; w8 without dx, x without dw.  tokens and n_out at
+ * most 2^24.                                                                  */
+dbs_status dbs_linear8_backward_work(const dbs_layer *L, int32_t tokens, int32_t n_in, int32_t n_out, int want_dx,
+                                     int want_dw, int want_db, size_t *bytes);
+dbs_status dbs_linear8_backward(dbs_layer *L, dbs_dtype dt, int32_t tokens, int32_t n_in, int32_t n_out, const void *d_dy,
+                                int64_t lddy, const void *d_x, int64_t ldx, const dbs_blocks8 *x8, const dbs_blocks8 *w8,
+                                void *d_dx, int64_t lddx, void *d_dw, int64_t lddw, void *d_db, void *d_work,
+                                size_t work_bytes);
+
+/* ---------------------------------------------------------------------- */
 /* Measurement hooks.                                                     */
 /* ---------------------------------------------------------------------- */
 

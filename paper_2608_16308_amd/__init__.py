@@ -13,7 +13,9 @@ current stream only.
     level, parent = ctx.bfs(A, source)
 
 The dense layers beside the pruned ones (linear, gated, their gradients, 8-bit
-activation checkpoints) run on a ``LayerContext`` (``layer.py``).
+activation checkpoints), the norms, joins and dropout around them (``edges.py``)
+and products in 8-bit floating point (``float8.py``) run on a ``LayerContext``
+(``layer.py``).
 """
 from __future__ import annotations
 
@@ -24,10 +26,12 @@ import numpy as np
 from . import _lib
 from ._lib import (BLOCK_TYPE_NAMES, DBS_F16, DBS_F32, DBS_OR_AND, DBS_PATH_AUTO, DBS_PATH_PULL,
                    DBS_PATH_PUSH, DBS_PATTERN, DBS_PLUS_TIMES, DbsError, check)
+from .edges import JoinGrads, Norm
+from .float8 import Blocks8
 from .layer import Checkpoint, LayerContext
 
 __all__ = ["HostMatrix", "Matrix", "Context", "BasicMatrix", "DbsError", "default_opts", "storage_model",
-           "spmspv_noalloc", "LayerContext", "Checkpoint",
+           "spmspv_noalloc", "LayerContext", "Checkpoint", "Norm", "JoinGrads", "Blocks8",
            "DBS_F32", "DBS_F16", "DBS_PATTERN", "PATHS"]
 
 PATHS = {"auto": DBS_PATH_AUTO, "push": DBS_PATH_PUSH, "pull": DBS_PATH_PULL}

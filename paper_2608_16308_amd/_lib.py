@@ -15,6 +15,8 @@ DBS_OK, DBS_ERR_ARG, DBS_ERR_ALLOC, DBS_ERR_DEVICE, DBS_ERR_UNSUPPORTED, DBS_ERR
 DBS_F32, DBS_F16, DBS_PATTERN, DBS_BF16 = 0, 1, 2, 3
 DBS_ACT_NONE, DBS_ACT_RELU, DBS_ACT_SILU, DBS_ACT_GELU, DBS_ACT_GELU_TANH = range(5)
 DBS_CK_GROUP = 32
+DBS_NORM_NONE, DBS_NORM_RMS, DBS_NORM_LAYER = range(3)
+DBS_BLOCK8 = 128
 DBS_PLUS_TIMES, DBS_OR_AND = 0, 1
 DBS_PATH_AUTO, DBS_PATH_PUSH, DBS_PATH_PULL = 0, 1, 2
 DBS_BLK_COO, DBS_BLK_DENSE, DBS_BLK_FCSR, DBS_BLK_FCSC, DBS_BLK_CSR = range(5)
@@ -33,6 +35,8 @@ EXPORTED = [
     "dbs_spmspv_noalloc", "dbs_ctx_set_single_launch",
     "dbs_layer_create", "dbs_layer_destroy", "dbs_linear", "dbs_gated", "dbs_forward_work", "dbs_backward_work",
     "dbs_linear_backward", "dbs_gated_backward", "dbs_pack", "dbs_unpack",
+    "dbs_norm", "dbs_norm_backward", "dbs_join", "dbs_join_backward", "dbs_edge_work", "dbs_dropout",
+    "dbs_pack8", "dbs_unpack8", "dbs_linear8", "dbs_linear8_work", "dbs_linear8_backward", "dbs_linear8_backward_work",
 ]
 DBS_NOALLOC_MAX_DIM = 1 << 20
 
@@ -93,6 +97,19 @@ class Held(ctypes.Structure):
     """dbs_held and dbs_keep."""
     _fields_ = [("d_values", ctypes.c_void_p), ("ld", ctypes.c_int64), ("d_codes", ctypes.c_void_p),
                 ("d_exps", ctypes.c_void_p)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int), ("eps", ctypes.c_float), ("d_weight", ctypes.c_void_p), ("d_bias", ctypes.c_void_p)]
+
+
+class DropDesc(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("d_rng", ctypes.c_void_p)]
+
+
+class Blocks(ctypes.Structure):
+    """dbs_blocks8."""
+    _fields_ = [("d_codes", ctypes.c_void_p), ("d_exps", ctypes.c_void_p)]
 
 
 class DbsError(RuntimeError):
@@ -166,6 +183,25 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                                               P(Held), ctypes.c_int, vp, i64, vp, i64, vp, i64, vp, ctypes.c_size_t]),
         "dbs_pack": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, vp, i64, vp, vp]),
         "dbs_unpack": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, vp, vp, vp, i64]),
+        "dbs_norm": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, vp, i64, P(NormDesc), vp, i64, P(Blocks)]),
+        "dbs_norm_backward": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, vp, i64, vp, i64, P(NormDesc), vp, i64, vp, i64, vp, vp,
+                                             vp, ctypes.c_size_t]),
+        "dbs_join": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, vp, i64, vp, i64, P(NormDesc), P(NormDesc), vp, i64, f32,
+                                    P(DropDesc), vp, i64, vp, i64, P(Blocks)]),
+        "dbs_join_backward": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, P(NormDesc),
+                                             P(NormDesc), vp, i64, f32, P(DropDesc), vp, i64, vp, i64, vp, i64, vp, vp, vp, vp,
+                                             vp, ctypes.c_size_t]),
+        "dbs_edge_work": (ctypes.c_int, [vp, i32, i32, ctypes.c_int, P(ctypes.c_size_t)]),
+        "dbs_dropout": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, vp, i64, P(DropDesc), vp, i64]),
+        "dbs_pack8": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, vp, i64, ctypes.c_int, ctypes.c_int, P(Blocks)]),
+        "dbs_unpack8": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, ctypes.c_int, P(Blocks), vp, i64]),
+        "dbs_linear8_work": (ctypes.c_int, [vp, i32, i32, i32, P(ctypes.c_size_t)]),
+        "dbs_linear8": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, vp, i64, P(Blocks), P(Blocks), vp, vp, i64, vp, i64, vp,
+                                       ctypes.c_size_t]),
+        "dbs_linear8_backward_work": (ctypes.c_int, [vp, i32, i32, i32, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                                     P(ctypes.c_size_t)]),
+        "dbs_linear8_backward": (ctypes.c_int, [vp, ctypes.c_int, i32, i32, i32, vp, i64, vp, i64, P(Blocks), P(Blocks), vp, i64,
+                                                vp, i64, vp, vp, ctypes.c_size_t]),
         "dbs_last_error": (ctypes.c_char_p, []),
         "dbs_version": (ctypes.c_char_p, []),
     }

@@ -1,0 +1,101 @@
+// Blocks of 8-bit floating point: their codes, scales and places in memory.
+#pragma once
+#include "layer.hpp"
+
+namespace dbs {
+
+// A block of E8_BLOCK columns (of a row, or of E8_BLOCK rows) shares the
+// exponent e, the least with a <= 448 * 2^e for its largest finite magnitude a; a
+// value is the e4m3 number nearest to v * 2^-e (ties to even), NaN if it is not
+// finite.  448 is the largest e4m3 number.  A scale that is a power of two costs
+// nothing here that a / 448 would keep: the codes are floating point themselves,
+// so a value has its four bits wherever it lies in their range (of which up to
+// one of 17 binades is given up), and the matrix cores apply such scales
+// themselves.
+constexpr int E8_BLOCK = 128;
+constexpr int E8_BIAS = 127;
+constexpr float E8_MAX = 448.f;
+
+// e of a block with largest finite magnitude a.
+__device__ __forceinline__ int e8_exp(float a)
+{
+    const int k = __builtin_amdgcn_frexp_expf(a);  // a = m 2^k, m in [1/2, 1); 448 = 7/8 2^9
+    const int e = __builtin_amdgcn_frexp_mantf(a) <= 0.875f ? k - 9 : k - 8;
+    return a == 0.f || e < -E8_BIAS ? -E8_BIAS : e;
+}
+// v * 2^-e as it is rounded; NaN if v is not finite.
+__device__ __forceinline__ float e8_scaled(float v, int e)
+{
+    return __builtin_fabsf(v) <= 3.402823466e38f ? __builtin_amdgcn_ldexpf(v, -e) : __builtin_nanf("");
+}
+// The codes of eight values.
+__device__ __forceinline__ uint2 e8_codes(const float (&v)[8], int e)
+{
+    int w[2] = {0, 0};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(e8_scaled(v[4 * h], e), e8_scaled(v[4 * h + 1], e), w[h], false);
+        w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(e8_scaled(v[4 * h + 2], e), e8_scaled(v[4 * h + 3], e), w[h], true);
+    }
+    return uint2{(uint32_t)w[0], (uint32_t)w[1]};
+}
+// The values of eight codes, limited to the finite numbers of the 16-bit type
+// (the largest of a block may reach the next power of two beyond them).
+template <class X> __device__ __forceinline__ void e8_values(uint2 c, int e, float (&v)[8])
+{
+    const int w[2] = {(int)c.x, (int)c.y};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        v[4 * h] = __builtin_amdgcn_cvt_f32_fp8(w[h], 0), v[4 * h + 1] = __builtin_amdgcn_cvt_f32_fp8(w[h], 1);
+        v[4 * h + 2] = __builtin_amdgcn_cvt_f32_fp8(w[h], 2), v[4 * h + 3] = __builtin_amdgcn_cvt_f32_fp8(w[h], 3);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float s = __builtin_amdgcn_ldexpf(v[i], e);
+        v[i] = s > X::MAX ? X::MAX : s < -X::MAX ? -X::MAX : s;  // (NaN stays)
+    }
+}
+
+// Codes of a matrix: rows of whole blocks, zeros behind the last column.
+// Exponents + 127: for each row (or E8_BLOCK rows) one byte for each block, rows
+// of whole fours, 127 behind the last.
+__host__ __device__ __forceinline__ int64_t e8_blocks(int64_t cols) { return (cols + E8_BLOCK - 1) / E8_BLOCK; }
+__host__ __device__ __forceinline__ int64_t e8_ld(int64_t cols) { return e8_blocks(cols) * E8_BLOCK; }
+__host__ __device__ __forceinline__ int64_t e8_ldexp(int64_t cols) { return (e8_blocks(cols) + 3) / 4 * 4; }
+
+// A matrix of `rows` rows in blocks.
+struct Blocks {
+    uint8_t *codes, *exps;
+    int64_t ld, lde;
+    int32_t shift;  // exponents of row r stand in row r >> shift
+};
+
+// x (16-bit values, or row blocks) into blocks: of x, of its transpose, or both
+// in one pass; the sums of its columns over each E8_BLOCK rows.
+struct Pack8Args {
+    const void *x;
+    int64_t ldx;
+    Blocks from;    // x as row blocks (codes not NULL)
+    int32_t rows, cols;
+    int32_t tile;   // one exponent for each tile
+    Blocks to, turned;  // codes NULL: not wanted
+    float *sums;    // NULL, or [ceil(rows / E8_BLOCK)][cols]
+    int32_t tiles_c, first;  // filled by the launcher
+};
+hipError_t launch_pack8(bool bf16, Pack8Args a, hipStream_t s);
+hipError_t launch_unpack8(bool bf16, const Blocks &b, int32_t rows, int32_t cols, void *y, int64_t ldy, int32_t cus, hipStream_t s);
+// The transpose of a matrix in tile blocks.
+hipError_t launch_turn8(const Blocks &b, int32_t rows, int32_t cols, const Blocks &to, hipStream_t s);
+
+// y = q p^T + bias + res: p [pn, kn], q [qn, kn] in blocks along k.
+struct Mul8Args {
+    Blocks p, q;
+    int32_t pn, qn, kn;
+    const void *bias, *res;
+    int64_t ldr;
+    void *y;
+    int64_t ldy;
+};
+hipError_t launch_mul8(const LayerWork &w, bool bf16, const Mul8Args &m, hipStream_t s);
+
+}  // namespace dbs

@@ -252,7 +252,7 @@ template <int NT, int MT> __device__ __forceinline__ void leave_part(const GemmA
 
 // The sums of the tiles in parts, added in the order of the parts; a workgroup
 // takes 16 rows of each of a tile's waves.
-template <class X, int KIND, int NWQ, int NWP, int MT> __global__ __launch_bounds__(64 * NWQ * NWP) void k_join(GemmArgs a)
+template <class X, int KIND, int NWQ, int NWP, int MT> static __global__ __launch_bounds__(64 * NWQ * NWP) void k_join(GemmArgs a)
 {
     using C = Tile<X, KIND, NWQ, NWP, MT>;
     const int tid = (int)threadIdx.x, wave = wave_id(), wq = wave / NWP, wp = wave % NWP;

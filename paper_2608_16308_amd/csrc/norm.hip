@@ -1,0 +1,495 @@
+// Norms before and after a block, the join with the residual stream, dropout,
+// and their gradients.
+#include <algorithm>
+
+#include "float8.hpp"
+#include "norm.hpp"
+
+namespace dbs {
+
+// A store at any alignment of its elements.
+template <class X> __device__ __forceinline__ void put_eight(typename X::T *p, int left, const float (&v)[8])
+{
+    typename X::V8 t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = (typename X::T)v[i];
+    if (left >= 8) ((Eight<X> *)p)->v = t;
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) p[i] = t[i];
+}
+// Eight elements of a row of which `left` are there; the rest reads as zeros.
+template <class X> __device__ __forceinline__ typename X::V8 get_eight(const typename X::T *p, int left)
+{
+    if (left >= 8) return load_eight<X>(p);
+    typename X::V8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (typename X::T)0.f;
+    return v;
+}
+template <class X> __device__ __forceinline__ void get_floats(const typename X::T *p, int left, float (&v)[8])
+{
+    const typename X::V8 t = get_eight<X>(p, left);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
+}
+// The same of a vector that may be missing: `none` then.
+template <class X>
+__device__ __forceinline__ typename X::V8 get_vector(const void *p, int col, int left, float none)
+{
+    if (p) return get_eight<X>((const typename X::T *)p + col, left);
+    typename X::V8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (typename X::T)none;
+    return v;
+}
+
+// Sums over a workgroup, the same in all its threads: `red` holds two rounds, so
+// that one barrier each is enough.
+template <int WAVES> struct GroupSum {
+    float (*red)[WAVES];
+    int round = 0;
+    __device__ float operator()(float v)
+    {
+        v = wave_sum(v);
+        if (WAVES == 1) return v;
+        if (lane_id() == 0) red[round][wave_id()] = v;
+        __syncthreads();
+        float s = red[round][0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) s += red[round][w];
+        round ^= 1;
+        return s;
+    }
+};
+
+// Chunk c of a row of h into 8 bits, the 16 of a block in neighbouring lanes (all
+// lanes of the wave come here); `last` chunks make whole blocks.
+template <class X>
+__device__ __forceinline__ void put_codes(const EdgeArgs &a, int64_t row, int c, int last, const float (&h)[8])
+{
+    float v[8], big = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)(typename X::T)h[i], big = fmaxf(big, ck_mag(v[i]));
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) big = fmaxf(big, __shfl_xor(big, o, 64));
+    if (c >= last) return;
+    const int e = e8_exp(big);
+    *(uint2 *)(a.codes + row * e8_ld(a.n) + 8 * c) = e8_codes(v, e);
+    if (c % 16) return;
+    uint8_t *exps = a.exps + row * e8_ldexp(a.n);
+    exps[c / 16] = (uint8_t)(e + E8_BIAS);
+    if (c + 16 == last)
+        for (int b = last / 16; b < (int)e8_ldexp(a.n); ++b) exps[b] = E8_BIAS;
+}
+
+__device__ __forceinline__ void rng_of(const Drop &d, uint64_t &seed, uint64_t &offset)
+{
+    seed = d.rng ? d.rng[0] : d.seed;
+    offset = d.rng ? d.rng[1] : d.offset;
+}
+
+constexpr float DOWN = 8.271806125530277e-25f;  // 2^-80
+
+// The statistics of a row whose values `at(chunk, v)` gives: the mean first, then
+// the squares around it, so that a large mean costs no precision.
+template <int WAVES, class F>
+__device__ __forceinline__ Stat row_stat(const NormOf &nm, int n, GroupSum<WAVES> &total, F &&at)
+{
+    const float by = 1.f / (float)n;
+    for (float f = 1.f;; f = DOWN) {
+        float mean = 0.f, var = 0.f;
+        if (nm.kind == DBS_NORM_LAYER) {
+            for (int c = (int)threadIdx.x; 8 * c < n; c += 64 * WAVES) {
+                float v[8];
+                at(c, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) mean += 8 * c + i < n ? v[i] * f * by : 0.f;
+            }
+            mean = total(mean);
+        }
+        for (int c = (int)threadIdx.x; 8 * c < n; c += 64 * WAVES) {
+            float v[8];
+            at(c, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = 8 * c + i < n ? __builtin_fmaf(v[i], f, -mean) : 0.f;
+                var = __builtin_fmaf(d, d, var);
+            }
+        }
+        var = total(var) * by;
+        if (!(var > 3.402823466e38f) || f != 1.f)
+            return Stat{f, mean, 1.f / sqrtf(var + nm.eps * f * f)};
+    }
+}
+
+// ---------------------------------------------------------------------------
+// rows of any length: read again from the caches for each step
+// ---------------------------------------------------------------------------
+constexpr int LONG_WAVES = 16;
+
+template <class X, bool BRANCH> __global__ __launch_bounds__(64 * LONG_WAVES) void k_edge_long(EdgeArgs a)
+{
+    typedef typename X::T T;
+    __shared__ float red[2][LONG_WAVES];
+    GroupSum<LONG_WAVES> total{red};
+    uint64_t seed, offset;
+    rng_of(a.drop, seed, offset);
+    const int64_t chunks = (a.n + 7) / 8;
+    for (int row = (int)blockIdx.x; row < a.rows; row += (int)gridDim.x) {
+        const T *res = (const T *)a.res + row * a.ldr, *branch = (const T *)a.branch + row * a.ldb;
+        Stat sa{};
+        if (BRANCH && a.after.kind != DBS_NORM_NONE)
+            sa = row_stat(a.after, a.n, total, [&](int c, float(&v)[8]) { get_floats<X>(branch + 8 * c, a.n - 8 * c, v); });
+        // the stream, 8 columns of it
+        auto stream = [&](int c, float(&s)[8]) {
+            const int col = 8 * c, left = a.n - col;
+            get_floats<X>(res + col, left, s);
+            if constexpr (BRANCH) {
+                float u[8];
+                get_floats<X>(branch + col, left, u);
+                if (a.after.kind != DBS_NORM_NONE) {
+                    const typename X::V8 w = get_vector<X>(a.after.w, col, left, 1.f), b = get_vector<X>(a.after.b, col, left, 0.f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) u[i] = __builtin_fmaf(sa.xh(u[i]), (float)w[i], (float)b[i]);
+                }
+                if (a.drop.threshold) drop_eight(a.drop, seed, offset, row * chunks + c, u);
+                const typename X::V8 g = get_vector<X>(a.gate ? (const T *)a.gate + row * a.ldg : nullptr, col, left, 1.f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[i] = __builtin_fmaf((float)g[i], u[i], a.scale * s[i]);
+            }
+        };
+        Stat sb{};
+        if (a.before.kind != DBS_NORM_NONE) sb = row_stat(a.before, a.n, total, stream);
+        __syncthreads();  // (the stream may replace the residual)
+        const int last = a.codes ? (int)e8_blocks(a.n) * 16 : (int)chunks;
+        for (int c = (int)threadIdx.x; c < (last + 63) / 64 * 64; c += 64 * LONG_WAVES) {
+            const int col = 8 * c, left = a.n - col;
+            float s[8] = {}, h[8] = {};
+            if (left > 0) {
+                stream(c, s);
+                if (BRANCH) put_eight<X>((T *)a.stream + row * a.lds + col, left, s);
+                if (a.before.kind != DBS_NORM_NONE) {
+                    const typename X::V8 w = get_vector<X>(a.before.w, col, left, 1.f), b = get_vector<X>(a.before.b, col, left, 0.f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[i] = i < left ? __builtin_fmaf(sb.xh(s[i]), (float)w[i], (float)b[i]) : 0.f;
+                    if (a.h) put_eight<X>((T *)a.h + row * a.ldh + col, left, h);
+                }
+            }
+            if (a.codes) put_codes<X>(a, row, c, last, h);
+        }
+        __syncthreads();
+    }
+}
+
+// One row's chunk of the backward pass: what it reads, and what follows from it.
+template <class X, bool BRANCH> struct BackChunk {
+    float dh[8], xb[8], d[8], g[8];       // gradient of h, normalised stream, ds*, dh w
+    float ub[8], keep[8], gate[8], du[8]; // normalised branch or branch, what dropout multiplies by, gradient behind the norm
+};
+// The part up to ds* (everything that `before` needs: its statistics, and with
+// `means` its two means).
+template <class X, bool BRANCH>
+__device__ __forceinline__ void back_before(const EdgeBackArgs &a, int64_t row, int col, int left, const BackStat &b, bool means,
+                                            BackChunk<X, BRANCH> &k)
+{
+    typedef typename X::T T;
+    if (a.ds) get_floats<X>((const T *)a.ds + row * a.ldds + col, left, k.d);
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k.d[i] = 0.f;
+    if (a.before.kind == DBS_NORM_NONE) return;
+    get_floats<X>((const T *)a.dh + row * a.lddh + col, left, k.dh);
+    get_floats<X>((const T *)a.stream + row * a.lds + col, left, k.xb);
+    const typename X::V8 w = get_vector<X>(a.before.w, col, left, 1.f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        k.xb[i] = b.s.xh(k.xb[i]);
+        k.g[i] = k.dh[i] * (float)w[i];
+        if (means) k.d[i] += b.dx(k.g[i], k.xb[i]);
+    }
+}
+// The part from ds* to the gradient behind `after` (with `means` through it).
+template <class X, bool BRANCH>
+__device__ __forceinline__ void back_after(const EdgeBackArgs &a, int64_t row, int col, int left, uint64_t seed, uint64_t offset,
+                                           const BackStat &f, BackChunk<X, BRANCH> &k)
+{
+    typedef typename X::T T;
+    const int64_t chunks = (a.n + 7) / 8;
+    if (a.branch) get_floats<X>((const T *)a.branch + row * a.ldb + col, left, k.ub);
+    const typename X::V8 g = get_vector<X>(a.gate ? (const T *)a.gate + row * a.ldg : nullptr, col, left, 1.f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        k.keep[i] = 1.f;
+        k.gate[i] = (float)g[i];
+        if (a.after.kind != DBS_NORM_NONE) k.ub[i] = f.s.xh(k.ub[i]);
+    }
+    if (a.drop.threshold) drop_eight(a.drop, seed, offset, row * chunks + col / 8, k.keep);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) k.du[i] = k.keep[i] != 0.f ? k.d[i] * k.gate[i] * k.keep[i] : 0.f;
+}
+
+// The statistics and means of each row.
+template <class X, bool BRANCH> __global__ __launch_bounds__(64 * LONG_WAVES) void k_edge_back_rows(EdgeBackArgs a)
+{
+    typedef typename X::T T;
+    __shared__ float red[2][LONG_WAVES];
+    GroupSum<LONG_WAVES> total{red};
+    uint64_t seed, offset;
+    rng_of(a.drop, seed, offset);
+    const float by = 1.f / (float)a.n;
+    for (int row = (int)blockIdx.x; row < a.rows; row += (int)gridDim.x) {
+        BackStat b{}, f{};
+        if (a.before.kind != DBS_NORM_NONE) {
+            const T *x = (const T *)a.stream + row * a.lds;
+            b.s = row_stat(a.before, a.n, total, [&](int c, float(&v)[8]) { get_floats<X>(x + 8 * c, a.n - 8 * c, v); });
+            float m1 = 0.f, m2 = 0.f;
+            for (int c = (int)threadIdx.x; 8 * c < a.n; c += 64 * LONG_WAVES) {
+                BackChunk<X, BRANCH> k;
+                back_before(a, row, 8 * c, a.n - 8 * c, b, false, k);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (8 * c + i < a.n) m1 = __builtin_fmaf(k.g[i], k.xb[i], m1), m2 += k.g[i];
+            }
+            b.m1 = total(m1) * by;
+            if (a.before.kind == DBS_NORM_LAYER) b.m2 = total(m2) * by;
+        }
+        if (BRANCH && a.after.kind != DBS_NORM_NONE) {
+            const T *x = (const T *)a.branch + row * a.ldb;
+            f.s = row_stat(a.after, a.n, total, [&](int c, float(&v)[8]) { get_floats<X>(x + 8 * c, a.n - 8 * c, v); });
+            float m1 = 0.f, m2 = 0.f;
+            for (int c = (int)threadIdx.x; 8 * c < a.n; c += 64 * LONG_WAVES) {
+                BackChunk<X, BRANCH> k;
+                const int left = a.n - 8 * c;
+                back_before(a, row, 8 * c, left, b, true, k);
+                back_after(a, row, 8 * c, left, seed, offset, f, k);
+                const typename X::V8 w = get_vector<X>(a.after.w, 8 * c, left, 1.f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float g = k.du[i] * (float)w[i];
+                    if (i < left) m1 = __builtin_fmaf(g, k.ub[i], m1), m2 += g;
+                }
+            }
+            f.m1 = total(m1) * by;
+            if (a.after.kind == DBS_NORM_LAYER) f.m2 = total(m2) * by;
+        }
+        if (threadIdx.x == 0) a.stat[2 * (int64_t)row] = b, a.stat[2 * (int64_t)row + 1] = f;
+    }
+}
+
+// Everything else: a workgroup has a strip of 512 columns and a range of rows,
+// a lane eight columns, whose sums it holds.
+constexpr int STRIP = 512, STRIP_WAVES = 4;
+__host__ __device__ __forceinline__ int first_row(int64_t rows, int blocks, int block) { return (int)(rows * block / blocks); }
+
+template <class X, bool BRANCH> __global__ __launch_bounds__(64 * STRIP_WAVES) void k_edge_back_strip(EdgeBackArgs a)
+{
+    typedef typename X::T T;
+    __shared__ float part[STRIP_WAVES][STRIP];
+    const int lane = lane_id(), wave = wave_id();
+    const int64_t col64 = (int64_t)blockIdx.x * STRIP + 8 * lane;
+    const int col = (int)min(col64, (int64_t)a.n), left = a.n - col, block = (int)blockIdx.y;
+    uint64_t seed, offset;
+    rng_of(a.drop, seed, offset);
+    const int r1 = first_row(a.rows, a.blocks, block + 1);
+    float sum[SUMS][8] = {};
+    const typename X::V8 wa = get_vector<X>(left > 0 ? a.after.w : nullptr, col, left, 1.f);
+    const typename X::V8 ba = get_vector<X>(left > 0 ? a.after.b : nullptr, col, left, 0.f);
+    for (int row = first_row(a.rows, a.blocks, block) + wave; row < r1 && left > 0; row += STRIP_WAVES) {
+        BackStat b{}, f{};
+        if (a.stat) b = a.stat[2 * (int64_t)row], f = a.stat[2 * (int64_t)row + 1];
+        BackChunk<X, BRANCH> k;
+        back_before(a, row, col, left, b, true, k);
+        if (a.before.kind != DBS_NORM_NONE)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sum[SUM_BEFORE_W][i] = __builtin_fmaf(k.dh[i], k.xb[i], sum[SUM_BEFORE_W][i]);
+                sum[SUM_BEFORE_B][i] += k.dh[i];
+            }
+        if (a.dres) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = k.d[i] * a.scale;
+            put_eight<X>((T *)a.dres + row * a.lddr + col, left, v);
+        }
+        if constexpr (BRANCH) {
+            back_after(a, row, col, left, seed, offset, f, k);
+            if (a.gate) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float u = a.after.kind != DBS_NORM_NONE ? __builtin_fmaf(k.ub[i], (float)wa[i], (float)ba[i]) : k.ub[i];
+                    v[i] = k.keep[i] != 0.f ? k.d[i] * u * k.keep[i] : 0.f;
+                    sum[SUM_GATE][i] += v[i];
+                }
+                if (a.dgate) put_eight<X>((T *)a.dgate + row * a.lddg + col, left, v);
+            }
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = k.du[i];
+                if (a.after.kind != DBS_NORM_NONE) {
+                    sum[SUM_AFTER_W][i] = __builtin_fmaf(v[i], k.ub[i], sum[SUM_AFTER_W][i]);
+                    sum[SUM_AFTER_B][i] += v[i];
+                    v[i] = f.dx(v[i] * (float)wa[i], k.ub[i]);
+                }
+            }
+            if (a.dbranch) put_eight<X>((T *)a.dbranch + row * a.lddb + col, left, v);
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < SUMS; ++q) {
+        if (a.at[q] < 0) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[wave][8 * lane + i] = sum[q][i];
+        __syncthreads();
+        for (int c = (int)threadIdx.x; c < STRIP; c += 64 * STRIP_WAVES) {
+            const int64_t at = (int64_t)blockIdx.x * STRIP + c;
+            if (at >= a.n) continue;
+            float s = part[0][c];
+#pragma unroll
+            for (int w = 1; w < STRIP_WAVES; ++w) s += part[w][c];
+            a.part[((int64_t)block * a.sums + a.at[q]) * a.n + at] = s;
+        }
+        __syncthreads();
+    }
+}
+
+// The workgroups' sums, in their order: a column a lane, the workgroups shared
+// out to the waves.
+constexpr int TOTAL_WAVES = 16;
+struct TotalArgs {
+    const float *part;
+    void *out[SUMS];
+    int32_t sums, blocks, n, first;
+};
+template <class X> __global__ __launch_bounds__(64 * TOTAL_WAVES) void k_edge_total(TotalArgs a)
+{
+    __shared__ float part[TOTAL_WAVES][64];
+    const int lane = lane_id(), wave = wave_id(), q = (int)blockIdx.y;
+    const int64_t c = ((int64_t)blockIdx.x + a.first) * 64 + lane;
+    float s = 0.f;
+    if (c < a.n)
+#pragma unroll 4
+        for (int i = wave; i < a.blocks; i += TOTAL_WAVES) s += a.part[((int64_t)i * a.sums + q) * a.n + c];
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || c >= a.n) return;
+#pragma unroll
+    for (int w = 1; w < TOTAL_WAVES; ++w) s += part[w][lane];
+    ((typename X::T *)a.out[q])[c] = (typename X::T)s;
+}
+
+// ---------------------------------------------------------------------------
+// dropout alone
+// ---------------------------------------------------------------------------
+constexpr int DROP_TPB = 256;
+
+// A thread takes chunks of eight columns, its next one a whole grid on.  Bound by
+// the bytes; 16 random bits an element keep the generator's products (two for each of
+// ten rounds) to two and a half an element, which the vector ALUs do beside them.
+template <class X>
+__global__ __launch_bounds__(DROP_TPB) void k_dropout(const typename X::T *x, int64_t ldx, int32_t rows, int32_t n, int32_t per,
+                                                      Drop d, typename X::T *y, int64_t ldy)
+{
+    uint64_t seed, offset;
+    rng_of(d, seed, offset);
+    const int64_t chunks = (int64_t)rows * per;
+    for (int64_t c = (int64_t)blockIdx.x * DROP_TPB + threadIdx.x; c < chunks; c += (int64_t)gridDim.x * DROP_TPB) {
+        const int64_t row = c / per;
+        const int col = 8 * (int)(c - row * per), left = n - col;
+        float v[8];
+        get_floats<X>(x + row * ldx + col, left, v);
+        if (d.threshold) drop_eight(d, seed, offset, c, v);
+        put_eight<X>(y + row * ldy + col, left, v);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+template <class X> static hipError_t edge_t(const EdgeArgs &a, int32_t cus, hipStream_t s)
+{
+    const dim3 grid((unsigned)std::min(a.rows, 2 * cus)), block(64 * LONG_WAVES);
+    if (a.branch) hipLaunchKernelGGL((k_edge_long<X, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_edge_long<X, false>), grid, block, 0, s, a);
+    return hipGetLastError();
+}
+hipError_t launch_edge(bool bf16, const EdgeArgs &a, int32_t cus, hipStream_t s)
+{
+    if (a.rows == 0 || a.n == 0) return hipSuccess;
+    return bf16 ? edge_t<Bf16>(a, cus, s) : edge_t<Fp16>(a, cus, s);
+}
+
+// Workgroups along the rows: enough to fill the device, none with less than a row
+// for each wave.
+static int32_t strip_blocks(int32_t rows, int32_t n, int32_t cus)
+{
+    const int64_t strips = ((int64_t)n + STRIP - 1) / STRIP, want = strips ? (4 * (int64_t)cus + strips - 1) / strips : 1;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ((int64_t)rows + STRIP_WAVES - 1) / STRIP_WAVES, 65535}));
+}
+static size_t part_bytes(int32_t rows, int32_t n, int sums, int32_t cus)
+{
+    return ((size_t)strip_blocks(rows, n, cus) * sums * n * 4 + 255) / 256 * 256;
+}
+size_t edge_back_work(int32_t rows, int32_t n, int sums, int32_t cus)
+{
+    if (n == 0) return 0;
+    return part_bytes(rows, n, sums, cus) + (size_t)rows * 2 * sizeof(BackStat);
+}
+
+template <class X> static hipError_t total_t(TotalArgs t, hipStream_t s)
+{
+    return launch_parts(((int64_t)t.n + 63) / 64, 64 * TOTAL_WAVES, [&](int32_t first, dim3 grid) {
+        t.first = first;
+        grid.y = (unsigned)t.sums;
+        hipLaunchKernelGGL(k_edge_total<X>, grid, dim3(64 * TOTAL_WAVES), 0, s, t);
+    });
+}
+template <class X, bool BRANCH> static hipError_t edge_back_t(const EdgeBackArgs &a, int32_t cus, hipStream_t s)
+{
+    if (a.rows > 0) {
+        if (a.stat) hipLaunchKernelGGL((k_edge_back_rows<X, BRANCH>), dim3((unsigned)std::min(a.rows, 2 * cus)), dim3(64 * LONG_WAVES), 0, s, a);
+        const dim3 grid((unsigned)(((int64_t)a.n + STRIP - 1) / STRIP), (unsigned)a.blocks);
+        hipLaunchKernelGGL((k_edge_back_strip<X, BRANCH>), grid, dim3(64 * STRIP_WAVES), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (!a.sums) return hipSuccess;
+    TotalArgs t{a.part, {}, a.sums, a.rows > 0 ? a.blocks : 0, a.n, 0};
+    for (int q = 0; q < SUMS; ++q)
+        if (a.at[q] >= 0) t.out[a.at[q]] = a.sum[q];
+    return total_t<X>(t, s);
+}
+hipError_t launch_column_total(bool bf16, const float *part, int32_t blocks, int32_t n, void *out, hipStream_t s)
+{
+    const TotalArgs t{part, {out}, 1, blocks, n, 0};
+    return bf16 ? total_t<Bf16>(t, s) : total_t<Fp16>(t, s);
+}
+hipError_t launch_edge_back(bool bf16, EdgeBackArgs a, bool has_branch, void *work, int32_t cus, hipStream_t s)
+{
+    if (a.n == 0) return hipSuccess;
+    a.sums = 0;
+    for (int q = 0; q < SUMS; ++q) a.at[q] = a.sum[q] ? a.sums++ : -1;
+    a.blocks = strip_blocks(a.rows, a.n, cus);
+    a.part = (float *)work;
+    const bool norms = a.before.kind != DBS_NORM_NONE || a.after.kind != DBS_NORM_NONE;
+    a.stat = norms && a.rows > 0 ? (BackStat *)((uint8_t *)work + part_bytes(a.rows, a.n, a.sums, cus)) : nullptr;
+    if (has_branch) return bf16 ? edge_back_t<Bf16, true>(a, cus, s) : edge_back_t<Fp16, true>(a, cus, s);
+    return bf16 ? edge_back_t<Bf16, false>(a, cus, s) : edge_back_t<Fp16, false>(a, cus, s);
+}
+
+hipError_t launch_dropout(bool bf16, const void *x, int64_t ldx, int32_t rows, int32_t n, const Drop &d, void *y, int64_t ldy,
+                          int32_t cus, hipStream_t s)
+{
+    if (rows == 0 || n == 0) return hipSuccess;
+    const int32_t per = (n + 7) / 8;
+    const int64_t chunks = (int64_t)rows * per;
+    const dim3 grid((unsigned)std::min<int64_t>((chunks + DROP_TPB - 1) / DROP_TPB, 16 * (int64_t)cus)), block(DROP_TPB);
+    if (bf16) hipLaunchKernelGGL(k_dropout<Bf16>, grid, block, 0, s, (const Bf16::T *)x, ldx, rows, n, per, d, (Bf16::T *)y, ldy);
+    else hipLaunchKernelGGL(k_dropout<Fp16>, grid, block, 0, s, (const Fp16::T *)x, ldx, rows, n, per, d, (Fp16::T *)y, ldy);
+    return hipGetLastError();
+}
+
+}  // namespace dbs
