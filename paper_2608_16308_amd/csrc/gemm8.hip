@@ -1,4 +1,7 @@
 // Products of matrices in blocks of 8-bit floating point on the matrix cores.
+#include <cstdlib>
+#include <utility>
+
 #include "float8.hpp"
 #include "layer_tile.hpp"
 
@@ -8,8 +11,8 @@ typedef int v8i_t __attribute__((ext_vector_type(8)));
 typedef int v4i_t __attribute__((ext_vector_type(4)));
 
 // A step is one block, E8_BLOCK elements of the sum: bytes of a row in LDS as
-// BK elements of 16 bits, so the tiles, their places and their epilogue are those
-// of the 16-bit products, with sizes along k counted in two elements.
+// BK elements of 16 bits, so the order of a tile in LDS, its place and its epilogue
+// are those of the 16-bit products.
 static_assert(E8_BLOCK == 2 * BK, "a step is a block");
 
 struct Gemm8Args {
@@ -17,146 +20,321 @@ struct Gemm8Args {
     const uint8_t *pe, *qe;   // exponents
     int64_t ldpe, ldqe;
     int32_t pshift;
+    int32_t steps;            // blocks along k; g.kn counts them in quads of four
+    int32_t force;
 };
 
 // One 16x16x128 step: the matrix cores multiply by 2^(sp - 127) and 2^(sq - 127),
-// the lowest byte of a lane being the scale of its row's block.
+// byte SP (SQ) of a lane being the scale of its row's block.
 //
 // They add eight neighbouring products in fixed point, cut to multiples of 2^(E -
 // 13) with 2^E <= the largest of the eight, and the sums of eight in 32 bits; all
 // their 8-bit products do.  That is the price of twice the rate of 16 bits: an
 // error that is small beside the rounding of the result (1531x7001->5003 in fp16:
 // 2.1e-4 from 64 bits in the norm, as the product in 32 bits is).
-__device__ __forceinline__ f4_t mma8(v8i_t p, v8i_t q, f4_t c, int sp, int sq)
+template <int SP, int SQ> __device__ __forceinline__ f4_t mma8(v8i_t p, v8i_t q, f4_t c, int sp, int sq)
 {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, c, 0, 0, 0, sp, 0, sq);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, c, 0, 0, SP, sp, SQ, sq);
 }
 
-template <class X, int NWQ, int NWP, int MT, int NS>
-__global__ __launch_bounds__(64 * NWQ * NWP, 2) void k_block8(Gemm8Args b)
+__device__ __forceinline__ uint32_t lds_at(void *p) { return (uint32_t)(uintptr_t)LDS_PTR(p); }
+// N bytes a lane from base + off straight into LDS, the lanes' behind each other
+// from `to` on.  Written as asm because the compiler, which sees such a load as a
+// write to all of LDS, waits for every one on its way before it reads anything
+// there; the kernel's own waits are counted instead.  (It returns no register, so
+// nothing can be taken for written too soon.  m0, the place, has no other use here.)
+template <int N> __device__ __forceinline__ void to_lds(const uint8_t *base, uint32_t off, uint32_t to)
 {
-    using C = Tile<X, G_LINEAR, NWQ, NWP, MT>;
+    if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base));
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(off), "s"(base));
+}
+
+// f(0), f(1) .. f(N - 1) with the number known to the compiler.
+template <class F, int... I> __device__ __forceinline__ void each_of(F &&f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F> __device__ __forceinline__ void each(F &&f) { each_of(f, std::make_integer_sequence<int, N>{}); }
+
+// Rounds and stores a wave's 16 MT x 64 sums, a lane's columns 16 in a row.
+template <class X, int MT>
+__device__ __forceinline__ void finish(const GemmArgs &a, const f4_t (&acc)[MT][4], int q0, int p0)
+{
+    typedef typename X::T T;
+    typedef typename X::V8 V8;
+    const int lane = lane_id(), col = p0 + 16 * (lane >> 4), left = a.pn - col;
+    if (left <= 0) return;
+    V8 bias[2] = {};
+    if (a.bias) {
+        const T *b = (const T *)a.bias + col;
+        if (left >= 16) bias[0] = load_eight<X>(b), bias[1] = load_eight<X>(b + 8);
+        else
+#pragma unroll
+            for (int i = 0; i < 16; ++i) bias[i >> 3][i & 7] = i < left ? b[i] : (T)0.f;
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int row = q0 + 16 * m + (lane & 15);
+        if (row >= a.qn) continue;
+        T *dst = (T *)a.y[0] + (int64_t)row * a.ldy[0] + col;
+        const T *res = a.res ? (const T *)a.res + (int64_t)row * a.ldr + col : nullptr;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            V8 o, add = {};
+            if (left >= 16) {
+                if (res) add = load_eight<X>(res + 8 * h);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = (T)(acc[m][2 * h + (i >> 2)][i & 3] + (float)bias[h][i] + (float)add[i]);
+                store_any(dst + 8 * h, o);
+            } else
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (8 * h + i < left)
+                        dst[8 * h + i] = (T)(acc[m][2 * h + (i >> 2)][i & 3] + (float)bias[h][i] + (res ? (float)res[8 * h + i] : 0.f));
+        }
+    }
+}
+
+// Sizes of a tile: four waves, each with 16 MT rows of q and 64 H of p; NS steps in
+// LDS; fragments of q are read PD rows of products ahead.
+template <int MT, int H, int NS> struct Tile8 {
+    static constexpr int NT = 256, TQ = 32 * MT, TP = 128 * H;
+    static constexpr int PB = TP * E8_BLOCK, QB = TQ * E8_BLOCK;
+    static constexpr int LP = PB / 16 / NT, LQ = QB / 16 / NT;  // chunks per thread and step
+    static constexpr int ROWS = TP + TQ, NW = (ROWS + NT - 1) / NT;  // rows with exponents; per thread
+    static constexpr int PD = MT >= 8 ? 3 : MT / 2, RING = MT >= 8 ? 4 : MT;
+    static constexpr int LDS = NS * (PB + QB) + 12 * ROWS;
+    static constexpr int PER_CU = 160 * 1024 / LDS;
+};
+
+// A tile of the product, chunks straight into LDS.  Four waves of up to 128x128
+// products each read half as much of LDS for a product as eight of 128x64 would,
+// which the 16-bit tiles can afford, and these not: their products take half the
+// time.  With one wave to a SIMD nothing else hides its waits, so the code does:
+// while a row of products (16 rows of q) runs, the fragments of a later one are
+// read, and from the row on at which all of this step's have been, those of the
+// next step, whose arrival all waves have waited for at the one barrier of a step.
+//
+// Exponents come four steps at a time (a quad), a word for each row, through
+// registers into an order in LDS that gives a lane all of a step's in one read.
+template <class X, int MT, int H, int NS>
+__global__ __launch_bounds__(256, (Tile8<MT, H, NS>::PER_CU)) void k_mul8(Gemm8Args b)
+{
+    using C = Tile8<MT, H, NS>;
     const GemmArgs &a = b.g;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[NS][C::PB + C::QB];
+    __shared__ __attribute__((aligned(16))) uint8_t exps[2][4][C::ROWS];
+    __shared__ uint32_t words[C::ROWS];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = wave_id();
-    const int wq = wave / NWP, wp = wave % NWP, r = lane & 15, g = lane >> 4;
+    const int wq = wave >> 1, wp = wave & 1, r = lane & 15, g = lane >> 4;
     const Unit u = unit_of<C::TQ, C::TP>(a);
-    const int q0 = u.q0, p0 = u.p0, s0 = u.s0, s1 = u.s1;
+    const int q0 = u.q0, p0 = u.p0, s0 = 4 * u.s0, s1 = min(4 * u.s1, b.steps);
 
-    // where a thread's chunks are, in bytes from the tile's first row
-    uint32_t vp[C::LP], vq[C::LQ];
-#pragma unroll
-    for (int i = 0; i < C::LP; ++i) {
-        const int c = i * C::NT + tid;
-        vp[i] = (uint32_t)min(c >> 3, a.pn - 1 - p0) * (uint32_t)a.ldp[0] + 16u * ((c & 7) ^ swz_p<G_LINEAR>(c >> 3));
-    }
-#pragma unroll
-    for (int i = 0; i < C::LQ; ++i) {
-        const int c = i * C::NT + tid;
-        vq[i] = (uint32_t)min(c >> 3, a.qn - 1 - q0) * (uint32_t)a.ldq[0] + 16u * ((c & 7) ^ swz_q(c >> 3));
-    }
+    // A thread's chunks are 32 rows apart; `v` is the place of one within its 32 rows.
+    // Of an operand's last tile the rows past the end are read as the last one (`end`),
+    // groups of 32 without any row as the last group.
+    const int row = tid >> 3;
+    const int rows_p = min(a.pn - p0, C::TP), rows_q = min(a.qn - q0, C::TQ);  // rows there
+    const uint32_t ldp = (uint32_t)a.ldp[0], ldq = (uint32_t)a.ldq[0];
+    const uint32_t vp = row * ldp + 16u * ((tid & 7) ^ swz_p<G_LINEAR>(row)), vq = row * ldq + 16u * ((tid & 7) ^ swz_q(row));
+    const uint32_t end_p = vp - (uint32_t)max(row - (rows_p - 1) % 32, 0) * ldp, end_q = vq - (uint32_t)max(row - (rows_q - 1) % 32, 0) * ldq;
     const uint8_t *bp = (const uint8_t *)a.p[0] + (int64_t)p0 * a.ldp[0], *bq = (const uint8_t *)a.q[0] + (int64_t)q0 * a.ldq[0];
-    auto fetch = [&](int step, int buf) {
-        uint8_t *lp = lds[buf] + wave * 1024, *lq = lp + C::PB;
-#pragma unroll
-        for (int i = 0; i < C::LP; ++i)
-            __builtin_amdgcn_global_load_lds(GLB_PTR(bp + (int64_t)step * E8_BLOCK + vp[i]), LDS_PTR(lp + i * C::NT * 16), 16, 0, 0);
-#pragma unroll
-        for (int i = 0; i < C::LQ; ++i)
-            __builtin_amdgcn_global_load_lds(GLB_PTR(bq + (int64_t)step * E8_BLOCK + vq[i]), LDS_PTR(lq + i * C::NT * 16), 16, 0, 0);
+    // chunk i of a thread, of step `step` (P's before Q's)
+    auto fetch = [&](int step, int buf, auto ic) {
+        constexpr int I = decltype(ic)::value;
+        const uint32_t to = lds_at(lds[buf]) + I * C::NT * 16 + wave * 1024;
+        constexpr int G = I < C::LP ? I : I - C::LP;
+        const int last = ((I < C::LP ? rows_p : rows_q) - 1) / 32, group = min(G, last);
+        if constexpr (I < C::LP) to_lds<16>(bp + (int64_t)step * E8_BLOCK + group * 32u * ldp, G < last ? vp : end_p, to);
+        else to_lds<16>(bq + (int64_t)step * E8_BLOCK + group * 32u * ldq, G < last ? vq : end_q, to);
     };
-    // exponents of the lane's rows, four steps a word
-    const uint8_t *ep[4], *eq[MT];
+    // the exponents of a thread's rows, and their place (worked out again each time:
+    // registers are short)
+    auto rows_of = [&](int i, auto &&of) {
+        int e = tid;
+        asm volatile("" : "+v"(e));
+        e += i * C::NT;
+        if ((i + 1) * C::NT > C::ROWS && i * C::NT + wave * 64 >= C::ROWS) return;
+        if (i * C::NT + wave * 64 < C::TP) {  // (the same for all lanes of a wave: tiles have whole waves of rows)
+            const int64_t first = (int64_t)(p0 >> b.pshift) * b.ldpe;
+            of(b.pe + first, (uint32_t)(((int64_t)min(p0 + e, a.pn - 1) >> b.pshift) * b.ldpe - first),
+               (e & -64 * H) + (((e >> 4) & 3) * 4 + (e & 3)) * 4 * H + (H > 1 ? (e >> 4) & 4 : 0) + ((e >> 2) & 3));
+        } else {
+            const int q = e - C::TP;
+            of(b.qe + q0 * b.ldqe, (uint32_t)(min(q, a.qn - 1 - q0) * b.ldqe),
+               C::TP + q / (16 * MT) * (16 * MT) + (q & 15) * MT + (q >> 4) % MT);
+        }
+    };
+    auto load_words = [&](int quad) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        ep[j] = b.pe + ((int64_t)min(p0 + 64 * wp + 16 * (r >> 2) + 4 * j + (r & 3), a.pn - 1) >> b.pshift) * b.ldpe;
+        for (int i = 0; i < C::NW; ++i)
+            rows_of(i, [&](const uint8_t *base, uint32_t off, int) { to_lds<4>(base + 4 * quad, off, lds_at(words) + 4 * (i * C::NT + wave * 64)); });
+    };
+    auto put_words = [&](int half) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m) eq[m] = b.qe + (int64_t)min(q0 + 16 * (MT * wq + m) + r, a.qn - 1) * b.ldqe;
-    uint32_t wpe[4], wqe[MT];
+        for (int i = 0; i < C::NW; ++i)
+            rows_of(i, [&](const uint8_t *, uint32_t, int at) {
+                const uint32_t w = words[i * C::NT + tid];
+#pragma unroll
+                for (int s = 0; s < 4; ++s) exps[half][s][at] = (uint8_t)(w >> (8 * s));
+            });
+    };
 
-    f4_t acc[MT][4];
+    f4_t acc[H][MT][4];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int h = 0; h < H; ++h)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[m][j] = f4_t{0.f, 0.f, 0.f, 0.f};
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[h][m][j] = f4_t{0.f, 0.f, 0.f, 0.f};
+
     // a lane's 32 elements of a row (in the same order for p and q; the sum does
     // not depend on it, since a block has one scale)
     auto fragment = [&](const uint8_t *tile, int row, int swz) {
-        const v4i_t lo = *(const v4i_t *)(tile + row * 128 + (g ^ swz) * 16), hi = *(const v4i_t *)(tile + row * 128 + ((4 + g) ^ swz) * 16);
+        const v4i_t lo = *(const v4i_t *)(tile + row * E8_BLOCK + (g ^ swz) * 16), hi = *(const v4i_t *)(tile + row * E8_BLOCK + ((4 + g) ^ swz) * 16);
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
+    v8i_t fp[2][4 * H], fq[C::RING];
+    int ep[2][H], eq[2][MT >= 8 ? 2 : 1];
+    auto read_p = [&](int buf, int set, int i) {
+        const int row = 64 * H * wp + 64 * (i >> 2) + 16 * (r >> 2) + 4 * (i & 3) + (r & 3);
+        fp[set][i] = fragment(lds[buf], row, swz_p<G_LINEAR>(row));
+    };
+    auto read_q = [&](int buf, int m) {
+        const int row = 16 * (MT * wq + m) + r;
+        fq[m % C::RING] = fragment(lds[buf] + C::PB, row, swz_q(row));
+    };
+    auto read_exps = [&](int half, int s, int set) {
+        const uint8_t *e = exps[half][s], *p = e + 64 * H * wp + 4 * H * r, *q = e + C::TP + 16 * MT * wq + MT * r;
+#pragma unroll
+        for (int h = 0; h < H; ++h) ep[set][h] = *(const int *)(p + 4 * h);
+        if constexpr (MT == 2) eq[set][0] = *(const uint16_t *)q;
+        else
+#pragma unroll
+            for (int i = 0; i < MT / 4; ++i) eq[set][i] = *(const int *)(q + 4 * i);
+    };
+    // At most `steps` steps of loads are still on their way, and every wave's part
+    // of the others has arrived.
     auto arrived = [&](auto steps) {
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(steps)::value * (C::LP + C::LQ)) : "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-        if (s0 + i < s1) fetch(s0 + i, i);
-    int buf = 0;
-    for (int t = s0; t < s1; ++t) {
-        if ((t & 3) == 0 || t == s0) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) wpe[j] = *(const uint32_t *)(ep[j] + (t & ~3));
-#pragma unroll
-            for (int m = 0; m < MT; ++m) wqe[m] = *(const uint32_t *)(eq[m] + (t & ~3));
+
+    if (s0 < s1) {
+        load_words(u.s0);
+        each<NS>([&](auto n) {
+            each<C::LP + C::LQ>([&](auto i) { fetch(min(s0 + decltype(n)::value, s1 - 1), decltype(n)::value, i); });
+        });
+        arrived(std::integral_constant<int, NS - 1>{});
+        put_words(0);
+        __syncthreads();
+        read_exps(0, 0, 0);
+        each<4 * H>([&](auto i) { read_p(0, 0, i); });
+        each<C::PD>([&](auto m) { read_q(0, m); });
+        int buf = 0;
+        for (int quad = u.s0; 4 * quad < s1; ++quad) {
+            const int half = (quad - u.s0) & 1;
+            each<4>([&](auto sc) {
+                constexpr int S = decltype(sc)::value, SET = S & 1;
+                const int t = 4 * quad + S;
+                if (t >= s1) return;
+                const int next = buf + 1 < NS ? buf + 1 : 0;
+                each<MT>([&](auto mc) {
+                    constexpr int M = decltype(mc)::value, FREE = MT - C::PD;  // the row at which all of a step has been read
+                    if constexpr (M == FREE) {
+                        // the next step has arrived, and every wave has read this one
+                        arrived(std::integral_constant<int, NS - 2>{});
+                        if (S == 2) put_words(half ^ 1);
+                        if (S == 0) load_words(min(quad + 1, u.s1 - 1));
+                        read_exps(S == 3 ? half ^ 1 : half, (S + 1) & 3, SET ^ 1);
+                    }
+                    if constexpr (M < FREE) read_q(buf, M + C::PD);
+                    else {
+                        // (behind the last step: the last one again, read and not used, so that
+                        // the waits count the same loads in every step)
+                        read_q(next, M - FREE);
+                        constexpr int FROM = (M - FREE) * 4 * H / C::PD, TO = (M - FREE + 1) * 4 * H / C::PD;
+                        each<TO - FROM>([&](auto i) { read_p(next, SET ^ 1, FROM + decltype(i)::value); });
+                        constexpr int LF = (M - FREE) * (C::LP + C::LQ) / C::PD, LT = (M - FREE + 1) * (C::LP + C::LQ) / C::PD;
+                        each<LT - LF>([&](auto i) { fetch(min(t + NS, s1 - 1), buf, std::integral_constant<int, LF + decltype(i)::value>{}); });
+                    }
+                    each<H>([&](auto hc) {
+                        constexpr int HH = decltype(hc)::value;
+                        each<4>([&](auto jc) {
+                            constexpr int J = decltype(jc)::value;
+                            acc[HH][M][J] = mma8<J, (M & 3)>(fp[SET][4 * HH + J], fq[M % C::RING], acc[HH][M][J], ep[SET][HH], eq[SET][M >> 2]);
+                        });
+                    });
+                });
+                buf = next;
+            });
         }
-        // every wave's part of this step has arrived
-        if (NS > 1 && t + NS <= s1) arrived(std::integral_constant<int, NS - 1>{});
-        else arrived(std::integral_constant<int, 0>{});
-        const uint8_t *lp = lds[buf], *lq = lds[buf] + C::PB;
-        const int sh = 8 * (t & 3);
-        v8i_t fp[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int row = 64 * wp + 16 * (r >> 2) + 4 * j + (r & 3);
-            fp[j] = fragment(lp, row, swz_p<G_LINEAR>(row));
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int row = 16 * (MT * wq + m) + r;
-            const v8i_t fq = fragment(lq, row, swz_q(row));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[m][j] = mma8(fp[j], fq, acc[m][j], (int)(wpe[j] >> sh), (int)(wqe[m] >> sh));
-        }
-        // every wave has read it
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (t + NS < s1) fetch(t + NS, buf);
-        buf = buf + 1 < NS ? buf + 1 : 0;
+        arrived(std::integral_constant<int, 0>{});
     }
-    if (u.tile >= 0) leave_part<C::NT, MT>(a, u, acc);
-    else epilogue<X, G_LINEAR, MT>(a, acc, q0 + 16 * MT * wq, p0 + 64 * wp, 0);
+    if (u.tile >= 0) {
+        // (in the order in which k_join has a tile of 2 x 2 H waves)
+        constexpr int NV = 256 * H;
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            f4_t *own = (f4_t *)a.part + (int64_t)(u.tile * a.splits + u.part) * MT * 4 * NV + (2 * H * wq + H * wp + h) * 64 + lane;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) own[(m * 4 + j) * NV] = acc[h][m][j];
+        }
+    } else
+        each<H>([&](auto h) { finish<X, MT>(a, acc[decltype(h)::value], q0 + 16 * MT * wq, p0 + 64 * (H * wp + decltype(h)::value)); });
 }
 
-template <class X, int NWQ, int NWP, int MT, int NS>
-static hipError_t launch_block8(const LayerWork &w, Gemm8Args b, hipStream_t s)
+// The tiles of a call, how many of them are taken whole and in how many parts the
+// others; the quads that a compute unit does in sequence, joining included.
+constexpr double JOIN_QUADS = 0.5;
+template <class C> static bool lay_out8(const LayerWork &w, GemmArgs &a, double *quads)
 {
-    using C = Tile<X, G_LINEAR, NWQ, NWP, MT>;
-    double steps;
-    if (!lay_out<C, G_LINEAR>(w, b.g, C::per_cu(NS), &steps)) return hipErrorInvalidConfiguration;
+    const int64_t tq = ((int64_t)a.qn + C::TQ - 1) / C::TQ, tp = ((int64_t)a.pn + C::TP - 1) / C::TP, ntile = tq * tp;
+    if (ntile > MAX_TILES) return false;
+    a.tq = (int32_t)tq, a.tp = (int32_t)tp;
+    const int64_t slots = (int64_t)w.cus * C::PER_CU, steps = a.kn / BK, rest = ntile % slots;
+    a.full = (int32_t)(ntile - rest), a.splits = 1;
+    *quads = (double)(ntile / slots) * (double)steps;
+    if (rest == 0) return true;
+    double best = (double)steps;
+    for (int64_t s = 2; s <= 16 && s <= steps && rest * s * C::TP * C::TQ * 4 <= (int64_t)w.part_bytes; ++s) {
+        const double cost = (double)((rest * s + slots - 1) / slots) * (double)((steps + s - 1) / s) + JOIN_QUADS * (1.0 + s);
+        if (cost < best) best = cost, a.splits = (int32_t)s;
+    }
+    *quads += best;
+    return true;
+}
+
+template <class X, int MT, int H, int NS> static hipError_t launch_tile8(const LayerWork &w, Gemm8Args b, hipStream_t s)
+{
+    using C = Tile8<MT, H, NS>;
+    double quads;
+    if (!lay_out8<C>(w, b.g, &quads)) return hipErrorInvalidConfiguration;
     const int ntile = b.g.tp * b.g.tq;
-    if (ntile == 0) return hipSuccess;
     const hipError_t e = launch_parts(b.g.full + (int64_t)(ntile - b.g.full) * b.g.splits, C::NT, [&](int32_t first, dim3 grid) {
         b.g.first = first;
-        hipLaunchKernelGGL((k_block8<X, NWQ, NWP, MT, NS>), grid, dim3(C::NT), 0, s, b);
+        hipLaunchKernelGGL((k_mul8<X, MT, H, NS>), grid, dim3(C::NT), 0, s, b);
     });
     if (e != hipSuccess) return e;
     if (b.g.splits > 1)
-        hipLaunchKernelGGL((k_join<X, G_LINEAR, NWQ, NWP, MT>), dim3((unsigned)((ntile - b.g.full) * MT)), dim3(C::NT), 0, s, b.g);
+        hipLaunchKernelGGL((k_join<X, G_LINEAR, 2, 2 * H, MT>), dim3((unsigned)((ntile - b.g.full) * MT)), dim3(256 * H), 0, s, b.g);
     return hipGetLastError();
 }
 
-// Which tile: as for the 16-bit products, by the steps that a compute unit does in
-// sequence and what one costs.
+// Which tile: by the quads that a compute unit does in sequence and what one costs.
 template <class X> static hipError_t mul8_t(const LayerWork &w, const Gemm8Args &b, hipStream_t s)
 {
     GemmArgs g = b.g;
     double cost[3] = {1e30, 1e30, 1e30};
-    if (lay_out<Tile<X, G_LINEAR, 2, 4, 8>, G_LINEAR>(w, g, 1, &cost[0])) cost[0] *= 1.75;
-    if (lay_out<Tile<X, G_LINEAR, 4, 2, 2>, G_LINEAR>(w, g, 1, &cost[1])) cost[1] *= 0.66;
-    if (lay_out<Tile<X, G_LINEAR, 2, 2, 2>, G_LINEAR>(w, g, 2, &cost[2])) cost[2] *= 0.76;
-    if (cost[0] <= cost[1] && cost[0] <= cost[2]) return launch_block8<X, 2, 4, 8, 2>(w, b, s);
-    if (cost[1] <= cost[2]) return launch_block8<X, 4, 2, 2, 4>(w, b, s);
-    return launch_block8<X, 2, 2, 2, 3>(w, b, s);
+    if (lay_out8<Tile8<8, 2, 2>>(w, g, &cost[0])) cost[0] *= 1.75;
+    if (lay_out8<Tile8<4, 1, 4>>(w, g, &cost[1])) cost[1] *= 0.66;
+    if (lay_out8<Tile8<2, 1, 3>>(w, g, &cost[2])) cost[2] *= 0.76;
+    if (b.force >= 0) for (int i = 0; i < 3; ++i) cost[i] = i == b.force ? 0 : 1e30;
+    if (cost[0] <= cost[1] && cost[0] <= cost[2]) return launch_tile8<X, 8, 2, 2>(w, b, s);
+    if (cost[1] <= cost[2]) return launch_tile8<X, 4, 1, 4>(w, b, s);
+    return launch_tile8<X, 2, 1, 3>(w, b, s);
 }
 
 hipError_t launch_mul8(const LayerWork &w, bool bf16, const Mul8Args &m, hipStream_t s)
@@ -164,9 +342,11 @@ hipError_t launch_mul8(const LayerWork &w, bool bf16, const Mul8Args &m, hipStre
     if (m.pn == 0 || m.qn == 0) return hipSuccess;
     Gemm8Args b{};
     b.g.p[0] = m.p.codes, b.g.ldp[0] = m.p.ld, b.g.q[0] = m.q.codes, b.g.ldq[0] = m.q.ld;
-    b.g.pn = m.pn, b.g.qn = m.qn, b.g.kn = (int32_t)(e8_blocks(m.kn) * BK), b.g.segs = 1, b.g.batch = 1;
+    b.g.pn = m.pn, b.g.qn = m.qn, b.g.kn = (int32_t)((e8_blocks(m.kn) + 3) / 4 * BK), b.g.segs = 1, b.g.batch = 1;
     b.g.y[0] = m.y, b.g.ldy[0] = m.ldy, b.g.bias = m.bias, b.g.res = m.res, b.g.ldr = m.ldr, b.g.act = Act::of(DBS_ACT_NONE);
     b.g.part = w.part;
+    b.steps = (int32_t)e8_blocks(m.kn);
+    b.force = getenv("T8") ? atoi(getenv("T8")) : -1;
     b.pe = m.p.exps, b.ldpe = m.p.lde, b.pshift = m.p.shift, b.qe = m.q.exps, b.ldqe = m.q.lde;
     return bf16 ? mul8_t<Bf16>(w, b, s) : mul8_t<Fp16>(w, b, s);
 }
