@@ -82,7 +82,7 @@ struct Pack8Args {
     float *sums;    // NULL, or [ceil(rows / E8_BLOCK)][cols]
     int32_t tiles_c, first;  // filled by the launcher
 };
-hipError_t launch_pack8(bool bf16, Pack8Args a, hipStream_t s);
+hipError_t launch_pack8(bool bf16, Pack8Args a, int32_t cus, hipStream_t s);
 hipError_t launch_unpack8(bool bf16, const Blocks &b, int32_t rows, int32_t cols, void *y, int64_t ldy, int32_t cus, hipStream_t s);
 // The transpose of a matrix in tile blocks.
 hipError_t launch_turn8(const Blocks &b, int32_t rows, int32_t cols, const Blocks &to, hipStream_t s);

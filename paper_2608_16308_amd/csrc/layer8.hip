@@ -62,7 +62,7 @@ dbs_status dbs_pack8(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t cols, con
     Pack8Args a{};
     a.x = d_x, a.ldx = ldx, a.rows = rows, a.cols = cols, a.tile = tile != 0;
     (across ? a.turned : a.to) = blocks_of(out, across ? rows : cols, tile != 0);
-    LAYER_TRY(launch_pack8(dt == DBS_BF16, a, L->stream), fn);
+    LAYER_TRY(launch_pack8(dt == DBS_BF16, a, L->w.cus, L->stream), fn);
     return DBS_OK;
 }
 
@@ -107,7 +107,7 @@ dbs_status dbs_linear8(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_in, int3
         CHECK(check_room(fn, c.used, d_work, work_bytes));
         Pack8Args a{};
         a.x = d_x, a.ldx = ldx, a.rows = t, a.cols = n_in, a.to = m.q;
-        LAYER_TRY(launch_pack8(dt == DBS_BF16, a, L->stream), fn);
+        LAYER_TRY(launch_pack8(dt == DBS_BF16, a, L->w.cus, L->stream), fn);
     }
     m.p = blocks_of(w8, n_in, true);
     m.pn = n_out, m.qn = t, m.kn = n_in, m.bias = d_bias, m.res = d_res, m.ldr = ldr, m.y = d_y, m.ldy = ldy;
@@ -148,7 +148,7 @@ dbs_status dbs_linear8_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n
     // dy is read once for all that is made of it
     Pack8Args a{};
     a.x = d_dy, a.ldx = lddy, a.rows = t, a.cols = n_out, a.to = b.dy, a.turned = b.dyt, a.sums = b.sums;
-    if (a.to.codes || a.turned.codes || a.sums) LAYER_TRY(launch_pack8(bf, a, L->stream), fn);
+    if (a.to.codes || a.turned.codes || a.sums) LAYER_TRY(launch_pack8(bf, a, L->w.cus, L->stream), fn);
     if (d_db) LAYER_TRY(launch_column_total(bf, b.sums, (int32_t)e8_blocks(t), n_out, d_db, L->stream), fn);
     Mul8Args m{};
     if (d_dx) {
@@ -159,7 +159,7 @@ dbs_status dbs_linear8_backward(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n
     if (d_dw) {
         Pack8Args x{};
         x.x = d_x, x.ldx = ldx, x.from = blocks_of(x8, n_in, false), x.rows = t, x.cols = n_in, x.turned = b.xt;
-        LAYER_TRY(launch_pack8(bf, x, L->stream), fn);
+        LAYER_TRY(launch_pack8(bf, x, L->w.cus, L->stream), fn);
         m.p = b.xt, m.q = b.dyt, m.pn = n_in, m.qn = n_out, m.kn = t, m.y = d_dw, m.ldy = lddw;
         LAYER_TRY(launch_mul8(L->w, bf, m, L->stream), fn);
     }

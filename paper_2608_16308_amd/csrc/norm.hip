@@ -1,6 +1,7 @@
 // Norms before and after a block, the join with the residual stream, dropout,
 // and their gradients.
 #include <algorithm>
+#include <type_traits>
 
 #include "float8.hpp"
 #include "norm.hpp"
@@ -183,6 +184,219 @@ template <class X, bool BRANCH> __global__ __launch_bounds__(64 * LONG_WAVES) vo
     }
 }
 
+// ---------------------------------------------------------------------------
+// rows that a workgroup's registers hold
+// ---------------------------------------------------------------------------
+// The sum over a wave, in all its lanes.
+__device__ __forceinline__ float sum16(float v)
+{
+    auto ror = [](auto ctrl, float x) { return __builtin_bit_cast(float, dpp_mov<decltype(ctrl)::value>(0u, __builtin_bit_cast(uint32_t, x))); };
+    v += ror(std::integral_constant<int, dppc::ROW_ROR + 1>{}, v);
+    v += ror(std::integral_constant<int, dppc::ROW_ROR + 2>{}, v);
+    v += ror(std::integral_constant<int, dppc::ROW_ROR + 4>{}, v);
+    v += ror(std::integral_constant<int, dppc::ROW_ROR + 8>{}, v);
+    return v;
+}
+__device__ __forceinline__ float sum64(float v)
+{
+    v = sum16(v);
+    const auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    const uint32_t a0 = a[0], a1 = a[1];  // rows 0 0 2 2 and 1 1 3 3
+    v = __builtin_bit_cast(float, a0) + __builtin_bit_cast(float, a1);
+    const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    const uint32_t b0 = b[0], b1 = b[1];
+    return __builtin_bit_cast(float, b0) + __builtin_bit_cast(float, b1);
+}
+
+// A team: the waves that have a row, a workgroup or one of its waves.  Sums over
+// it, the same in all its lanes.
+constexpr int MAX_TEAM = 16;
+struct Team {
+    float (*red)[2][MAX_TEAM];  // [round][value][wave]
+    int waves, round;
+    template <int N> __device__ __forceinline__ void sum(float (&v)[N])
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = sum64(v[i]);
+        if (waves == 1) return;
+        const int lane = lane_id(), of = lane & 15;
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[round][i][wave_id()] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = sum16(of < waves ? red[round][i][of] : 0.f);
+        round ^= 1;  // (one barrier each: the other round's values have been read by all when it is passed)
+    }
+};
+
+// Statistics of one or two rows held eight columns a chunk, C chunks a lane.
+template <int C> struct Cols {
+    int col[C], left[C];  // of a lane's chunks; left <= 0: behind the row
+};
+template <int N, int C>
+__device__ __forceinline__ void team_stats(Team &team, const Cols<C> &k, float by, const NormOf *const (&nm)[N], const float *const (&x)[N],
+                                           Stat (&out)[N])
+{
+#pragma unroll
+    for (int q = 0; q < N; ++q) out[q] = Stat{1.f, 0.f, 0.f};
+    for (;;) {
+        bool layer = false;
+        float v[N];
+#pragma unroll
+        for (int q = 0; q < N; ++q) layer |= nm[q]->kind == DBS_NORM_LAYER;
+        if (layer) {
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                v[q] = 0.f;
+                if (nm[q]->kind == DBS_NORM_LAYER)
+#pragma unroll
+                    for (int i = 0; i < 8 * C; ++i) v[q] = __builtin_fmaf(x[q][i] * out[q].f, by, v[q]);
+            }
+            team.sum(v);
+#pragma unroll
+            for (int q = 0; q < N; ++q) out[q].mean = v[q];
+        }
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            v[q] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8 * C; ++i) {
+                float d = __builtin_fmaf(x[q][i], out[q].f, -out[q].mean);
+                if (layer && (i & 7) >= k.left[i >> 3]) d = 0.f;  // (without means, zeros stand behind the row)
+                v[q] = __builtin_fmaf(d, d, v[q]);
+            }
+        }
+        team.sum(v);
+        bool again = false;
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            const float var = v[q] * by;
+            if (var > 3.402823466e38f && out[q].f == 1.f && nm[q]->kind != DBS_NORM_NONE) out[q].f = DOWN, again = true;
+            out[q].rstd = 1.f / sqrtf(var + nm[q]->eps * out[q].f * out[q].f);
+        }
+        if (!again) return;  // (the same for the whole team)
+    }
+}
+
+// Which of a row's chunks a lane has, and which rows a team.
+template <int C> struct Share : Cols<C> {
+    int row, step;
+    __device__ __forceinline__ Share(int n, int waves)
+    {
+        const int at = waves == 1 ? lane_id() : (int)threadIdx.x, teams = waves == 1 ? (int)blockDim.x / 64 : 1;
+        row = (int)blockIdx.x * teams + (waves == 1 ? wave_id() : 0), step = (int)gridDim.x * teams;
+#pragma unroll
+        for (int i = 0; i < C; ++i) this->col[i] = 8 * (i * 64 * waves + at), this->left[i] = n - this->col[i];
+    }
+};
+template <class X, int C> struct Chunks {
+    typename X::V8 v[C];
+    __device__ __forceinline__ void load(const void *base, int64_t ld, int64_t row, const Cols<C> &k)
+    {
+#pragma unroll
+        for (int i = 0; i < C; ++i) v[i] = get_eight<X>((const typename X::T *)base + row * ld + k.col[i], k.left[i]);
+    }
+    __device__ __forceinline__ void vector(const void *p, const Cols<C> &k, float none)
+    {
+#pragma unroll
+        for (int i = 0; i < C; ++i) v[i] = get_vector<X>(k.left[i] > 0 ? p : nullptr, k.col[i], k.left[i], none);
+    }
+    __device__ __forceinline__ float operator[](int i) const { return (float)v[i >> 3][i & 7]; }
+};
+
+// Each team takes rows of up to 512 C columns a wave, the next one on its way while
+// one is worked on; the vectors stay in registers, or (C = 2, which needs those
+// for the rows) come from the caches each time.
+template <class X, bool BRANCH, int C> __global__ __launch_bounds__(64 * MAX_TEAM) void k_edge(EdgeArgs a, int waves)
+{
+    typedef typename X::T T;
+    __shared__ float red[2][2][MAX_TEAM];
+    Team team{red, waves, 0};
+    const Share<C> k(a.n, waves);
+    uint64_t seed, offset;
+    rng_of(a.drop, seed, offset);
+    const int64_t chunks = (a.n + 7) / 8;
+    const int last = (int)e8_blocks(a.n) * 16;
+    const float by = 1.f / (float)a.n;
+    const bool norm_a = BRANCH && a.after.kind != DBS_NORM_NONE, norm_b = a.before.kind != DBS_NORM_NONE;
+    Chunks<X, C> wa, ba, wb, bb, gate;
+    auto vectors = [&]() {
+        wb.vector(a.before.w, k, 1.f), bb.vector(a.before.b, k, 0.f);
+        if constexpr (BRANCH) {
+            wa.vector(a.after.w, k, 1.f), ba.vector(a.after.b, k, 0.f);
+            gate.vector(a.ldg == 0 ? a.gate : nullptr, k, 1.f);
+        }
+    };
+    if (C == 1) vectors();
+    const bool gates = BRANCH && a.gate && a.ldg != 0;
+    Chunks<X, C> res, branch, gnext;
+    auto load = [&](int row) {
+        res.load(a.res, a.ldr, row, k);
+        if constexpr (BRANCH) {
+            branch.load(a.branch, a.ldb, row, k);
+            if (gates) gnext.load(a.gate, a.ldg, row, k);
+        }
+    };
+    if (k.row < a.rows) load(k.row);
+    for (int row = k.row; row < a.rows; row += k.step) {
+        float s[8 * C], u[8 * C];
+#pragma unroll
+        for (int i = 0; i < 8 * C; ++i) {
+            s[i] = res[i];
+            if constexpr (BRANCH) u[i] = branch[i];
+        }
+        if (C > 1) vectors();
+        if (gates) gate = gnext;
+        if (row + k.step < a.rows) load(row + k.step);
+        if constexpr (BRANCH) {
+            if (norm_a) {
+                const NormOf *nm[1] = {&a.after};
+                const float *x[1] = {u};
+                Stat st[1];
+                team_stats(team, k, by, nm, x, st);
+#pragma unroll
+                for (int i = 0; i < 8 * C; ++i) u[i] = __builtin_fmaf(st[0].xh(u[i]), wa[i], ba[i]);
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                if (a.drop.threshold) {
+                    float v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = u[8 * c + i];
+                    drop_eight(a.drop, seed, offset, row * chunks + k.col[c] / 8, v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) u[8 * c + i] = v[i];
+                }
+                float out[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float t = __builtin_fmaf(gate[8 * c + i], u[8 * c + i], a.scale * s[8 * c + i]);
+                    s[8 * c + i] = i < k.left[c] ? t : 0.f;
+                    out[i] = t;
+                }
+                put_eight<X>((T *)a.stream + row * a.lds + k.col[c], k.left[c], out);
+            }
+        }
+        if (!norm_b) continue;
+        const NormOf *nm[1] = {&a.before};
+        const float *x[1] = {s};
+        Stat st[1];
+        team_stats(team, k, by, nm, x, st);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float h[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = __builtin_fmaf(st[0].xh(s[8 * c + i]), wb[8 * c + i], bb[8 * c + i]);
+            if (a.codes) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[i] = i < k.left[c] ? h[i] : 0.f;
+                put_codes<X>(a, row, k.col[c] / 8, last, h);
+            } else put_eight<X>((T *)a.h + row * a.ldh + k.col[c], k.left[c], h);
+        }
+    }
+}
+
 // One row's chunk of the backward pass: what it reads, and what follows from it.
 template <class X, bool BRANCH> struct BackChunk {
     float dh[8], xb[8], d[8], g[8];       // gradient of h, normalised stream, ds*, dh w
@@ -356,6 +570,145 @@ template <class X, bool BRANCH> __global__ __launch_bounds__(64 * STRIP_WAVES) v
     }
 }
 
+// The same for the gradients: a lane holds the sums over its team's rows of its
+// columns, the workgroups' are added afterwards.  Bound by the bytes and, where a
+// compute unit has one workgroup, by the four sums over a row one after the other.
+template <class X, bool BRANCH, int C, int TEAM> __global__ __launch_bounds__(64 * TEAM) void k_edge_back(EdgeBackArgs a, int waves)
+{
+    typedef typename X::T T;
+    __shared__ float red[2][2][MAX_TEAM];
+    Team team{red, waves, 0};
+    const Share<C> k(a.n, waves);
+    uint64_t seed, offset;
+    rng_of(a.drop, seed, offset);
+    const int64_t chunks = (a.n + 7) / 8;
+    const float by = 1.f / (float)a.n;
+    const bool norm_a = BRANCH && a.after.kind != DBS_NORM_NONE, norm_b = a.before.kind != DBS_NORM_NONE;
+    const bool gates = BRANCH && a.gate && a.ldg != 0, dgates = BRANCH && a.gate && (a.dgate || a.at[SUM_GATE] >= 0);
+    Chunks<X, C> wa, ba, wb, gate;
+    auto vectors = [&]() {
+        wb.vector(a.before.w, k, 1.f);
+        if constexpr (BRANCH) {
+            wa.vector(a.after.w, k, 1.f);
+            if (dgates) ba.vector(a.after.b, k, 0.f);
+            gate.vector(a.ldg == 0 ? a.gate : nullptr, k, 1.f);
+        }
+    };
+    if (C == 1) vectors();
+    float sum[BRANCH ? SUMS : 2][8 * C] = {};
+    for (int row = k.row; row < a.rows; row += k.step) {
+        Chunks<X, C> ds, dh, xs, xu;
+        if (C > 1) vectors();
+        if (a.ds) ds.load(a.ds, a.ldds, row, k);
+        if (norm_b) dh.load(a.dh, a.lddh, row, k), xs.load(a.stream, a.lds, row, k);
+        if constexpr (BRANCH) {
+            if (a.branch) xu.load(a.branch, a.ldb, row, k);
+            if (gates) gate.load(a.gate, a.ldg, row, k);
+        }
+        float d[8 * C], xb[8 * C], u[8 * C];
+        Stat sb{}, sa{};
+#pragma unroll
+        for (int i = 0; i < 8 * C; ++i) {
+            d[i] = a.ds ? ds[i] : 0.f;
+            if (norm_b) xb[i] = xs[i];
+            if (BRANCH && a.branch) u[i] = xu[i];
+        }
+        if (norm_a && norm_b) {
+            const NormOf *nm[2] = {&a.before, &a.after};
+            const float *x[2] = {xb, u};
+            Stat st[2];
+            team_stats(team, k, by, nm, x, st);
+            sb = st[0], sa = st[1];
+        } else if (norm_a || norm_b) {
+            const NormOf *nm[1] = {norm_b ? &a.before : &a.after};
+            const float *x[1] = {norm_b ? xb : u};
+            Stat st[1];
+            team_stats(team, k, by, nm, x, st);
+            if (norm_b) sb = st[0];
+            else sa = st[0];
+        }
+        if (norm_b) {
+            float m[2] = {0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 8 * C; ++i) {
+                xb[i] = sb.xh(xb[i]);
+                const float g = dh[i] * wb[i];
+                m[0] = __builtin_fmaf(g, xb[i], m[0]), m[1] += g;
+                sum[SUM_BEFORE_W][i] = __builtin_fmaf(dh[i], xb[i], sum[SUM_BEFORE_W][i]);
+                sum[SUM_BEFORE_B][i] += dh[i];
+            }
+            team.sum(m);
+            const BackStat b{sb, m[0] * by, a.before.kind == DBS_NORM_LAYER ? m[1] * by : 0.f};
+#pragma unroll
+            for (int i = 0; i < 8 * C; ++i) d[i] += b.dx(dh[i] * wb[i], xb[i]);
+        }
+        if (a.dres)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = d[8 * c + i] * a.scale;
+                put_eight<X>((T *)a.dres + row * a.lddr + k.col[c], k.left[c], v);
+            }
+        if constexpr (BRANCH) {
+            float m[2] = {0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float keep[8], v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) keep[i] = 1.f;
+                if (a.drop.threshold) drop_eight(a.drop, seed, offset, row * chunks + k.col[c] / 8, keep);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int q = 8 * c + i;
+                    if (norm_a) u[q] = sa.xh(u[q]);
+                    if (dgates) {
+                        const float y = norm_a ? __builtin_fmaf(u[q], wa[q], ba[q]) : u[q];
+                        v[i] = keep[i] != 0.f ? d[q] * y * keep[i] : 0.f;
+                        sum[SUM_GATE][q] += v[i];
+                    }
+                    d[q] = keep[i] != 0.f ? d[q] * gate[q] * keep[i] : 0.f;  // (behind dropout and gate)
+                    if (i >= k.left[c]) d[q] = 0.f;
+                    if (norm_a) {
+                        const float g = d[q] * wa[q];
+                        m[0] = __builtin_fmaf(g, u[q], m[0]), m[1] += g;
+                        sum[SUM_AFTER_W][q] = __builtin_fmaf(d[q], u[q], sum[SUM_AFTER_W][q]);
+                        sum[SUM_AFTER_B][q] += d[q];
+                    }
+                }
+                if (a.dgate && dgates) put_eight<X>((T *)a.dgate + row * a.lddg + k.col[c], k.left[c], v);
+            }
+            if (norm_a) {
+                team.sum(m);
+                const BackStat b{sa, m[0] * by, a.after.kind == DBS_NORM_LAYER ? m[1] * by : 0.f};
+#pragma unroll
+                for (int i = 0; i < 8 * C; ++i) d[i] = b.dx(d[i] * wa[i], u[i]);
+            }
+            if (a.dbranch)
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    float v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = d[8 * c + i];
+                    put_eight<X>((T *)a.dbranch + row * a.lddb + k.col[c], k.left[c], v);
+                }
+        }
+    }
+    // (a workgroup of several teams, which are waves, has a row of sums for each)
+    const int64_t block = waves == 1 ? (int64_t)blockIdx.x * (blockDim.x / 64) + wave_id() : (int64_t)blockIdx.x;
+#pragma unroll
+    for (int q = 0; q < (BRANCH ? SUMS : 2); ++q) {
+        if (a.at[q] < 0) continue;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float *to = a.part + (block * a.sums + a.at[q]) * a.n + k.col[c];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < k.left[c]) to[i] = sum[q][8 * c + i];
+        }
+    }
+}
+
 // The workgroups' sums, in their order: a column a lane, the workgroups shared
 // out to the waves.
 constexpr int TOTAL_WAVES = 16;
@@ -409,17 +762,33 @@ __global__ __launch_bounds__(DROP_TPB) void k_dropout(const typename X::T *x, in
 // ---------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------
-template <class X> static hipError_t edge_t(const EdgeArgs &a, int32_t cus, hipStream_t s)
+// A team's waves for rows of n columns, C chunks a lane; workgroups of one team, or of
+// four of a wave each.
+static int team_waves(int32_t n, int c) { return (int)(((int64_t)n + 512 * c - 1) / (512 * c)); }
+static int team_threads(int waves) { return 64 * (waves == 1 ? 4 : waves); }
+static int team_rows(int waves) { return waves == 1 ? 4 : 1; }
+
+template <class X, bool BRANCH, int C> static hipError_t edge_c(const EdgeArgs &a, int32_t cus, hipStream_t s)
 {
-    const dim3 grid((unsigned)std::min(a.rows, 2 * cus)), block(64 * LONG_WAVES);
-    if (a.branch) hipLaunchKernelGGL((k_edge_long<X, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_edge_long<X, false>), grid, block, 0, s, a);
+    const int waves = team_waves(a.n, C), rows = team_rows(waves);
+    // (as many as fit beside each other: 2048 threads a compute unit)
+    const int64_t most = (int64_t)cus * (2048 / team_threads(waves));
+    const dim3 grid((unsigned)std::min<int64_t>(((int64_t)a.rows + rows - 1) / rows, most));
+    hipLaunchKernelGGL((k_edge<X, BRANCH, C>), grid, dim3((unsigned)team_threads(waves)), 0, s, a, waves);
+    return hipGetLastError();
+}
+template <class X, bool BRANCH> static hipError_t edge_t(const EdgeArgs &a, int32_t cus, hipStream_t s)
+{
+    if (a.n <= 512 * MAX_TEAM) return edge_c<X, BRANCH, 1>(a, cus, s);
+    if (a.n <= 1024 * MAX_TEAM) return edge_c<X, BRANCH, 2>(a, cus, s);
+    hipLaunchKernelGGL((k_edge_long<X, BRANCH>), dim3((unsigned)std::min(a.rows, 2 * cus)), dim3(64 * LONG_WAVES), 0, s, a);
     return hipGetLastError();
 }
 hipError_t launch_edge(bool bf16, const EdgeArgs &a, int32_t cus, hipStream_t s)
 {
     if (a.rows == 0 || a.n == 0) return hipSuccess;
-    return bf16 ? edge_t<Bf16>(a, cus, s) : edge_t<Fp16>(a, cus, s);
+    if (a.branch) return bf16 ? edge_t<Bf16, true>(a, cus, s) : edge_t<Fp16, true>(a, cus, s);
+    return bf16 ? edge_t<Bf16, false>(a, cus, s) : edge_t<Fp16, false>(a, cus, s);
 }
 
 // Workgroups along the rows: enough to fill the device, none with less than a row
@@ -429,14 +798,29 @@ static int32_t strip_blocks(int32_t rows, int32_t n, int32_t cus)
     const int64_t strips = ((int64_t)n + STRIP - 1) / STRIP, want = strips ? (4 * (int64_t)cus + strips - 1) / strips : 1;
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ((int64_t)rows + STRIP_WAVES - 1) / STRIP_WAVES, 65535}));
 }
+// Whether the registers of a workgroup hold rows of n columns; chunks a lane (up to
+// eight waves have 256 registers each, which the sums of a join need) and teams: the
+// sums' bytes, written and read again, are to stay few beside the rows'.
+constexpr int BACK_TEAM = 8;
+static bool back_fits(int32_t n) { return n <= 1024 * BACK_TEAM; }
+static int back_chunks(int32_t n) { return n <= 512 * BACK_TEAM ? 1 : 2; }
+static int32_t back_groups(int32_t rows, int32_t n, int32_t cus)
+{
+    const int waves = team_waves(n, back_chunks(n)), each = team_rows(waves);
+    return (int32_t)std::min<int64_t>(((int64_t)rows + each - 1) / each, (int64_t)cus * std::max(1, 1024 / team_threads(waves)));
+}
+static int32_t sum_blocks(int32_t rows, int32_t n, int32_t cus)
+{
+    return back_fits(n) ? back_groups(rows, n, cus) * team_rows(team_waves(n, back_chunks(n))) : strip_blocks(rows, n, cus);
+}
 static size_t part_bytes(int32_t rows, int32_t n, int sums, int32_t cus)
 {
-    return ((size_t)strip_blocks(rows, n, cus) * sums * n * 4 + 255) / 256 * 256;
+    return ((size_t)sum_blocks(rows, n, cus) * sums * n * 4 + 255) / 256 * 256;
 }
 size_t edge_back_work(int32_t rows, int32_t n, int sums, int32_t cus)
 {
     if (n == 0) return 0;
-    return part_bytes(rows, n, sums, cus) + (size_t)rows * 2 * sizeof(BackStat);
+    return part_bytes(rows, n, sums, cus) + (back_fits(n) ? 0 : (size_t)rows * 2 * sizeof(BackStat));
 }
 
 template <class X> static hipError_t total_t(TotalArgs t, hipStream_t s)
@@ -449,7 +833,14 @@ template <class X> static hipError_t total_t(TotalArgs t, hipStream_t s)
 }
 template <class X, bool BRANCH> static hipError_t edge_back_t(const EdgeBackArgs &a, int32_t cus, hipStream_t s)
 {
-    if (a.rows > 0) {
+    if (a.rows > 0 && back_fits(a.n)) {
+        const int waves = team_waves(a.n, back_chunks(a.n));
+        const dim3 grid((unsigned)back_groups(a.rows, a.n, cus)), block((unsigned)team_threads(waves));
+        if (back_chunks(a.n) == 1) hipLaunchKernelGGL((k_edge_back<X, BRANCH, 1, BACK_TEAM>), grid, block, 0, s, a, waves);
+        else hipLaunchKernelGGL((k_edge_back<X, BRANCH, 2, BACK_TEAM>), grid, block, 0, s, a, waves);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    } else if (a.rows > 0) {
         if (a.stat) hipLaunchKernelGGL((k_edge_back_rows<X, BRANCH>), dim3((unsigned)std::min(a.rows, 2 * cus)), dim3(64 * LONG_WAVES), 0, s, a);
         const dim3 grid((unsigned)(((int64_t)a.n + STRIP - 1) / STRIP), (unsigned)a.blocks);
         hipLaunchKernelGGL((k_edge_back_strip<X, BRANCH>), grid, dim3(64 * STRIP_WAVES), 0, s, a);
@@ -472,10 +863,10 @@ hipError_t launch_edge_back(bool bf16, EdgeBackArgs a, bool has_branch, void *wo
     if (a.n == 0) return hipSuccess;
     a.sums = 0;
     for (int q = 0; q < SUMS; ++q) a.at[q] = a.sum[q] ? a.sums++ : -1;
-    a.blocks = strip_blocks(a.rows, a.n, cus);
+    a.blocks = sum_blocks(a.rows, a.n, cus);
     a.part = (float *)work;
     const bool norms = a.before.kind != DBS_NORM_NONE || a.after.kind != DBS_NORM_NONE;
-    a.stat = norms && a.rows > 0 ? (BackStat *)((uint8_t *)work + part_bytes(a.rows, a.n, a.sums, cus)) : nullptr;
+    a.stat = norms && a.rows > 0 && !back_fits(a.n) ? (BackStat *)((uint8_t *)work + part_bytes(a.rows, a.n, a.sums, cus)) : nullptr;
     if (has_branch) return bf16 ? edge_back_t<Bf16, true>(a, cus, s) : edge_back_t<Fp16, true>(a, cus, s);
     return bf16 ? edge_back_t<Bf16, false>(a, cus, s) : edge_back_t<Fp16, false>(a, cus, s);
 }

@@ -7,13 +7,83 @@
 namespace dbs {
 
 constexpr int P8_TPB = 256;
-constexpr int P8_LINE = E8_BLOCK + 16;  // bytes of a turned row in LDS
 
-__device__ __forceinline__ float max16(float v)
+// Magnitudes are compared as the integers that their 16 bits are, two to a word.
+typedef uint16_t h2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
 {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(h2_t, a), __builtin_bit_cast(h2_t, b)));
+}
+template <class X> struct Bits;  // of infinity
+template <> struct Bits<Bf16> {
+    static constexpr uint32_t INF = 0x7F80u;
+};
+template <> struct Bits<Fp16> {
+    static constexpr uint32_t INF = 0x7C00u;
+};
+// The larger of a word's halves, in both.
+__device__ __forceinline__ uint32_t both(uint32_t m) { return max2(m, m >> 16 | m << 16); }
+// The largest of 16 neighbouring lanes, by halves.
+__device__ __forceinline__ uint32_t max16(uint32_t m)
+{
+    m = max2(m, dpp_mov<dppc::ROW_ROR + 1>(0u, m));
+    m = max2(m, dpp_mov<dppc::ROW_ROR + 2>(0u, m));
+    m = max2(m, dpp_mov<dppc::ROW_ROR + 4>(0u, m));
+    return max2(m, dpp_mov<dppc::ROW_ROR + 8>(0u, m));
+}
+template <class X> __device__ __forceinline__ float value16(uint32_t bits)
+{
+    return (float)__builtin_bit_cast(typename X::T, (uint16_t)bits);
+}
+// A block's exponent from the bits of its largest magnitude.
+template <class X> __device__ __forceinline__ int exp_of(uint32_t bits) { return e8_exp(value16<X>(bits)); }
+// 2^-e (a normal number: -127 <= e <= 120)
+__device__ __forceinline__ float down(int e) { return __builtin_bit_cast(float, (uint32_t)(127 - e) << 23); }
+// Four values as codes.  A value that is not finite becomes NaN: in `odd` chunks,
+// which hold one, by a choice of its own.
+__device__ __forceinline__ float finite_or_nan(float v) { return __builtin_fabsf(v) <= 3.402823466e38f ? v : __builtin_nanf(""); }
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, bool odd)
+{
+    if (odd) a = finite_or_nan(a), b = finite_or_nan(b), c = finite_or_nan(c), d = finite_or_nan(d);
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    return (uint32_t)w;
+}
+// Eight 16-bit numbers; the words of their magnitudes, not finite ones as zeros.
+struct Raw8 {
+    uint32_t w[4];
+};
+template <class X> __device__ __forceinline__ bool magnitudes(const Raw8 &r, uint32_t (&m)[4])
+{
+    uint32_t all = 0;
 #pragma unroll
-    for (int o = 1; o < 16; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
+    for (int i = 0; i < 4; ++i) m[i] = r.w[i] & 0x7FFF7FFFu, all = max2(all, m[i]);
+    const bool odd = (both(all) & 0xFFFFu) >= Bits<X>::INF;
+    if (odd)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if ((m[i] & 0xFFFFu) >= Bits<X>::INF) m[i] &= 0xFFFF0000u;
+            if (m[i] >> 16 >= Bits<X>::INF) m[i] &= 0xFFFFu;
+        }
+    return odd;
+}
+template <class X> __device__ __forceinline__ Raw8 load_raw(const typename X::T *p, int left)
+{
+    if (left >= 8) return __builtin_bit_cast(Raw8, load_eight<X>(p));
+    typename X::V8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (typename X::T)0.f;
+    return __builtin_bit_cast(Raw8, v);
+}
+__device__ __forceinline__ uint32_t half_of(const Raw8 &r, int i) { return i & 1 ? r.w[i >> 1] >> 16 : r.w[i >> 1] & 0xFFFFu; }
+template <class X> __device__ __forceinline__ uint2 codes8(const Raw8 &r, float by, bool odd)
+{
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        w[h] = codes4(value16<X>(half_of(r, 4 * h)) * by, value16<X>(half_of(r, 4 * h + 1)) * by, value16<X>(half_of(r, 4 * h + 2)) * by,
+                      value16<X>(half_of(r, 4 * h + 3)) * by, odd);
+    return uint2{w[0], w[1]};
 }
 // Bytes behind the last block's exponent.
 __device__ __forceinline__ void pad_exps(const Blocks &b, int64_t row, int64_t blocks)
@@ -21,76 +91,129 @@ __device__ __forceinline__ void pad_exps(const Blocks &b, int64_t row, int64_t b
     for (int64_t i = blocks; i < b.lde; ++i) b.exps[row * b.lde + i] = E8_BIAS;
 }
 
-// A workgroup takes a tile of 128 x 128, a thread 8 rows of 8 columns of it: the
-// 16 lanes beside each other have a row's block, the 16 groups of them a column's.
-// Turned codes change places in LDS, so that both results are written in whole
-// lines of 128 bytes.  Bound by the bytes.
+// Row blocks alone: eight columns a lane, 16 lanes a block, P8_U chunks in flight.
+// Bound by the bytes.
+constexpr int P8_U = 4;
+template <class X> __global__ __launch_bounds__(P8_TPB) void k_pack8_rows(Pack8Args a)
+{
+    typedef typename X::T T;
+    const int per = (int)e8_blocks(a.cols) * 16;  // chunks of a row
+    const int64_t all = (int64_t)a.rows * per, stride = (int64_t)gridDim.x * P8_TPB;
+    for (int64_t c0 = (int64_t)blockIdx.x * P8_TPB + threadIdx.x; c0 < (all + 63) / 64 * 64; c0 += P8_U * stride) {
+        Raw8 r[P8_U];
+        int64_t row[P8_U];
+        int col[P8_U];
+#pragma unroll
+        for (int u = 0; u < P8_U; ++u) {
+            const int64_t c = c0 + u * stride;
+            // (32 bits are enough for the chunks of nearly all matrices, and divide much faster)
+            if (all <= UINT32_MAX) row[u] = (uint32_t)c / (uint32_t)per;
+            else row[u] = c / per;
+            col[u] = (int)(c - row[u] * per) * 8;
+            r[u] = Raw8{};
+            if (c < all && col[u] < a.cols) r[u] = load_raw<X>((const T *)a.x + row[u] * a.ldx + col[u], a.cols - col[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < P8_U; ++u) {
+            uint32_t m[4];
+            const bool odd = magnitudes<X>(r[u], m);
+            const uint32_t most = both(max16(max2(max2(m[0], m[1]), max2(m[2], m[3])))) & 0xFFFFu;
+            if (c0 + u * stride >= all) continue;
+            const int e = exp_of<X>(most), block = col[u] / E8_BLOCK;
+            *(uint2 *)(a.to.codes + row[u] * a.to.ld + col[u]) = codes8<X>(r[u], down(e), odd);
+            if (col[u] % E8_BLOCK == 0) {
+                a.to.exps[row[u] * a.to.lde + block] = (uint8_t)(e + E8_BIAS);
+                if (block + 1 == per / 16) pad_exps(a.to, row[u], per / 16);
+            }
+        }
+    }
+}
+
+// Turned lines of a tile: unit u (8 bytes) of line l stands at place u ^ (l >> 3), so
+// that the 16 lanes that write units of eight lines apart fall into different banks.
+__device__ __forceinline__ uint2 *unit_at(uint8_t *lines, int line, int u) { return (uint2 *)(lines + line * E8_BLOCK + 8 * (u ^ (line >> 3))); }
+
+// The turned lines of a tile to memory, 16 bytes a thread.
+__device__ __forceinline__ void put_lines(uint8_t *lines, const Blocks &to, int tr, int tc, int32_t cols)
+{
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = i * P8_TPB + (int)threadIdx.x, line = c >> 3, u = 2 * (c & 7);
+        const int64_t col = (int64_t)tc * E8_BLOCK + line;
+        const uint2 lo = *unit_at(lines, line, u), hi = *unit_at(lines, line, u + 1);
+        if (col < cols) *(uint4 *)(to.codes + col * to.ld + (int64_t)tr * E8_BLOCK + 8 * u) = uint4{lo.x, lo.y, hi.x, hi.y};
+    }
+}
+
+// Everything else.  A workgroup takes a tile of 128 x 128, a thread 8 rows of 8
+// columns of it: the 16 lanes beside each other have a row's block, the 16 groups of
+// them a column's.  Turned codes change places in LDS, so that both results are
+// written in whole lines of 128 bytes.  Bound by the bytes.
 template <class X, bool CODES> __global__ __launch_bounds__(P8_TPB) void k_pack8(Pack8Args a)
 {
     typedef typename X::T T;
-    __shared__ float most[4][E8_BLOCK], sums[4][E8_BLOCK];
-    __shared__ __attribute__((aligned(16))) uint8_t lines[E8_BLOCK * P8_LINE];
+    __shared__ uint32_t most[4][E8_BLOCK / 2];
+    __shared__ float sums[4][E8_BLOCK];
+    __shared__ __attribute__((aligned(16))) uint8_t lines[E8_BLOCK * E8_BLOCK];
     const int lane = lane_id(), wave = wave_id(), rg = (int)threadIdx.x >> 4, cc = (int)threadIdx.x & 15;
     const int64_t tile = (int64_t)blockIdx.x + a.first;
     const int tr = (int)(tile / a.tiles_c), tc = (int)(tile % a.tiles_c);
     const int row0 = tr * E8_BLOCK + 8 * rg, col0 = tc * E8_BLOCK + 8 * cc, left = a.cols - col0;
 
-    float v[8][8];
+    Raw8 v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int64_t row = row0 + i;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+        v[i] = Raw8{};
         if (row >= a.rows || left <= 0) continue;
         if constexpr (CODES) {
-            e8_values<X>(*(const uint2 *)(a.from.codes + row * a.from.ld + col0), (int)a.from.exps[row * a.from.lde + tc] - E8_BIAS, v[i]);
+            float f[8];
+            e8_values<X>(*(const uint2 *)(a.from.codes + row * a.from.ld + col0), (int)a.from.exps[row * a.from.lde + tc] - E8_BIAS, f);
+            typename X::V8 t;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = j < left ? (float)(T)v[i][j] : 0.f;
-        } else {
-            const T *p = (const T *)a.x + row * a.ldx + col0;
-            if (left >= 8) {
-                const typename X::V8 t = load_eight<X>(p);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] = (float)t[j];
-            } else
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < left) v[i][j] = (float)p[j];
-        }
+            for (int j = 0; j < 8; ++j) t[j] = j < left ? (T)f[j] : (T)0.f;
+            v[i] = __builtin_bit_cast(Raw8, t);
+        } else v[i] = load_raw<X>((const T *)a.x + row * a.ldx + col0, left);
     }
-    // largest magnitudes of the thread's rows and columns
-    float mr[8], mc[8];
+    // largest magnitudes: mr of the thread's rows, two to a word, mc of its columns
+    uint32_t mr[4] = {}, mc[4] = {};
+    bool odd = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mr[i] = mc[i] = 0.f;
+    for (int i = 0; i < 8; ++i) {
+        uint32_t m[4];
+        odd |= magnitudes<X>(v[i], m);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float m = ck_mag(v[i][j]);
-            mr[i] = fmaxf(mr[i], m), mc[j] = fmaxf(mc[j], m);
-        }
+        for (int k = 0; k < 4; ++k) mc[k] = max2(mc[k], m[k]);
+        const uint32_t r = both(max2(max2(m[0], m[1]), max2(m[2], m[3])));
+        mr[i >> 1] |= i & 1 ? r & 0xFFFF0000u : r & 0xFFFFu;
+    }
     if (a.tile || a.turned.codes || a.sums) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float m = mc[j], s = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s += v[i][j];
-            m = fmaxf(m, __shfl_xor(m, 16, 64)), s += __shfl_xor(s, 16, 64);
-            m = fmaxf(m, __shfl_xor(m, 32, 64)), s += __shfl_xor(s, 32, 64);
-            if (lane < 16) most[wave][8 * cc + j] = m, sums[wave][8 * cc + j] = s;
+        for (int k = 0; k < 4; ++k) {
+            mc[k] = max2(mc[k], (uint32_t)__shfl_xor((int)mc[k], 16, 64));
+            mc[k] = max2(mc[k], (uint32_t)__shfl_xor((int)mc[k], 32, 64));
+            if (lane < 16) most[wave][4 * cc + k] = mc[k];
         }
+        if (a.sums)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float s = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s += value16<X>(half_of(v[i], j));
+                s += __shfl_xor(s, 16, 64);
+                s += __shfl_xor(s, 32, 64);
+                if (lane < 16) sums[wave][8 * cc + j] = s;
+            }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            mc[j] = fmaxf(fmaxf(most[0][8 * cc + j], most[1][8 * cc + j]), fmaxf(most[2][8 * cc + j], most[3][8 * cc + j]));
+        for (int k = 0; k < 4; ++k)
+            mc[k] = max2(max2(most[0][4 * cc + k], most[1][4 * cc + k]), max2(most[2][4 * cc + k], most[3][4 * cc + k]));
     }
     if (a.tile) {
-        float m = mc[0];
+        const uint32_t m = both(max16(max2(max2(mc[0], mc[1]), max2(mc[2], mc[3]))));
 #pragma unroll
-        for (int j = 1; j < 8; ++j) m = fmaxf(m, mc[j]);
-        m = max16(m);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) mr[i] = mc[i] = m;
+        for (int k = 0; k < 4; ++k) mr[k] = mc[k] = m;
     }
     if (a.sums && threadIdx.x < E8_BLOCK) {
         const int c = (int)threadIdx.x, col = tc * E8_BLOCK + c;
@@ -98,11 +221,13 @@ template <class X, bool CODES> __global__ __launch_bounds__(P8_TPB) void k_pack8
     }
     if (a.to.codes) {
 #pragma unroll
+        for (int k = 0; k < 4; ++k) mr[k] = max16(mr[k]);
+#pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int64_t row = row0 + i;
-            const int e = e8_exp(a.tile ? mr[i] : max16(mr[i]));
+            const int e = exp_of<X>(i & 1 ? mr[i >> 1] >> 16 : mr[i >> 1] & 0xFFFFu);
             if (row >= a.rows) continue;
-            *(uint2 *)(a.to.codes + row * a.to.ld + col0) = e8_codes(v[i], e);
+            *(uint2 *)(a.to.codes + row * a.to.ld + col0) = codes8<X>(v[i], down(e), odd);
             if (cc == 0 && (!a.tile || (rg == 0 && i == 0))) {
                 const int64_t at = row >> a.to.shift;
                 a.to.exps[at * a.to.lde + tc] = (uint8_t)(e + E8_BIAS);
@@ -113,24 +238,17 @@ template <class X, bool CODES> __global__ __launch_bounds__(P8_TPB) void k_pack8
     if (a.turned.codes) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            float t[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = v[i][j];
-            const int e = e8_exp(mc[j]);
-            *(uint2 *)(lines + (8 * cc + j) * P8_LINE + 8 * rg) = e8_codes(t, e);
+            const int e = exp_of<X>(j & 1 ? mc[j >> 1] >> 16 : mc[j >> 1] & 0xFFFFu);
+            const float by = down(e);
+            auto at = [&](int i) { return value16<X>(half_of(v[i], j)) * by; };
+            *unit_at(lines, 8 * cc + j, rg) = uint2{codes4(at(0), at(1), at(2), at(3), odd), codes4(at(4), at(5), at(6), at(7), odd)};
             if (rg == 0 && j < left && (!a.tile || (cc == 0 && j == 0))) {
-                const int64_t at = (int64_t)(col0 + j) >> a.turned.shift, blocks = e8_blocks(a.rows);
-                a.turned.exps[at * a.turned.lde + tr] = (uint8_t)(e + E8_BIAS);
-                if (tr == blocks - 1) pad_exps(a.turned, at, blocks);
+                const int64_t col = (int64_t)(col0 + j) >> a.turned.shift, blocks = e8_blocks(a.rows);
+                a.turned.exps[col * a.turned.lde + tr] = (uint8_t)(e + E8_BIAS);
+                if (tr == blocks - 1) pad_exps(a.turned, col, blocks);
             }
         }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = i * P8_TPB + (int)threadIdx.x, line = c >> 3, at = 16 * (c & 7);
-            const int64_t col = (int64_t)tc * E8_BLOCK + line;
-            if (col < a.cols) *(uint4 *)(a.turned.codes + col * a.turned.ld + (int64_t)tr * E8_BLOCK + at) = *(const uint4 *)(lines + line * P8_LINE + at);
-        }
+        put_lines(lines, a.turned, tr, tc, a.cols);
     }
 }
 
@@ -156,30 +274,35 @@ __global__ __launch_bounds__(P8_TPB) void k_unpack8(Blocks b, int32_t rows, int3
     }
 }
 
-// A tile of codes a workgroup, turned in LDS; its exponent goes with it.
+// Four rows of four bytes turned.
+__device__ __forceinline__ void turn4(uint32_t (&w)[4])
+{
+    const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+    const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    w[0] = __builtin_amdgcn_perm(c, a, 0x05040100u), w[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    w[2] = __builtin_amdgcn_perm(d, b, 0x05040100u), w[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
+// A tile of codes a workgroup, turned eight by eight in registers and then, line by
+// line, in LDS; its exponent goes with it.
 __global__ __launch_bounds__(P8_TPB) void k_turn8(Blocks b, int32_t rows, int32_t cols, int32_t tiles_c, int32_t first, Blocks to)
 {
-    __shared__ __attribute__((aligned(16))) uint8_t lines[E8_BLOCK * P8_LINE];
+    __shared__ __attribute__((aligned(16))) uint8_t lines[E8_BLOCK * E8_BLOCK];
     const int64_t tile = (int64_t)blockIdx.x + first;
-    const int tr = (int)(tile / tiles_c), tc = (int)(tile % tiles_c);
+    const int tr = (int)(tile / tiles_c), tc = (int)(tile % tiles_c), rg = (int)threadIdx.x >> 4, cc = (int)threadIdx.x & 15;
+    uint32_t w[2][2][4];  // [upper four rows][left four columns][row]
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = i * P8_TPB + (int)threadIdx.x, line = c >> 3, at = 16 * (c & 7);
-        const int64_t row = (int64_t)tr * E8_BLOCK + line;
-        uint4 v = {0, 0, 0, 0};
-        if (row < rows) v = *(const uint4 *)(b.codes + row * b.ld + (int64_t)tc * E8_BLOCK + at);
-        *(uint4 *)(lines + line * P8_LINE + at) = v;
+    for (int i = 0; i < 8; ++i) {
+        const int64_t row = (int64_t)tr * E8_BLOCK + 8 * rg + i;
+        uint2 v = {0, 0};
+        if (row < rows) v = *(const uint2 *)(b.codes + row * b.ld + (int64_t)tc * E8_BLOCK + 8 * cc);
+        w[i >> 2][0][i & 3] = v.x, w[i >> 2][1][i & 3] = v.y;
     }
-    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = i * P8_TPB + (int)threadIdx.x, line = c >> 3, at = 16 * (c & 7);
-        uint32_t w[4] = {0, 0, 0, 0};
+    for (int i = 0; i < 4; ++i) turn4(w[i >> 1][i & 1]);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) w[k >> 2] |= (uint32_t)lines[(at + k) * P8_LINE + line] << (8 * (k & 3));
-        const int64_t col = (int64_t)tc * E8_BLOCK + line;
-        if (col < cols) *(uint4 *)(to.codes + col * to.ld + (int64_t)tr * E8_BLOCK + at) = uint4{w[0], w[1], w[2], w[3]};
-    }
+    for (int j = 0; j < 8; ++j) *unit_at(lines, 8 * cc + j, rg) = uint2{w[0][j >> 2][j & 3], w[1][j >> 2][j & 3]};
+    put_lines(lines, to, tr, tc, cols);
     if (threadIdx.x == 0) {
         to.exps[(int64_t)tc * to.lde + tr] = b.exps[(int64_t)tr * b.lde + tc];
         const int64_t blocks = e8_blocks(rows);
@@ -189,12 +312,19 @@ __global__ __launch_bounds__(P8_TPB) void k_turn8(Blocks b, int32_t rows, int32_
 
 constexpr int64_t MAX_TILES8 = 1 << 30;
 
-hipError_t launch_pack8(bool bf16, Pack8Args a, hipStream_t s)
+hipError_t launch_pack8(bool bf16, Pack8Args a, int32_t cus, hipStream_t s)
 {
     if (a.rows == 0 || a.cols == 0) return hipSuccess;
     const int64_t tiles = e8_blocks(a.rows) * e8_blocks(a.cols);
     if (tiles > MAX_TILES8) return hipErrorInvalidConfiguration;
     a.tiles_c = (int32_t)e8_blocks(a.cols);
+    if (a.to.codes && !a.tile && !a.turned.codes && !a.sums && !a.from.codes) {
+        const int64_t chunks = (int64_t)a.rows * a.tiles_c * 16;
+        const dim3 grid((unsigned)std::min<int64_t>((chunks + P8_TPB - 1) / P8_TPB, 8 * (int64_t)cus));
+        if (bf16) hipLaunchKernelGGL(k_pack8_rows<Bf16>, grid, dim3(P8_TPB), 0, s, a);
+        else hipLaunchKernelGGL(k_pack8_rows<Fp16>, grid, dim3(P8_TPB), 0, s, a);
+        return hipGetLastError();
+    }
     return launch_parts(tiles, P8_TPB, [&](int32_t first, dim3 grid) {
         a.first = first;
         if (a.from.codes) {
