@@ -27,7 +27,7 @@ CXX_FLAGS = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-pthread"]
 
 HIP_SOURCES = ["kernels.hip", "entries.hip", "bfs.hip", "decode.hip", "api.hip", "basic.hip", "convert.hip",
                "layer.hip", "layer_gemm.hip", "layer_rows.hip", "checkpoint.hip", "norm.hip", "edges.hip",
-               "pack8.hip", "gemm8.hip", "layer8.hip"]
+               "pack8.hip", "gemm8.hip", "rows8.hip", "layer8.hip"]
 CXX_SOURCES = ["builder.cpp"]
 
 

@@ -1,5 +1,6 @@
 // Blocks of 8-bit floating point: their codes, scales and places in memory.
 #pragma once
+#include "device_common.hpp"
 #include "layer.hpp"
 
 namespace dbs {
@@ -56,6 +57,83 @@ template <class X> __device__ __forceinline__ void e8_values(uint2 c, int e, flo
     }
 }
 
+// Magnitudes are compared as the integers that their 16 bits are, two to a word.
+typedef uint16_t h2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(h2_t, a), __builtin_bit_cast(h2_t, b)));
+}
+template <class X> struct Bits;  // of infinity
+template <> struct Bits<Bf16> {
+    static constexpr uint32_t INF = 0x7F80u;
+};
+template <> struct Bits<Fp16> {
+    static constexpr uint32_t INF = 0x7C00u;
+};
+// The larger of a word's halves, in both.
+__device__ __forceinline__ uint32_t both(uint32_t m) { return max2(m, m >> 16 | m << 16); }
+// The largest of 16 neighbouring lanes, by halves.
+__device__ __forceinline__ uint32_t max16(uint32_t m)
+{
+    m = max2(m, dpp_mov<dppc::ROW_ROR + 1>(0u, m));
+    m = max2(m, dpp_mov<dppc::ROW_ROR + 2>(0u, m));
+    m = max2(m, dpp_mov<dppc::ROW_ROR + 4>(0u, m));
+    return max2(m, dpp_mov<dppc::ROW_ROR + 8>(0u, m));
+}
+template <class X> __device__ __forceinline__ float value16(uint32_t bits)
+{
+    return (float)__builtin_bit_cast(typename X::T, (uint16_t)bits);
+}
+// A block's exponent from the bits of its largest magnitude.
+template <class X> __device__ __forceinline__ int exp_of(uint32_t bits) { return e8_exp(value16<X>(bits)); }
+// 2^-e (a normal number: -127 <= e <= 120)
+__device__ __forceinline__ float down(int e) { return __builtin_bit_cast(float, (uint32_t)(127 - e) << 23); }
+// Four values as codes.  A value that is not finite becomes NaN: in `odd` chunks,
+// which hold one, by a choice of its own.
+__device__ __forceinline__ float finite_or_nan(float v) { return __builtin_fabsf(v) <= 3.402823466e38f ? v : __builtin_nanf(""); }
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, bool odd)
+{
+    if (odd) a = finite_or_nan(a), b = finite_or_nan(b), c = finite_or_nan(c), d = finite_or_nan(d);
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    return (uint32_t)w;
+}
+// Eight 16-bit numbers; the words of their magnitudes, not finite ones as zeros.
+struct Raw8 {
+    uint32_t w[4];
+};
+template <class X> __device__ __forceinline__ bool magnitudes(const Raw8 &r, uint32_t (&m)[4])
+{
+    uint32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = r.w[i] & 0x7FFF7FFFu, all = max2(all, m[i]);
+    const bool odd = (both(all) & 0xFFFFu) >= Bits<X>::INF;
+    if (odd)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if ((m[i] & 0xFFFFu) >= Bits<X>::INF) m[i] &= 0xFFFF0000u;
+            if (m[i] >> 16 >= Bits<X>::INF) m[i] &= 0xFFFFu;
+        }
+    return odd;
+}
+template <class X> __device__ __forceinline__ Raw8 load_raw(const typename X::T *p, int left)
+{
+    if (left >= 8) return __builtin_bit_cast(Raw8, load_eight<X>(p));
+    typename X::V8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (typename X::T)0.f;
+    return __builtin_bit_cast(Raw8, v);
+}
+__device__ __forceinline__ uint32_t half_of(const Raw8 &r, int i) { return i & 1 ? r.w[i >> 1] >> 16 : r.w[i >> 1] & 0xFFFFu; }
+template <class X> __device__ __forceinline__ uint2 codes8(const Raw8 &r, float by, bool odd)
+{
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        w[h] = codes4(value16<X>(half_of(r, 4 * h)) * by, value16<X>(half_of(r, 4 * h + 1)) * by, value16<X>(half_of(r, 4 * h + 2)) * by,
+                      value16<X>(half_of(r, 4 * h + 3)) * by, odd);
+    return uint2{w[0], w[1]};
+}
 // Codes of a matrix: rows of whole blocks, zeros behind the last column.
 // Exponents + 127: for each row (or E8_BLOCK rows) one byte for each block, rows
 // of whole fours, 127 behind the last.
@@ -96,6 +174,11 @@ struct Mul8Args {
     void *y;
     int64_t ldy;
 };
+// The same for up to ROWS8_TOKENS rows of q, given in blocks or (x not NULL) as 16-bit
+// values, which the kernel brings into blocks itself where they fit its LDS.
+constexpr int ROWS8_TOKENS = 16;
+bool rows8_pack(int64_t tokens, int64_t cols);
+hipError_t launch_rows8(const LayerWork &w, bool bf16, const Mul8Args &m, const void *x, int64_t ldx, hipStream_t s);
 hipError_t launch_mul8(const LayerWork &w, bool bf16, const Mul8Args &m, hipStream_t s);
 
 }  // namespace dbs

@@ -1,5 +1,4 @@
 // Products of matrices in blocks of 8-bit floating point on the matrix cores.
-#include <cstdlib>
 #include <utility>
 
 #include "float8.hpp"
@@ -21,7 +20,6 @@ struct Gemm8Args {
     int64_t ldpe, ldqe;
     int32_t pshift;
     int32_t steps;            // blocks along k; g.kn counts them in quads of four
-    int32_t force;
 };
 
 // One 16x16x128 step: the matrix cores multiply by 2^(sp - 127) and 2^(sq - 127),
@@ -287,31 +285,31 @@ __global__ __launch_bounds__(256, (Tile8<MT, H, NS>::PER_CU)) void k_mul8(Gemm8A
 }
 
 // The tiles of a call, how many of them are taken whole and in how many parts the
-// others; the quads that a compute unit does in sequence, joining included.
-constexpr double JOIN_QUADS = 0.5;
-template <class C> static bool lay_out8(const LayerWork &w, GemmArgs &a, double *quads)
+// others; microseconds that this takes, a quad with all compute units at it taking
+// `quad`, and joining a launch and the bytes of the parts written and read.
+template <class C> static double lay_out8(const LayerWork &w, GemmArgs &a, double quad)
 {
     const int64_t tq = ((int64_t)a.qn + C::TQ - 1) / C::TQ, tp = ((int64_t)a.pn + C::TP - 1) / C::TP, ntile = tq * tp;
-    if (ntile > MAX_TILES) return false;
+    if (ntile > MAX_TILES) return 1e30;
     a.tq = (int32_t)tq, a.tp = (int32_t)tp;
-    const int64_t slots = (int64_t)w.cus * C::PER_CU, steps = a.kn / BK, rest = ntile % slots;
+    const int64_t slots = (int64_t)w.cus * C::PER_CU, quads = a.kn / BK, rest = ntile % slots;
     a.full = (int32_t)(ntile - rest), a.splits = 1;
-    *quads = (double)(ntile / slots) * (double)steps;
-    if (rest == 0) return true;
-    double best = (double)steps;
-    for (int64_t s = 2; s <= 16 && s <= steps && rest * s * C::TP * C::TQ * 4 <= (int64_t)w.part_bytes; ++s) {
-        const double cost = (double)((rest * s + slots - 1) / slots) * (double)((steps + s - 1) / s) + JOIN_QUADS * (1.0 + s);
+    const double whole = (double)(ntile / slots) * (double)quads * quad;
+    if (rest == 0) return whole;
+    double best = (double)quads * quad;
+    for (int64_t s = 2; s <= 16 && s <= quads; ++s) {
+        const int64_t bytes = rest * s * C::TP * C::TQ * 4;
+        if (bytes > (int64_t)w.part_bytes) break;
+        const double cost = (double)((rest * s + slots - 1) / slots) * (double)((quads + s - 1) / s) * quad + 4 + (double)bytes * 0.45e-6;
         if (cost < best) best = cost, a.splits = (int32_t)s;
     }
-    *quads += best;
-    return true;
+    return whole + best;
 }
 
-template <class X, int MT, int H, int NS> static hipError_t launch_tile8(const LayerWork &w, Gemm8Args b, hipStream_t s)
+template <class X, int MT, int H, int NS> static hipError_t launch_tile8(const LayerWork &w, Gemm8Args b, double quad, hipStream_t s)
 {
     using C = Tile8<MT, H, NS>;
-    double quads;
-    if (!lay_out8<C>(w, b.g, &quads)) return hipErrorInvalidConfiguration;
+    if (lay_out8<C>(w, b.g, quad) >= 1e30) return hipErrorInvalidConfiguration;
     const int ntile = b.g.tp * b.g.tq;
     const hipError_t e = launch_parts(b.g.full + (int64_t)(ntile - b.g.full) * b.g.splits, C::NT, [&](int32_t first, dim3 grid) {
         b.g.first = first;
@@ -323,18 +321,25 @@ template <class X, int MT, int H, int NS> static hipError_t launch_tile8(const L
     return hipGetLastError();
 }
 
-// Which tile: by the quads that a compute unit does in sequence and what one costs.
+// Which tile: the one with the least time by the rule above.
 template <class X> static hipError_t mul8_t(const LayerWork &w, const Gemm8Args &b, hipStream_t s)
 {
+    constexpr double QUAD[4] = {7.0, 2.25, 2.53, 3.8};
     GemmArgs g = b.g;
-    double cost[3] = {1e30, 1e30, 1e30};
-    if (lay_out8<Tile8<8, 2, 2>>(w, g, &cost[0])) cost[0] *= 1.75;
-    if (lay_out8<Tile8<4, 1, 4>>(w, g, &cost[1])) cost[1] *= 0.66;
-    if (lay_out8<Tile8<2, 1, 3>>(w, g, &cost[2])) cost[2] *= 0.76;
-    if (b.force >= 0) for (int i = 0; i < 3; ++i) cost[i] = i == b.force ? 0 : 1e30;
-    if (cost[0] <= cost[1] && cost[0] <= cost[2]) return launch_tile8<X, 8, 2, 2>(w, b, s);
-    if (cost[1] <= cost[2]) return launch_tile8<X, 4, 1, 4>(w, b, s);
-    return launch_tile8<X, 2, 1, 3>(w, b, s);
+    double cost[4];
+    cost[0] = lay_out8<Tile8<8, 2, 2>>(w, g, QUAD[0]);
+    cost[1] = lay_out8<Tile8<4, 1, 4>>(w, g, QUAD[1]);
+    cost[2] = lay_out8<Tile8<2, 1, 3>>(w, g, QUAD[2]);
+    cost[3] = lay_out8<Tile8<4, 2, 3>>(w, g, QUAD[3]);
+    int tile = 0;
+    for (int i = 1; i < 4; ++i)
+        if (cost[i] < cost[tile]) tile = i;
+    switch (tile) {
+    case 0: return launch_tile8<X, 8, 2, 2>(w, b, QUAD[0], s);
+    case 1: return launch_tile8<X, 4, 1, 4>(w, b, QUAD[1], s);
+    case 2: return launch_tile8<X, 2, 1, 3>(w, b, QUAD[2], s);
+    default: return launch_tile8<X, 4, 2, 3>(w, b, QUAD[3], s);
+    }
 }
 
 hipError_t launch_mul8(const LayerWork &w, bool bf16, const Mul8Args &m, hipStream_t s)
@@ -346,7 +351,6 @@ hipError_t launch_mul8(const LayerWork &w, bool bf16, const Mul8Args &m, hipStre
     b.g.y[0] = m.y, b.g.ldy[0] = m.ldy, b.g.bias = m.bias, b.g.res = m.res, b.g.ldr = m.ldr, b.g.act = Act::of(DBS_ACT_NONE);
     b.g.part = w.part;
     b.steps = (int32_t)e8_blocks(m.kn);
-    b.force = getenv("T8") ? atoi(getenv("T8")) : -1;
     b.pe = m.p.exps, b.ldpe = m.p.lde, b.pshift = m.p.shift, b.qe = m.q.exps, b.ldqe = m.q.lde;
     return bf16 ? mul8_t<Bf16>(w, b, s) : mul8_t<Fp16>(w, b, s);
 }

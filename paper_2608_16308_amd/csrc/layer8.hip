@@ -81,7 +81,7 @@ dbs_status dbs_linear8_work(const dbs_layer *L, int32_t t, int32_t n_in, int32_t
     CHECK(check_call("dbs_linear8_work", L, DBS_F16, t, n_in, n_out));
     if (!bytes) return dbs_fail(DBS_ERR_ARG, "dbs_linear8_work: bytes is NULL");
     Carve c{nullptr};
-    take_blocks(c, t, n_in, false);
+    if (!rows8_pack(t, n_in)) take_blocks(c, t, n_in, false);
     *bytes = c.used;
     return DBS_OK;
 }
@@ -101,7 +101,8 @@ dbs_status dbs_linear8(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_in, int3
     CHECK(check_operand(fn, "y", d_y, t, n_out, ldy));
     Mul8Args m{};
     m.q = blocks_of(x8, n_in, false);
-    if (!x8) {
+    const bool few = t <= ROWS8_TOKENS, pack = !x8 && few && rows8_pack(t, n_in);
+    if (!x8 && !pack) {
         Carve c{(uint8_t *)d_work};
         m.q = take_blocks(c, t, n_in, false);
         CHECK(check_room(fn, c.used, d_work, work_bytes));
@@ -111,7 +112,8 @@ dbs_status dbs_linear8(dbs_layer *L, dbs_dtype dt, int32_t t, int32_t n_in, int3
     }
     m.p = blocks_of(w8, n_in, true);
     m.pn = n_out, m.qn = t, m.kn = n_in, m.bias = d_bias, m.res = d_res, m.ldr = ldr, m.y = d_y, m.ldy = ldy;
-    LAYER_TRY(launch_mul8(L->w, dt == DBS_BF16, m, L->stream), fn);
+    if (few) LAYER_TRY(launch_rows8(L->w, dt == DBS_BF16, m, pack ? d_x : nullptr, ldx, L->stream), fn);
+    else LAYER_TRY(launch_mul8(L->w, dt == DBS_BF16, m, L->stream), fn);
     return DBS_OK;
 }
 

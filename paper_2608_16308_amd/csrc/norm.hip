@@ -8,25 +8,60 @@
 
 namespace dbs {
 
-// A store at any alignment of its elements.
+// Eight elements in words; `left` of them (1 to 7), at any alignment, as four, two
+// and one.
+struct Words {
+    uint32_t w[4];
+};
+struct __attribute__((packed, aligned(2))) Four {
+    uint32_t w[2];
+};
+struct __attribute__((packed, aligned(2))) Two {
+    uint32_t w;
+};
+__device__ __forceinline__ Words get_part(const void *p, int left)
+{
+    const uint16_t *at = (const uint16_t *)p;
+    Words r = {{0u, 0u, 0u, 0u}};
+    uint32_t lo = 0, hi = 0;  // what follows the four
+    if (left & 1) lo = at[left & 6];
+    if (left & 2) {
+        const uint32_t two = ((const Two *)(at + (left & 4)))->w;
+        hi = lo, lo = two;
+    }
+    if (left & 4) {
+        const Four four = *(const Four *)at;
+        r.w[0] = four.w[0], r.w[1] = four.w[1], r.w[2] = lo, r.w[3] = hi;
+    } else r.w[0] = lo, r.w[1] = hi;
+    return r;
+}
+__device__ __forceinline__ void put_part(void *p, int left, Words v)
+{
+    uint16_t *at = (uint16_t *)p;
+    if (left & 4) {
+        *(Four *)at = Four{{v.w[0], v.w[1]}};
+        v.w[0] = v.w[2], v.w[1] = v.w[3];
+    }
+    if (left & 2) {
+        ((Two *)(at + (left & 4)))->w = v.w[0];
+        v.w[0] = v.w[1];
+    }
+    if (left & 1) at[left & 6] = (uint16_t)v.w[0];
+}
 template <class X> __device__ __forceinline__ void put_eight(typename X::T *p, int left, const float (&v)[8])
 {
     typename X::V8 t;
 #pragma unroll
     for (int i = 0; i < 8; ++i) t[i] = (typename X::T)v[i];
     if (left >= 8) ((Eight<X> *)p)->v = t;
-    else
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < left) p[i] = t[i];
+    else if (left > 0) put_part(p, left, __builtin_bit_cast(Words, t));
 }
 // Eight elements of a row of which `left` are there; the rest reads as zeros.
 template <class X> __device__ __forceinline__ typename X::V8 get_eight(const typename X::T *p, int left)
 {
-    if (left >= 8) return load_eight<X>(p);
-    typename X::V8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (typename X::T)0.f;
+    typename X::V8 v = {};
+    if (left >= 8) v = load_eight<X>(p);
+    else if (left > 0) v = __builtin_bit_cast(typename X::V8, get_part(p, left));
     return v;
 }
 template <class X> __device__ __forceinline__ void get_floats(const typename X::T *p, int left, float (&v)[8])
@@ -233,50 +268,70 @@ struct Team {
 // Statistics of one or two rows held eight columns a chunk, C chunks a lane.
 template <int C> struct Cols {
     int col[C], left[C];  // of a lane's chunks; left <= 0: behind the row
+    bool full;            // all chunks of the wave have eight columns
 };
 template <int N, int C>
 __device__ __forceinline__ void team_stats(Team &team, const Cols<C> &k, float by, const NormOf *const (&nm)[N], const float *const (&x)[N],
                                            Stat (&out)[N])
 {
+    bool layer = false;
+    float v[N];
 #pragma unroll
-    for (int q = 0; q < N; ++q) out[q] = Stat{1.f, 0.f, 0.f};
-    for (;;) {
-        bool layer = false;
-        float v[N];
+    for (int q = 0; q < N; ++q) layer |= nm[q]->kind == DBS_NORM_LAYER, out[q] = Stat{1.f, 0.f, 0.f};
+    auto means = [&]() {
 #pragma unroll
-        for (int q = 0; q < N; ++q) layer |= nm[q]->kind == DBS_NORM_LAYER;
-        if (layer) {
+        for (int q = 0; q < N; ++q) {
+            v[q] = 0.f;
+            if (nm[q]->kind == DBS_NORM_LAYER)
 #pragma unroll
-            for (int q = 0; q < N; ++q) {
-                v[q] = 0.f;
-                if (nm[q]->kind == DBS_NORM_LAYER)
-#pragma unroll
-                    for (int i = 0; i < 8 * C; ++i) v[q] = __builtin_fmaf(x[q][i] * out[q].f, by, v[q]);
-            }
-            team.sum(v);
-#pragma unroll
-            for (int q = 0; q < N; ++q) out[q].mean = v[q];
+                for (int i = 0; i < 8 * C; ++i) v[q] = __builtin_fmaf(x[q][i], by * out[q].f, v[q]);
         }
+        team.sum(v);
+#pragma unroll
+        for (int q = 0; q < N; ++q) out[q].mean = v[q];
+    };
+    auto squares = [&](bool masked) {
 #pragma unroll
         for (int q = 0; q < N; ++q) {
             v[q] = 0.f;
 #pragma unroll
             for (int i = 0; i < 8 * C; ++i) {
                 float d = __builtin_fmaf(x[q][i], out[q].f, -out[q].mean);
-                if (layer && (i & 7) >= k.left[i >> 3]) d = 0.f;  // (without means, zeros stand behind the row)
+                if (masked && (i & 7) >= k.left[i >> 3]) d = 0.f;
                 v[q] = __builtin_fmaf(d, d, v[q]);
             }
         }
+    };
+    // (without means, zeros stand behind the row)
+    const bool masked = layer && !k.full;
+    for (;;) {
+        if (layer) means();
+        if (masked) squares(true);
+        else squares(false);
         team.sum(v);
         bool again = false;
 #pragma unroll
         for (int q = 0; q < N; ++q) {
             const float var = v[q] * by;
-            if (var > 3.402823466e38f && out[q].f == 1.f && nm[q]->kind != DBS_NORM_NONE) out[q].f = DOWN, again = true;
+            if (var > 3.402823466e38f && out[q].f == 1.f) out[q].f = DOWN, again = true;
             out[q].rstd = 1.f / sqrtf(var + nm[q]->eps * out[q].f * out[q].f);
         }
         if (!again) return;  // (the same for the whole team)
     }
+}
+
+// Column `col` of a row: an offset of 32 bits from an address that all lanes share.
+template <class T> __device__ __forceinline__ T *at_col(T *row, int col)
+{
+    const uint32_t off = (uint32_t)col * (uint32_t)sizeof(T);
+    return (T *)((char *)row + off);
+}
+// Chunk c of a lane into a row.
+template <class X, int C> __device__ __forceinline__ void put_chunk(void *base, int64_t ld, int64_t row, const Cols<C> &k, int c, const float (&v)[8])
+{
+    typename X::T *p = (typename X::T *)base + row * ld;
+    if (k.full) put_eight<X>(at_col(p, k.col[c]), 8, v);
+    else put_eight<X>(p + k.col[c], k.left[c], v);
 }
 
 // Which of a row's chunks a lane has, and which rows a team.
@@ -285,17 +340,28 @@ template <int C> struct Share : Cols<C> {
     __device__ __forceinline__ Share(int n, int waves)
     {
         const int at = waves == 1 ? lane_id() : (int)threadIdx.x, teams = waves == 1 ? (int)blockDim.x / 64 : 1;
-        row = (int)blockIdx.x * teams + (waves == 1 ? wave_id() : 0), step = (int)gridDim.x * teams;
+        row = __builtin_amdgcn_readfirstlane((int)blockIdx.x * teams + (waves == 1 ? wave_id() : 0));
+        step = (int)gridDim.x * teams;
 #pragma unroll
         for (int i = 0; i < C; ++i) this->col[i] = 8 * (i * 64 * waves + at), this->left[i] = n - this->col[i];
+        bool ragged = false;
+#pragma unroll
+        for (int i = 0; i < C; ++i) ragged |= this->left[i] < 8;
+        this->full = ballot(ragged) == 0;
     }
 };
+typedef uint32_t v4u_t __attribute__((ext_vector_type(4)));
 template <class X, int C> struct Chunks {
     typename X::V8 v[C];
     __device__ __forceinline__ void load(const void *base, int64_t ld, int64_t row, const Cols<C> &k)
     {
+        const typename X::T *p = (const typename X::T *)base + row * ld;
+        if (k.full) {
 #pragma unroll
-        for (int i = 0; i < C; ++i) v[i] = get_eight<X>((const typename X::T *)base + row * ld + k.col[i], k.left[i]);
+            for (int i = 0; i < C; ++i) v[i] = load_eight<X>(at_col(p, k.col[i]));
+        } else
+#pragma unroll
+            for (int i = 0; i < C; ++i) v[i] = get_eight<X>(p + k.col[i], k.left[i]);
     }
     __device__ __forceinline__ void vector(const void *p, const Cols<C> &k, float none)
     {
@@ -303,14 +369,24 @@ template <class X, int C> struct Chunks {
         for (int i = 0; i < C; ++i) v[i] = get_vector<X>(k.left[i] > 0 ? p : nullptr, k.col[i], k.left[i], none);
     }
     __device__ __forceinline__ float operator[](int i) const { return (float)v[i >> 3][i & 7]; }
+    // (to be taken apart where it is used: values that stay over the rows would
+    // otherwise be held in 32 bits each)
+    __device__ __forceinline__ void hold()
+    {
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            v4u_t w = __builtin_bit_cast(v4u_t, v[i]);
+            asm volatile("" : "+v"(w));
+            v[i] = __builtin_bit_cast(typename X::V8, w);
+        }
+    }
 };
 
 // Each team takes rows of up to 512 C columns a wave, the next one on its way while
 // one is worked on; the vectors stay in registers, or (C = 2, which needs those
 // for the rows) come from the caches each time.
-template <class X, bool BRANCH, int C> __global__ __launch_bounds__(64 * MAX_TEAM) void k_edge(EdgeArgs a, int waves)
+template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __launch_bounds__(64 * MAX_TEAM) void k_edge(EdgeArgs a, int waves)
 {
-    typedef typename X::T T;
     __shared__ float red[2][2][MAX_TEAM];
     Team team{red, waves, 0};
     const Share<C> k(a.n, waves);
@@ -319,14 +395,11 @@ template <class X, bool BRANCH, int C> __global__ __launch_bounds__(64 * MAX_TEA
     const int64_t chunks = (a.n + 7) / 8;
     const int last = (int)e8_blocks(a.n) * 16;
     const float by = 1.f / (float)a.n;
-    const bool norm_a = BRANCH && a.after.kind != DBS_NORM_NONE, norm_b = a.before.kind != DBS_NORM_NONE;
     Chunks<X, C> wa, ba, wb, bb, gate;
     auto vectors = [&]() {
-        wb.vector(a.before.w, k, 1.f), bb.vector(a.before.b, k, 0.f);
-        if constexpr (BRANCH) {
-            wa.vector(a.after.w, k, 1.f), ba.vector(a.after.b, k, 0.f);
-            gate.vector(a.ldg == 0 ? a.gate : nullptr, k, 1.f);
-        }
+        if constexpr (BEFORE) wb.vector(a.before.w, k, 1.f), bb.vector(a.before.b, k, 0.f);
+        if constexpr (AFTER) wa.vector(a.after.w, k, 1.f), ba.vector(a.after.b, k, 0.f);
+        if constexpr (BRANCH) gate.vector(a.ldg == 0 ? a.gate : nullptr, k, 1.f);
     };
     if (C == 1) vectors();
     const bool gates = BRANCH && a.gate && a.ldg != 0;
@@ -350,7 +423,7 @@ template <class X, bool BRANCH, int C> __global__ __launch_bounds__(64 * MAX_TEA
         if (gates) gate = gnext;
         if (row + k.step < a.rows) load(row + k.step);
         if constexpr (BRANCH) {
-            if (norm_a) {
+            if constexpr (AFTER) {
                 const NormOf *nm[1] = {&a.after};
                 const float *x[1] = {u};
                 Stat st[1];
@@ -370,29 +443,29 @@ template <class X, bool BRANCH, int C> __global__ __launch_bounds__(64 * MAX_TEA
                 }
                 float out[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float t = __builtin_fmaf(gate[8 * c + i], u[8 * c + i], a.scale * s[8 * c + i]);
-                    s[8 * c + i] = i < k.left[c] ? t : 0.f;
-                    out[i] = t;
-                }
-                put_eight<X>((T *)a.stream + row * a.lds + k.col[c], k.left[c], out);
+                for (int i = 0; i < 8; ++i) out[i] = s[8 * c + i] = __builtin_fmaf(gate[8 * c + i], u[8 * c + i], a.scale * s[8 * c + i]);
+                if (!k.full)  // (zeros behind the row, as everywhere)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[8 * c + i] = i < k.left[c] ? s[8 * c + i] : 0.f;
+                put_chunk<X, C>(a.stream, a.lds, row, k, c, out);
             }
         }
-        if (!norm_b) continue;
-        const NormOf *nm[1] = {&a.before};
-        const float *x[1] = {s};
-        Stat st[1];
-        team_stats(team, k, by, nm, x, st);
+        if constexpr (BEFORE) {
+            const NormOf *nm[1] = {&a.before};
+            const float *x[1] = {s};
+            Stat st[1];
+            team_stats(team, k, by, nm, x, st);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            float h[8];
+            for (int c = 0; c < C; ++c) {
+                float h[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] = __builtin_fmaf(st[0].xh(s[8 * c + i]), wb[8 * c + i], bb[8 * c + i]);
-            if (a.codes) {
+                for (int i = 0; i < 8; ++i) h[i] = __builtin_fmaf(st[0].xh(s[8 * c + i]), wb[8 * c + i], bb[8 * c + i]);
+                if (a.codes) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[i] = i < k.left[c] ? h[i] : 0.f;
-                put_codes<X>(a, row, k.col[c] / 8, last, h);
-            } else put_eight<X>((T *)a.h + row * a.ldh + k.col[c], k.left[c], h);
+                    for (int i = 0; i < 8; ++i) h[i] = i < k.left[c] ? h[i] : 0.f;
+                    put_codes<X>(a, row, k.col[c] / 8, last, h);
+                } else put_chunk<X, C>(a.h, a.ldh, row, k, c, h);
+            }
         }
     }
 }
@@ -573,9 +646,10 @@ template <class X, bool BRANCH> __global__ __launch_bounds__(64 * STRIP_WAVES) v
 // The same for the gradients: a lane holds the sums over its team's rows of its
 // columns, the workgroups' are added afterwards.  Bound by the bytes and, where a
 // compute unit has one workgroup, by the four sums over a row one after the other.
-template <class X, bool BRANCH, int C, int TEAM> __global__ __launch_bounds__(64 * TEAM) void k_edge_back(EdgeBackArgs a, int waves)
+template <class X, bool BRANCH, bool AFTER, bool BEFORE, int TEAM>
+__global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs a, int waves)
 {
-    typedef typename X::T T;
+    constexpr int C = 1;
     __shared__ float red[2][2][MAX_TEAM];
     Team team{red, waves, 0};
     const Share<C> k(a.n, waves);
@@ -583,51 +657,53 @@ template <class X, bool BRANCH, int C, int TEAM> __global__ __launch_bounds__(64
     rng_of(a.drop, seed, offset);
     const int64_t chunks = (a.n + 7) / 8;
     const float by = 1.f / (float)a.n;
-    const bool norm_a = BRANCH && a.after.kind != DBS_NORM_NONE, norm_b = a.before.kind != DBS_NORM_NONE;
     const bool gates = BRANCH && a.gate && a.ldg != 0, dgates = BRANCH && a.gate && (a.dgate || a.at[SUM_GATE] >= 0);
     Chunks<X, C> wa, ba, wb, gate;
     auto vectors = [&]() {
-        wb.vector(a.before.w, k, 1.f);
-        if constexpr (BRANCH) {
-            wa.vector(a.after.w, k, 1.f);
-            if (dgates) ba.vector(a.after.b, k, 0.f);
-            gate.vector(a.ldg == 0 ? a.gate : nullptr, k, 1.f);
-        }
+        if constexpr (BEFORE) wb.vector(a.before.w, k, 1.f);
+        if constexpr (AFTER) wa.vector(a.after.w, k, 1.f), ba.vector(dgates ? a.after.b : nullptr, k, 0.f);
+        if constexpr (BRANCH) gate.vector(a.ldg == 0 ? a.gate : nullptr, k, 1.f);
     };
-    if (C == 1) vectors();
+    vectors();
     float sum[BRANCH ? SUMS : 2][8 * C] = {};
+    Chunks<X, C> nds{}, ndh, nxs, nxu{};
+    auto load = [&](int row) {
+        if (a.ds) nds.load(a.ds, a.ldds, row, k);
+        if constexpr (BEFORE) ndh.load(a.dh, a.lddh, row, k), nxs.load(a.stream, a.lds, row, k);
+        if constexpr (BRANCH)
+            if (a.branch) nxu.load(a.branch, a.ldb, row, k);
+    };
+    if (k.row < a.rows) load(k.row);
     for (int row = k.row; row < a.rows; row += k.step) {
-        Chunks<X, C> ds, dh, xs, xu;
-        if (C > 1) vectors();
-        if (a.ds) ds.load(a.ds, a.ldds, row, k);
-        if (norm_b) dh.load(a.dh, a.lddh, row, k), xs.load(a.stream, a.lds, row, k);
-        if constexpr (BRANCH) {
-            if (a.branch) xu.load(a.branch, a.ldb, row, k);
+        const Chunks<X, C> dh = ndh;
+        if constexpr (BEFORE) wb.hold();
+        if constexpr (AFTER) wa.hold(), ba.hold();
+        if constexpr (BRANCH) gate.hold();
+        if constexpr (BRANCH)
             if (gates) gate.load(a.gate, a.ldg, row, k);
-        }
         float d[8 * C], xb[8 * C], u[8 * C];
         Stat sb{}, sa{};
 #pragma unroll
         for (int i = 0; i < 8 * C; ++i) {
-            d[i] = a.ds ? ds[i] : 0.f;
-            if (norm_b) xb[i] = xs[i];
-            if (BRANCH && a.branch) u[i] = xu[i];
+            d[i] = nds[i];
+            if (BEFORE) xb[i] = nxs[i];
+            if (BRANCH) u[i] = nxu[i];
         }
-        if (norm_a && norm_b) {
+        if (row + k.step < a.rows) load(row + k.step);
+        if constexpr (AFTER && BEFORE) {
             const NormOf *nm[2] = {&a.before, &a.after};
             const float *x[2] = {xb, u};
             Stat st[2];
             team_stats(team, k, by, nm, x, st);
             sb = st[0], sa = st[1];
-        } else if (norm_a || norm_b) {
-            const NormOf *nm[1] = {norm_b ? &a.before : &a.after};
-            const float *x[1] = {norm_b ? xb : u};
+        } else if constexpr (AFTER || BEFORE) {
+            const NormOf *nm[1] = {BEFORE ? &a.before : &a.after};
+            const float *x[1] = {BEFORE ? xb : u};
             Stat st[1];
             team_stats(team, k, by, nm, x, st);
-            if (norm_b) sb = st[0];
-            else sa = st[0];
+            (BEFORE ? sb : sa) = st[0];
         }
-        if (norm_b) {
+        if constexpr (BEFORE) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 8 * C; ++i) {
@@ -648,37 +724,46 @@ template <class X, bool BRANCH, int C, int TEAM> __global__ __launch_bounds__(64
                 float v[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = d[8 * c + i] * a.scale;
-                put_eight<X>((T *)a.dres + row * a.lddr + k.col[c], k.left[c], v);
+                put_chunk<X, C>(a.dres, a.lddr, row, k, c, v);
             }
         if constexpr (BRANCH) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                float keep[8], v[8];
+                uint32_t kept = 255u;
+                if (a.drop.threshold) kept = kept_of(a.drop, seed, offset, row * chunks + k.col[c] / 8);
+                const float by_kept = a.drop.threshold ? a.drop.scale : 1.f;
+                if constexpr (AFTER)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) keep[i] = 1.f;
-                if (a.drop.threshold) drop_eight(a.drop, seed, offset, row * chunks + k.col[c] / 8, keep);
+                    for (int i = 0; i < 8; ++i) u[8 * c + i] = sa.xh(u[8 * c + i]);
+                if (dgates) {
+                    float v[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int q = 8 * c + i;
-                    if (norm_a) u[q] = sa.xh(u[q]);
-                    if (dgates) {
-                        const float y = norm_a ? __builtin_fmaf(u[q], wa[q], ba[q]) : u[q];
-                        v[i] = keep[i] != 0.f ? d[q] * y * keep[i] : 0.f;
+                    for (int i = 0; i < 8; ++i) {
+                        const int q = 8 * c + i;
+                        const float y = AFTER ? __builtin_fmaf(u[q], wa[q], ba[q]) : u[q];
+                        v[i] = kept >> i & 1 ? d[q] * y * by_kept : 0.f;
                         sum[SUM_GATE][q] += v[i];
                     }
-                    d[q] = keep[i] != 0.f ? d[q] * gate[q] * keep[i] : 0.f;  // (behind dropout and gate)
-                    if (i >= k.left[c]) d[q] = 0.f;
-                    if (norm_a) {
+                    if (a.dgate) put_chunk<X, C>(a.dgate, a.lddg, row, k, c, v);
+                }
+                // (behind dropout and gate)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[8 * c + i] = kept >> i & 1 ? d[8 * c + i] * gate[8 * c + i] * by_kept : 0.f;
+                if (!k.full)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[8 * c + i] = i < k.left[c] ? d[8 * c + i] : 0.f;
+                if constexpr (AFTER)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int q = 8 * c + i;
                         const float g = d[q] * wa[q];
                         m[0] = __builtin_fmaf(g, u[q], m[0]), m[1] += g;
                         sum[SUM_AFTER_W][q] = __builtin_fmaf(d[q], u[q], sum[SUM_AFTER_W][q]);
                         sum[SUM_AFTER_B][q] += d[q];
                     }
-                }
-                if (a.dgate && dgates) put_eight<X>((T *)a.dgate + row * a.lddg + k.col[c], k.left[c], v);
             }
-            if (norm_a) {
+            if constexpr (AFTER) {
                 team.sum(m);
                 const BackStat b{sa, m[0] * by, a.after.kind == DBS_NORM_LAYER ? m[1] * by : 0.f};
 #pragma unroll
@@ -690,7 +775,7 @@ template <class X, bool BRANCH, int C, int TEAM> __global__ __launch_bounds__(64
                     float v[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[i] = d[8 * c + i];
-                    put_eight<X>((T *)a.dbranch + row * a.lddb + k.col[c], k.left[c], v);
+                    put_chunk<X, C>(a.dbranch, a.lddb, row, k, c, v);
                 }
         }
     }
@@ -768,27 +853,31 @@ static int team_waves(int32_t n, int c) { return (int)(((int64_t)n + 512 * c - 1
 static int team_threads(int waves) { return 64 * (waves == 1 ? 4 : waves); }
 static int team_rows(int waves) { return waves == 1 ? 4 : 1; }
 
-template <class X, bool BRANCH, int C> static hipError_t edge_c(const EdgeArgs &a, int32_t cus, hipStream_t s)
+template <class X, bool BRANCH, bool AFTER, bool BEFORE> static hipError_t edge_t(const EdgeArgs &a, int32_t cus, hipStream_t s)
 {
-    const int waves = team_waves(a.n, C), rows = team_rows(waves);
+    if (a.n > 1024 * MAX_TEAM) {
+        hipLaunchKernelGGL((k_edge_long<X, BRANCH>), dim3((unsigned)std::min(a.rows, 2 * cus)), dim3(64 * LONG_WAVES), 0, s, a);
+        return hipGetLastError();
+    }
+    const int c = a.n <= 512 * MAX_TEAM ? 1 : 2, waves = team_waves(a.n, c), rows = team_rows(waves);
     // (as many as fit beside each other: 2048 threads a compute unit)
     const int64_t most = (int64_t)cus * (2048 / team_threads(waves));
-    const dim3 grid((unsigned)std::min<int64_t>(((int64_t)a.rows + rows - 1) / rows, most));
-    hipLaunchKernelGGL((k_edge<X, BRANCH, C>), grid, dim3((unsigned)team_threads(waves)), 0, s, a, waves);
+    const dim3 grid((unsigned)std::min<int64_t>(((int64_t)a.rows + rows - 1) / rows, most)), block((unsigned)team_threads(waves));
+    if (c == 1) hipLaunchKernelGGL((k_edge<X, BRANCH, AFTER, BEFORE, 1>), grid, block, 0, s, a, waves);
+    else hipLaunchKernelGGL((k_edge<X, BRANCH, AFTER, BEFORE, 2>), grid, block, 0, s, a, waves);
     return hipGetLastError();
 }
-template <class X, bool BRANCH> static hipError_t edge_t(const EdgeArgs &a, int32_t cus, hipStream_t s)
+template <class X> static hipError_t edge_x(const EdgeArgs &a, int32_t cus, hipStream_t s)
 {
-    if (a.n <= 512 * MAX_TEAM) return edge_c<X, BRANCH, 1>(a, cus, s);
-    if (a.n <= 1024 * MAX_TEAM) return edge_c<X, BRANCH, 2>(a, cus, s);
-    hipLaunchKernelGGL((k_edge_long<X, BRANCH>), dim3((unsigned)std::min(a.rows, 2 * cus)), dim3(64 * LONG_WAVES), 0, s, a);
-    return hipGetLastError();
+    const bool after = a.after.kind != DBS_NORM_NONE, before = a.before.kind != DBS_NORM_NONE;
+    if (!a.branch) return edge_t<X, false, false, true>(a, cus, s);
+    if (after) return before ? edge_t<X, true, true, true>(a, cus, s) : edge_t<X, true, true, false>(a, cus, s);
+    return before ? edge_t<X, true, false, true>(a, cus, s) : edge_t<X, true, false, false>(a, cus, s);
 }
 hipError_t launch_edge(bool bf16, const EdgeArgs &a, int32_t cus, hipStream_t s)
 {
     if (a.rows == 0 || a.n == 0) return hipSuccess;
-    if (a.branch) return bf16 ? edge_t<Bf16, true>(a, cus, s) : edge_t<Fp16, true>(a, cus, s);
-    return bf16 ? edge_t<Bf16, false>(a, cus, s) : edge_t<Fp16, false>(a, cus, s);
+    return bf16 ? edge_x<Bf16>(a, cus, s) : edge_x<Fp16>(a, cus, s);
 }
 
 // Workgroups along the rows: enough to fill the device, none with less than a row
@@ -798,20 +887,17 @@ static int32_t strip_blocks(int32_t rows, int32_t n, int32_t cus)
     const int64_t strips = ((int64_t)n + STRIP - 1) / STRIP, want = strips ? (4 * (int64_t)cus + strips - 1) / strips : 1;
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ((int64_t)rows + STRIP_WAVES - 1) / STRIP_WAVES, 65535}));
 }
-// Whether the registers of a workgroup hold rows of n columns; chunks a lane (up to
-// eight waves have 256 registers each, which the sums of a join need) and teams: the
-// sums' bytes, written and read again, are to stay few beside the rows'.
-constexpr int BACK_TEAM = 8;
-static bool back_fits(int32_t n) { return n <= 1024 * BACK_TEAM; }
-static int back_chunks(int32_t n) { return n <= 512 * BACK_TEAM ? 1 : 2; }
+// Whether the registers of a workgroup hold rows of n columns, and its teams: the sums'
+// bytes, written and read again, are to stay few beside the rows'.
+static bool back_fits(int32_t n) { return n <= 512 * MAX_TEAM; }
 static int32_t back_groups(int32_t rows, int32_t n, int32_t cus)
 {
-    const int waves = team_waves(n, back_chunks(n)), each = team_rows(waves);
+    const int waves = team_waves(n, 1), each = team_rows(waves);
     return (int32_t)std::min<int64_t>(((int64_t)rows + each - 1) / each, (int64_t)cus * std::max(1, 1024 / team_threads(waves)));
 }
 static int32_t sum_blocks(int32_t rows, int32_t n, int32_t cus)
 {
-    return back_fits(n) ? back_groups(rows, n, cus) * team_rows(team_waves(n, back_chunks(n))) : strip_blocks(rows, n, cus);
+    return back_fits(n) ? back_groups(rows, n, cus) * team_rows(team_waves(n, 1)) : strip_blocks(rows, n, cus);
 }
 static size_t part_bytes(int32_t rows, int32_t n, int sums, int32_t cus)
 {
@@ -831,13 +917,15 @@ template <class X> static hipError_t total_t(TotalArgs t, hipStream_t s)
         hipLaunchKernelGGL(k_edge_total<X>, grid, dim3(64 * TOTAL_WAVES), 0, s, t);
     });
 }
-template <class X, bool BRANCH> static hipError_t edge_back_t(const EdgeBackArgs &a, int32_t cus, hipStream_t s)
+template <class X, bool BRANCH, bool AFTER, bool BEFORE> static hipError_t edge_back_t(const EdgeBackArgs &a, int32_t cus, hipStream_t s)
 {
     if (a.rows > 0 && back_fits(a.n)) {
-        const int waves = team_waves(a.n, back_chunks(a.n));
+        const int waves = team_waves(a.n, 1);
         const dim3 grid((unsigned)back_groups(a.rows, a.n, cus)), block((unsigned)team_threads(waves));
-        if (back_chunks(a.n) == 1) hipLaunchKernelGGL((k_edge_back<X, BRANCH, 1, BACK_TEAM>), grid, block, 0, s, a, waves);
-        else hipLaunchKernelGGL((k_edge_back<X, BRANCH, 2, BACK_TEAM>), grid, block, 0, s, a, waves);
+        // (the fewer waves, the more registers each)
+        if (waves <= 8) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, 8>), grid, block, 0, s, a, waves);
+        else if (waves <= 12) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, 12>), grid, block, 0, s, a, waves);
+        else hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, 16>), grid, block, 0, s, a, waves);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     } else if (a.rows > 0) {
@@ -853,6 +941,13 @@ template <class X, bool BRANCH> static hipError_t edge_back_t(const EdgeBackArgs
         if (a.at[q] >= 0) t.out[a.at[q]] = a.sum[q];
     return total_t<X>(t, s);
 }
+template <class X> static hipError_t edge_back_x(const EdgeBackArgs &a, bool has_branch, int32_t cus, hipStream_t s)
+{
+    const bool after = a.after.kind != DBS_NORM_NONE, before = a.before.kind != DBS_NORM_NONE;
+    if (!has_branch) return edge_back_t<X, false, false, true>(a, cus, s);
+    if (after) return before ? edge_back_t<X, true, true, true>(a, cus, s) : edge_back_t<X, true, true, false>(a, cus, s);
+    return before ? edge_back_t<X, true, false, true>(a, cus, s) : edge_back_t<X, true, false, false>(a, cus, s);
+}
 hipError_t launch_column_total(bool bf16, const float *part, int32_t blocks, int32_t n, void *out, hipStream_t s)
 {
     const TotalArgs t{part, {out}, 1, blocks, n, 0};
@@ -867,8 +962,7 @@ hipError_t launch_edge_back(bool bf16, EdgeBackArgs a, bool has_branch, void *wo
     a.part = (float *)work;
     const bool norms = a.before.kind != DBS_NORM_NONE || a.after.kind != DBS_NORM_NONE;
     a.stat = norms && a.rows > 0 && !back_fits(a.n) ? (BackStat *)((uint8_t *)work + part_bytes(a.rows, a.n, a.sums, cus)) : nullptr;
-    if (has_branch) return bf16 ? edge_back_t<Bf16, true>(a, cus, s) : edge_back_t<Fp16, true>(a, cus, s);
-    return bf16 ? edge_back_t<Bf16, false>(a, cus, s) : edge_back_t<Fp16, false>(a, cus, s);
+    return bf16 ? edge_back_x<Bf16>(a, has_branch, cus, s) : edge_back_x<Fp16>(a, has_branch, cus, s);
 }
 
 hipError_t launch_dropout(bool bf16, const void *x, int64_t ldx, int32_t rows, int32_t n, const Drop &d, void *y, int64_t ldy,

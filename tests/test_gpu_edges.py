@@ -182,16 +182,17 @@ def test_strides_and_alignment(ctx, size, pad, offset, dt):
 
 def test_rows_around_outputs_stay(ctx):
     """What lies beside and behind an output is left as it was."""
-    for t, n in ((3, 100), (2, 33001), (5, 4096)):
-        buf = torch.full((t + 2, n + 16), 7.0, dtype=torch.float16, device="cuda")
-        x = torch.randn((t, n), device="cuda").half()
+    g = gen(15)
+    for t, n in ((3, 100), (2, 33001), (5, 4096), (4, 5003)):
+        buf = torch.full((t + 2, n + 16), 30000.0, dtype=torch.float16, device="cuda")
+        x = rnd(g, (t, n), torch.float16)
         out = buf[1:t + 1, 8:8 + n]
         around = torch.ones_like(buf, dtype=torch.bool)
         around[1:t + 1, 8:8 + n] = False
         for call in (lambda: ctx.norm(x, Norm(), y=out), lambda: ctx.dropout(x, 0.5, (1, 2), y=out),
                      lambda: ctx.join(x, x.clone(), before=Norm(), stream=out)):
             call()
-            assert bool((buf[around] == 7.0).all()) and not bool((out == 7.0).any())
+            assert bool((buf[around] == 30000.0).all()) and not bool((out == 30000.0).any())
 
 
 @pytest.mark.parametrize("n", [300, 4096, 33000])
