@@ -156,7 +156,7 @@ __device__ __forceinline__ Stat row_stat(const NormOf &nm, int n, GroupSum<WAVES
         }
         var = total(var) * by;
         if (!(var > 3.402823466e38f) || f != 1.f)
-            return Stat{f, mean, 1.f / sqrtf(var + nm.eps * f * f)};
+            return Stat{f, mean, rsqrtf(var + nm.eps * f * f)};
     }
 }
 
@@ -270,14 +270,20 @@ template <int C> struct Cols {
     int col[C], left[C];  // of a lane's chunks; left <= 0: behind the row
     bool full;            // all chunks of the wave have eight columns
 };
-template <int N, int C>
+// MEANS: some may be a layer norm; without, xh is x rstd (and f in rstd).
+template <bool MEANS> __device__ __forceinline__ float xh_of(const Stat &s, float x) { return MEANS ? s.xh(x) : x * s.rstd; }
+template <bool MEANS> __device__ __forceinline__ float dx_of(const BackStat &b, float g, float xh)
+{
+    return MEANS ? b.dx(g, xh) : __builtin_fmaf(-xh, b.m1, g) * b.s.rstd;
+}
+template <bool MEANS, int N, int C>
 __device__ __forceinline__ void team_stats(Team &team, const Cols<C> &k, float by, const NormOf *const (&nm)[N], const float *const (&x)[N],
                                            Stat (&out)[N])
 {
     bool layer = false;
     float v[N];
 #pragma unroll
-    for (int q = 0; q < N; ++q) layer |= nm[q]->kind == DBS_NORM_LAYER, out[q] = Stat{1.f, 0.f, 0.f};
+    for (int q = 0; q < N; ++q) layer |= MEANS && nm[q]->kind == DBS_NORM_LAYER, out[q] = Stat{1.f, 0.f, 0.f};
     auto means = [&]() {
 #pragma unroll
         for (int q = 0; q < N; ++q) {
@@ -290,13 +296,13 @@ __device__ __forceinline__ void team_stats(Team &team, const Cols<C> &k, float b
 #pragma unroll
         for (int q = 0; q < N; ++q) out[q].mean = v[q];
     };
-    auto squares = [&](bool masked) {
+    auto squares = [&](bool masked, bool plain) {
 #pragma unroll
         for (int q = 0; q < N; ++q) {
             v[q] = 0.f;
 #pragma unroll
             for (int i = 0; i < 8 * C; ++i) {
-                float d = __builtin_fmaf(x[q][i], out[q].f, -out[q].mean);
+                float d = plain ? x[q][i] : __builtin_fmaf(x[q][i], out[q].f, -out[q].mean);
                 if (masked && (i & 7) >= k.left[i >> 3]) d = 0.f;
                 v[q] = __builtin_fmaf(d, d, v[q]);
             }
@@ -304,19 +310,24 @@ __device__ __forceinline__ void team_stats(Team &team, const Cols<C> &k, float b
     };
     // (without means, zeros stand behind the row)
     const bool masked = layer && !k.full;
-    for (;;) {
+    for (bool first = true;; first = false) {
         if (layer) means();
-        if (masked) squares(true);
-        else squares(false);
+        if (masked) squares(true, false);
+        else if (!MEANS && first) squares(false, true);
+        else squares(false, false);
         team.sum(v);
         bool again = false;
 #pragma unroll
         for (int q = 0; q < N; ++q) {
             const float var = v[q] * by;
             if (var > 3.402823466e38f && out[q].f == 1.f) out[q].f = DOWN, again = true;
-            out[q].rstd = 1.f / sqrtf(var + nm[q]->eps * out[q].f * out[q].f);
+            out[q].rstd = rsqrtf(var + nm[q]->eps * out[q].f * out[q].f);
         }
-        if (!again) return;  // (the same for the whole team)
+        if (again) continue;  // (the same for the whole team)
+        if (!MEANS)
+#pragma unroll
+            for (int q = 0; q < N; ++q) out[q].rstd *= out[q].f;
+        return;
     }
 }
 
@@ -325,6 +336,12 @@ template <class T> __device__ __forceinline__ T *at_col(T *row, int col)
 {
     const uint32_t off = (uint32_t)col * (uint32_t)sizeof(T);
     return (T *)((char *)row + off);
+}
+__device__ __forceinline__ void put_floats(float *to, int left, const float *v, int at)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) to[i] = v[at + i];
 }
 // Chunk c of a lane into a row.
 template <class X, int C> __device__ __forceinline__ void put_chunk(void *base, int64_t ld, int64_t row, const Cols<C> &k, int c, const float (&v)[8])
@@ -427,7 +444,7 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __lau
                 const NormOf *nm[1] = {&a.after};
                 const float *x[1] = {u};
                 Stat st[1];
-                team_stats(team, k, by, nm, x, st);
+                team_stats<true>(team, k, by, nm, x, st);
 #pragma unroll
                 for (int i = 0; i < 8 * C; ++i) u[i] = __builtin_fmaf(st[0].xh(u[i]), wa[i], ba[i]);
             }
@@ -454,7 +471,7 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __lau
             const NormOf *nm[1] = {&a.before};
             const float *x[1] = {s};
             Stat st[1];
-            team_stats(team, k, by, nm, x, st);
+            team_stats<true>(team, k, by, nm, x, st);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 float h[8];
@@ -646,11 +663,10 @@ template <class X, bool BRANCH> __global__ __launch_bounds__(64 * STRIP_WAVES) v
 // The same for the gradients: a lane holds the sums over its team's rows of its
 // columns, the workgroups' are added afterwards.  Bound by the bytes and, where a
 // compute unit has one workgroup, by the four sums over a row one after the other.
-template <class X, bool BRANCH, bool AFTER, bool BEFORE, int TEAM>
+template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool MEANS, int C, int TEAM>
 __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs a, int waves)
 {
-    constexpr int C = 1;
-    __shared__ float red[2][2][MAX_TEAM];
+    __shared__ float red[2][2][MAX_TEAM], lanes[4][C * 512];
     Team team{red, waves, 0};
     const Share<C> k(a.n, waves);
     uint64_t seed, offset;
@@ -673,12 +689,16 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
         if constexpr (BRANCH)
             if (a.branch) nxu.load(a.branch, a.ldb, row, k);
     };
-    if (k.row < a.rows) load(k.row);
+    constexpr bool AHEAD = C == 1;  // (two chunks a lane leave no registers for it)
+    if (AHEAD && k.row < a.rows) load(k.row);
     for (int row = k.row; row < a.rows; row += k.step) {
+        if (!AHEAD) load(row);
         const Chunks<X, C> dh = ndh;
-        if constexpr (BEFORE) wb.hold();
-        if constexpr (AFTER) wa.hold(), ba.hold();
-        if constexpr (BRANCH) gate.hold();
+        if constexpr (TEAM > 8 || C > 1) {
+            if constexpr (BEFORE) wb.hold();
+            if constexpr (AFTER) wa.hold(), ba.hold();
+            if constexpr (BRANCH) gate.hold();
+        }
         if constexpr (BRANCH)
             if (gates) gate.load(a.gate, a.ldg, row, k);
         float d[8 * C], xb[8 * C], u[8 * C];
@@ -689,34 +709,37 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
             if (BEFORE) xb[i] = nxs[i];
             if (BRANCH) u[i] = nxu[i];
         }
-        if (row + k.step < a.rows) load(row + k.step);
+        if (AHEAD && row + k.step < a.rows) load(row + k.step);
         if constexpr (AFTER && BEFORE) {
             const NormOf *nm[2] = {&a.before, &a.after};
             const float *x[2] = {xb, u};
             Stat st[2];
-            team_stats(team, k, by, nm, x, st);
+            team_stats<MEANS>(team, k, by, nm, x, st);
             sb = st[0], sa = st[1];
         } else if constexpr (AFTER || BEFORE) {
             const NormOf *nm[1] = {BEFORE ? &a.before : &a.after};
             const float *x[1] = {BEFORE ? xb : u};
             Stat st[1];
-            team_stats(team, k, by, nm, x, st);
+            team_stats<MEANS>(team, k, by, nm, x, st);
             (BEFORE ? sb : sa) = st[0];
         }
         if constexpr (BEFORE) {
-            float m[2] = {0.f, 0.f};
+            float m[MEANS ? 2 : 1] = {};
 #pragma unroll
             for (int i = 0; i < 8 * C; ++i) {
-                xb[i] = sb.xh(xb[i]);
+                xb[i] = xh_of<MEANS>(sb, xb[i]);
                 const float g = dh[i] * wb[i];
-                m[0] = __builtin_fmaf(g, xb[i], m[0]), m[1] += g;
+                m[0] = __builtin_fmaf(g, xb[i], m[0]);
+                if (MEANS) m[MEANS] += g;
                 sum[SUM_BEFORE_W][i] = __builtin_fmaf(dh[i], xb[i], sum[SUM_BEFORE_W][i]);
-                sum[SUM_BEFORE_B][i] += dh[i];
             }
-            team.sum(m);
-            const BackStat b{sb, m[0] * by, a.before.kind == DBS_NORM_LAYER ? m[1] * by : 0.f};
+            if (a.at[SUM_BEFORE_B] >= 0)
 #pragma unroll
-            for (int i = 0; i < 8 * C; ++i) d[i] += b.dx(dh[i] * wb[i], xb[i]);
+                for (int i = 0; i < 8 * C; ++i) sum[SUM_BEFORE_B][i] += dh[i];
+            team.sum(m);
+            const BackStat b{sb, m[0] * by, MEANS && a.before.kind == DBS_NORM_LAYER ? m[MEANS] * by : 0.f};
+#pragma unroll
+            for (int i = 0; i < 8 * C; ++i) d[i] += dx_of<MEANS>(b, dh[i] * wb[i], xb[i]);
         }
         if (a.dres)
 #pragma unroll
@@ -727,7 +750,7 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
                 put_chunk<X, C>(a.dres, a.lddr, row, k, c, v);
             }
         if constexpr (BRANCH) {
-            float m[2] = {0.f, 0.f};
+            float m[MEANS ? 2 : 1] = {};
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 uint32_t kept = 255u;
@@ -735,7 +758,7 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
                 const float by_kept = a.drop.threshold ? a.drop.scale : 1.f;
                 if constexpr (AFTER)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) u[8 * c + i] = sa.xh(u[8 * c + i]);
+                    for (int i = 0; i < 8; ++i) u[8 * c + i] = xh_of<MEANS>(sa, u[8 * c + i]);
                 if (dgates) {
                     float v[8];
 #pragma unroll
@@ -748,26 +771,34 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
                     if (a.dgate) put_chunk<X, C>(a.dgate, a.lddg, row, k, c, v);
                 }
                 // (behind dropout and gate)
+                if (a.gate)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[8 * c + i] = kept >> i & 1 ? d[8 * c + i] * gate[8 * c + i] * by_kept : 0.f;
+                    for (int i = 0; i < 8; ++i) d[8 * c + i] *= gate[8 * c + i];
+                if (a.drop.threshold)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[8 * c + i] = kept >> i & 1 ? d[8 * c + i] * by_kept : 0.f;
                 if (!k.full)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) d[8 * c + i] = i < k.left[c] ? d[8 * c + i] : 0.f;
-                if constexpr (AFTER)
+                if constexpr (AFTER) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int q = 8 * c + i;
                         const float g = d[q] * wa[q];
-                        m[0] = __builtin_fmaf(g, u[q], m[0]), m[1] += g;
+                        m[0] = __builtin_fmaf(g, u[q], m[0]);
+                        if (MEANS) m[MEANS] += g;
                         sum[SUM_AFTER_W][q] = __builtin_fmaf(d[q], u[q], sum[SUM_AFTER_W][q]);
-                        sum[SUM_AFTER_B][q] += d[q];
                     }
+                    if (a.at[SUM_AFTER_B] >= 0)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sum[SUM_AFTER_B][8 * c + i] += d[8 * c + i];
+                }
             }
             if constexpr (AFTER) {
                 team.sum(m);
-                const BackStat b{sa, m[0] * by, a.after.kind == DBS_NORM_LAYER ? m[1] * by : 0.f};
+                const BackStat b{sa, m[0] * by, MEANS && a.after.kind == DBS_NORM_LAYER ? m[MEANS] * by : 0.f};
 #pragma unroll
-                for (int i = 0; i < 8 * C; ++i) d[i] = b.dx(d[i] * wa[i], u[i]);
+                for (int i = 0; i < 8 * C; ++i) d[i] = dx_of<MEANS>(b, d[i] * wa[i], u[i]);
             }
             if (a.dbranch)
 #pragma unroll
@@ -779,21 +810,21 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
                 }
         }
     }
-    // (a workgroup of several teams, which are waves, has a row of sums for each)
-    const int64_t block = waves == 1 ? (int64_t)blockIdx.x * (blockDim.x / 64) + wave_id() : (int64_t)blockIdx.x;
 #pragma unroll
     for (int q = 0; q < (BRANCH ? SUMS : 2); ++q) {
         if (a.at[q] < 0) continue;
+        float *to = a.part + ((int64_t)blockIdx.x * a.sums + a.at[q]) * a.n;
+        if (waves == 1) {  // a workgroup's four teams are waves: their sums are added here
+            __syncthreads();
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            float *to = a.part + (block * a.sums + a.at[q]) * a.n + k.col[c];
+            for (int i = 0; i < 8 * C; ++i) lanes[wave_id()][k.col[i >> 3] + (i & 7)] = sum[q][i];
+            __syncthreads();
+            for (int c = (int)threadIdx.x; c < a.n; c += (int)blockDim.x) to[c] = lanes[0][c] + lanes[1][c] + lanes[2][c] + lanes[3][c];
+        } else
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < k.left[c]) to[i] = sum[q][8 * c + i];
-        }
+            for (int c = 0; c < C; ++c) put_floats(to + k.col[c], k.left[c], sum[q], 8 * c);
     }
 }
-
 // The workgroups' sums, in their order: a column a lane, the workgroups shared
 // out to the waves.
 constexpr int TOTAL_WAVES = 16;
@@ -887,26 +918,31 @@ static int32_t strip_blocks(int32_t rows, int32_t n, int32_t cus)
     const int64_t strips = ((int64_t)n + STRIP - 1) / STRIP, want = strips ? (4 * (int64_t)cus + strips - 1) / strips : 1;
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ((int64_t)rows + STRIP_WAVES - 1) / STRIP_WAVES, 65535}));
 }
-// Whether the registers of a workgroup hold rows of n columns, and its teams: the sums'
-// bytes, written and read again, are to stay few beside the rows'.
-static bool back_fits(int32_t n) { return n <= 512 * MAX_TEAM; }
-static int32_t back_groups(int32_t rows, int32_t n, int32_t cus)
+// Rows of up to 8192 columns are held in registers: one chunk a lane, or (a join from
+// 6144 columns on, whose sums 16 waves have no registers for) two.
+constexpr int BACK_COLUMNS = 8192;
+static bool back_fits(int32_t n) { return n <= BACK_COLUMNS; }
+static int back_chunks(bool branch, int32_t n) { return branch && n > 6144 ? 2 : 1; }
+// Workgroups: as many as run beside each other, each with a few rows, since its sums'
+// bytes are written and read again; but no compute unit is left without.
+static int32_t back_groups(bool branch, int32_t rows, int32_t n, int32_t cus)
 {
-    const int waves = team_waves(n, 1), each = team_rows(waves);
-    return (int32_t)std::min<int64_t>(((int64_t)rows + each - 1) / each, (int64_t)cus * std::max(1, 1024 / team_threads(waves)));
+    const int waves = team_waves(n, back_chunks(branch, n)), each = team_rows(waves);
+    const int64_t teams = ((int64_t)rows + each - 1) / each, most = (int64_t)cus * std::max(1, 1024 / team_threads(waves));
+    return (int32_t)std::min(std::min(teams, most), std::max<int64_t>(cus, (teams + 7) / 8));
 }
-static int32_t sum_blocks(int32_t rows, int32_t n, int32_t cus)
+static int32_t sum_blocks(bool branch, int32_t rows, int32_t n, int32_t cus)
 {
-    return back_fits(n) ? back_groups(rows, n, cus) * team_rows(team_waves(n, 1)) : strip_blocks(rows, n, cus);
+    return back_fits(n) ? back_groups(branch, rows, n, cus) : strip_blocks(rows, n, cus);
 }
-static size_t part_bytes(int32_t rows, int32_t n, int sums, int32_t cus)
+static size_t part_bytes(bool branch, int32_t rows, int32_t n, int sums, int32_t cus)
 {
-    return ((size_t)sum_blocks(rows, n, cus) * sums * n * 4 + 255) / 256 * 256;
+    return ((size_t)sum_blocks(branch, rows, n, cus) * sums * n * 4 + 255) / 256 * 256;
 }
 size_t edge_back_work(int32_t rows, int32_t n, int sums, int32_t cus)
 {
     if (n == 0) return 0;
-    return part_bytes(rows, n, sums, cus) + (back_fits(n) ? 0 : (size_t)rows * 2 * sizeof(BackStat));
+    return std::max(part_bytes(false, rows, n, sums, cus), part_bytes(true, rows, n, sums, cus)) + (back_fits(n) ? 0 : (size_t)rows * 2 * sizeof(BackStat));
 }
 
 template <class X> static hipError_t total_t(TotalArgs t, hipStream_t s)
@@ -917,15 +953,27 @@ template <class X> static hipError_t total_t(TotalArgs t, hipStream_t s)
         hipLaunchKernelGGL(k_edge_total<X>, grid, dim3(64 * TOTAL_WAVES), 0, s, t);
     });
 }
+template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool MEANS> static void edge_back_m(const EdgeBackArgs &a, hipStream_t s)
+{
+    const int chunks = back_chunks(BRANCH, a.n), waves = team_waves(a.n, chunks);
+    const dim3 grid((unsigned)a.blocks), block((unsigned)team_threads(waves));
+    // (the fewer waves, the more registers each)
+    if constexpr (BRANCH)
+        if (chunks == 2) {
+            hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 2, 8>), grid, block, 0, s, a, waves);
+            return;
+        }
+    if (waves <= 8) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 8>), grid, block, 0, s, a, waves);
+    else if (waves <= 12) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 12>), grid, block, 0, s, a, waves);
+    else if constexpr (!BRANCH) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 16>), grid, block, 0, s, a, waves);
+}
 template <class X, bool BRANCH, bool AFTER, bool BEFORE> static hipError_t edge_back_t(const EdgeBackArgs &a, int32_t cus, hipStream_t s)
 {
     if (a.rows > 0 && back_fits(a.n)) {
-        const int waves = team_waves(a.n, 1);
-        const dim3 grid((unsigned)back_groups(a.rows, a.n, cus)), block((unsigned)team_threads(waves));
-        // (the fewer waves, the more registers each)
-        if (waves <= 8) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, 8>), grid, block, 0, s, a, waves);
-        else if (waves <= 12) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, 12>), grid, block, 0, s, a, waves);
-        else hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, 16>), grid, block, 0, s, a, waves);
+        if constexpr (AFTER || BEFORE) {
+            if ((AFTER && a.after.kind == DBS_NORM_LAYER) || (BEFORE && a.before.kind == DBS_NORM_LAYER)) edge_back_m<X, BRANCH, AFTER, BEFORE, true>(a, s);
+            else edge_back_m<X, BRANCH, AFTER, BEFORE, false>(a, s);
+        } else edge_back_m<X, BRANCH, AFTER, BEFORE, false>(a, s);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     } else if (a.rows > 0) {
@@ -958,10 +1006,10 @@ hipError_t launch_edge_back(bool bf16, EdgeBackArgs a, bool has_branch, void *wo
     if (a.n == 0) return hipSuccess;
     a.sums = 0;
     for (int q = 0; q < SUMS; ++q) a.at[q] = a.sum[q] ? a.sums++ : -1;
-    a.blocks = sum_blocks(a.rows, a.n, cus);
+    a.blocks = sum_blocks(has_branch, a.rows, a.n, cus);
     a.part = (float *)work;
     const bool norms = a.before.kind != DBS_NORM_NONE || a.after.kind != DBS_NORM_NONE;
-    a.stat = norms && a.rows > 0 && !back_fits(a.n) ? (BackStat *)((uint8_t *)work + part_bytes(a.rows, a.n, a.sums, cus)) : nullptr;
+    a.stat = norms && a.rows > 0 && !back_fits(a.n) ? (BackStat *)((uint8_t *)work + part_bytes(has_branch, a.rows, a.n, a.sums, cus)) : nullptr;
     return bf16 ? edge_back_x<Bf16>(a, has_branch, cus, s) : edge_back_x<Fp16>(a, has_branch, cus, s);
 }
 
