@@ -75,8 +75,11 @@ def _drop_desc(torch, p, rng, device):
     return _lib.DropDesc(p, seed, offset, None), None
 
 
-def _wants(*tensors):
-    return any(t is not None and t.requires_grad for t in tensors)
+def _wants(tensors):
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            return True
+    return False
 
 
 def _at(t):
@@ -127,15 +130,16 @@ class EdgeOps:
                 out = self._new_blocks(t, n, "row", x.dtype)
                 check(self._fn.dbs_norm(self._h, dt, t, n, x.data_ptr(), ldx, ctypes.byref(desc), None, 0, out._ref()))
                 return out
-            out = given if given is not None else torch.empty((t, n), dtype=x.dtype, device=dev)
+            out = given if given is not None else x.new_empty((t, n))
             check(self._fn.dbs_norm(self._h, dt, t, n, x.data_ptr(), ldx, ctypes.byref(desc), out.data_ptr(),
                                     n if given is None else ldy, None))
             return out
         out = self._call(body, (x, norm.weight, norm.bias, given))
         if to8:
             return out
-        if _wants(x, norm.weight, norm.bias):
-            out, = _no_graph(torch, "norm", (x, norm.weight, norm.bias), (out,))
+        inputs = (x, norm.weight, norm.bias)
+        if _wants(inputs):
+            out, = _no_graph(torch, "norm", inputs, (out,))
         return out[0] if one else out
 
     def _edge_work(self, rows, n, sums):
@@ -161,7 +165,7 @@ class EdgeOps:
         ldadd = 0 if add is None else check_rows(add, "add", dy.dtype, dev, t, n)
 
         def body():
-            new = lambda *shape: torch.empty(shape, dtype=dy.dtype, device=dev)  # noqa: E731
+            new = lambda *shape: dy.new_empty(shape)  # noqa: E731
             dx = new(t, n) if need_dx else None
             dw = new(n) if need_dw and norm.weight is not None else None
             db = new(n) if need_dw and norm.bias is not None else None
@@ -205,18 +209,18 @@ class EdgeOps:
             _check_apart(stream, "stream", tuple((None if same and v is residual else v, k) for v, k in zip(inputs, names)))
 
         def body():
-            out = given if given is not None else torch.empty((t, n), dtype=dtype, device=dev)
+            out = given if given is not None else branch.new_empty((t, n))
             h = h8 = None
             if to8:
                 h8 = self._new_blocks(t, n, "row", dtype)
             elif before is not None:
-                h = torch.empty((t, n), dtype=dtype, device=dev)
+                h = branch.new_empty((t, n))
             check(self._fn.dbs_join(self._h, dt, t, n, branch.data_ptr(), ldb, residual.data_ptr(), ldr, _ref(da), _ref(db),
                                     _at(gate), ldg, scale, _ref(drop), out.data_ptr(), n if given is None else lds, _at(h), n,
                                     None if h8 is None else h8._ref()))
             return out, h8 if to8 else h
         out, h = self._call(body, (*inputs, rng_t, given))
-        if _wants(*inputs):
+        if _wants(inputs):
             out, h = _no_graph(torch, "join", inputs, (out, h))
         if one:
             out, h = out[0], h if to8 or h is None else h[0]
@@ -251,7 +255,7 @@ class EdgeOps:
         drop, rng_t = _drop_desc(torch, p, rng, dev)
 
         def body():
-            new = lambda *shape: torch.empty(shape, dtype=dtype, device=dev)  # noqa: E731
+            new = lambda *shape: lead.new_empty(shape)  # noqa: E731
             vector = lambda v: new(n) if need_dw and v is not None else None  # noqa: E731
             wa, ba, wb, bb = (vector(v) for v in (*_params(after), *_params(before)))
             dgate = None if gate is None or not need_dw else new(n) if ldg == 0 else new(t, n)
@@ -286,11 +290,11 @@ class EdgeOps:
             _check_apart(y, "y", ((None if y.data_ptr() == x.data_ptr() and ldy == ldx else x, "x"),))
 
         def body():
-            out = given if given is not None else torch.empty((t, n), dtype=x.dtype, device=dev)
+            out = given if given is not None else x.new_empty((t, n))
             check(self._fn.dbs_dropout(self._h, dt, t, n, x.data_ptr(), ldx, ctypes.byref(drop), out.data_ptr(),
                                        n if given is None else ldy))
             return out
         out = self._call(body, (x, rng_t, given))
-        if _wants(x):
+        if x.requires_grad:
             out, = _no_graph(torch, "dropout", (x,), (out,), "its gradient is the same call on the gradient")
         return out[0] if one else out
