@@ -11,7 +11,7 @@ typedef int v4i_t __attribute__((ext_vector_type(4)));
 
 constexpr int R8_U = 8;               // blocks that a wave has on their way
 constexpr int R8_WAVES = 8;
-constexpr int64_t R8_LDS = 48 << 10;  // of x in blocks
+constexpr int64_t R8_PACK = 128;      // blocks of x that a workgroup packs itself
 
 struct Rows8Args {
     Mul8Args m;
@@ -39,13 +39,15 @@ template <class X, bool RAW> __global__ __launch_bounds__(64 * R8_WAVES) void k_
     const uint8_t *q = m.q.codes + token * m.q.ld + 16 * g, *qe = m.q.exps + token * m.q.lde;
     uint8_t *xs = lds, *xe = lds + (int64_t)t * a.ldl;
 
-    v4i_t lo[R8_U], hi[R8_U];
+    v4i_t lo[R8_U], hi[R8_U], xl[R8_U], xh[R8_U];
+    int se[R8_U];
     auto fetch = [&](int b) {
 #pragma unroll
         for (int u = 0; u < R8_U; ++u)
             if (b + u < b1) {
-                lo[u] = __builtin_nontemporal_load((const v4i_t *)(w + (int64_t)(b + u) * E8_BLOCK));
-                hi[u] = __builtin_nontemporal_load((const v4i_t *)(w + (int64_t)(b + u) * E8_BLOCK + 64));
+                const int64_t at = (int64_t)(b + u) * E8_BLOCK;
+                lo[u] = *(const v4i_t *)(w + at), hi[u] = *(const v4i_t *)(w + at + 64);
+                if constexpr (!RAW) xl[u] = *(const v4i_t *)(q + at), xh[u] = *(const v4i_t *)(q + at + 64), se[u] = qe[b + u];
             }
     };
     fetch(b0);
@@ -69,12 +71,13 @@ template <class X, bool RAW> __global__ __launch_bounds__(64 * R8_WAVES) void k_
 #pragma unroll
         for (int u = 0; u < R8_U; ++u)
             if (b + u < b1) {
-                const uint8_t *x = RAW ? xs + token * a.ldl + (b + u) * E8_BLOCK + 16 * g : q + (int64_t)(b + u) * E8_BLOCK;
-                const v4i_t xl = *(const v4i_t *)x, xh = *(const v4i_t *)(x + 64);
-                const int se = RAW ? xe[token * a.blocks + b + u] : qe[b + u];
+                if constexpr (RAW) {
+                    const uint8_t *x = xs + token * a.ldl + (b + u) * E8_BLOCK + 16 * g;
+                    xl[u] = *(const v4i_t *)x, xh[u] = *(const v4i_t *)(x + 64), se[u] = xe[token * a.blocks + b + u];
+                }
                 acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_shufflevector(lo[u], hi[u], 0, 1, 2, 3, 4, 5, 6, 7),
-                                                                       __builtin_shufflevector(xl, xh, 0, 1, 2, 3, 4, 5, 6, 7), acc, 0, 0, 0,
-                                                                       (int)pe[b + u], 0, se);
+                                                                       __builtin_shufflevector(xl[u], xh[u], 0, 1, 2, 3, 4, 5, 6, 7), acc, 0, 0, 0,
+                                                                       (int)pe[b + u], 0, se[u]);
             }
         fetch(b + R8_U);
     }
@@ -99,7 +102,7 @@ static int64_t token_bytes(int64_t blocks) { return blocks * E8_BLOCK + 16; }
 
 bool rows8_pack(int64_t tokens, int64_t cols)
 {
-    return tokens <= ROWS8_TOKENS && tokens * (token_bytes(e8_blocks(cols)) + e8_blocks(cols)) <= R8_LDS;
+    return tokens <= ROWS8_TOKENS && tokens * e8_blocks(cols) <= R8_PACK;
 }
 
 template <class X> static hipError_t rows8_t(Rows8Args a, hipStream_t s)
