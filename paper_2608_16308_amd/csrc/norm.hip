@@ -428,8 +428,10 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __lau
             if (gates) gnext.load(a.gate, a.ldg, row, k);
         }
     };
-    if (k.row < a.rows) load(k.row);
+    constexpr bool AHEAD = C == 1 || !(AFTER && BEFORE);  // (where registers are left for it)
+    if (AHEAD && k.row < a.rows) load(k.row);
     for (int row = k.row; row < a.rows; row += k.step) {
+        if (!AHEAD) load(row);
         float s[8 * C], u[8 * C];
 #pragma unroll
         for (int i = 0; i < 8 * C; ++i) {
@@ -438,7 +440,7 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __lau
         }
         if (C > 1) vectors();
         if (gates) gate = gnext;
-        if (row + k.step < a.rows) load(row + k.step);
+        if (AHEAD && row + k.step < a.rows) load(row + k.step);
         if constexpr (BRANCH) {
             if constexpr (AFTER) {
                 const NormOf *nm[1] = {&a.after};
@@ -866,7 +868,7 @@ __global__ __launch_bounds__(DROP_TPB) void k_dropout(const typename X::T *x, in
     rng_of(d, seed, offset);
     const int64_t chunks = (int64_t)rows * per;
     for (int64_t c = (int64_t)blockIdx.x * DROP_TPB + threadIdx.x; c < chunks; c += (int64_t)gridDim.x * DROP_TPB) {
-        const int64_t row = c / per;
+        const int64_t row = chunks <= UINT32_MAX ? (uint32_t)c / (uint32_t)per : c / per;  // (32 bits divide much faster)
         const int col = 8 * (int)(c - row * per), left = n - col;
         float v[8];
         get_floats<X>(x + row * ldx + col, left, v);
@@ -918,11 +920,10 @@ static int32_t strip_blocks(int32_t rows, int32_t n, int32_t cus)
     const int64_t strips = ((int64_t)n + STRIP - 1) / STRIP, want = strips ? (4 * (int64_t)cus + strips - 1) / strips : 1;
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ((int64_t)rows + STRIP_WAVES - 1) / STRIP_WAVES, 65535}));
 }
-// Rows of up to 8192 columns are held in registers: one chunk a lane, or (a join from
-// 6144 columns on, whose sums 16 waves have no registers for) two.
-constexpr int BACK_COLUMNS = 8192;
-static bool back_fits(int32_t n) { return n <= BACK_COLUMNS; }
-static int back_chunks(bool branch, int32_t n) { return branch && n > 6144 ? 2 : 1; }
+// Rows of up to 8192 columns (a norm alone: 16384) are held in registers: one chunk a
+// lane, or, where 16 waves have no registers for the sums, two or four of eight waves.
+static bool back_fits(bool branch, int32_t n) { return n <= (branch ? 8192 : 16384); }
+static int back_chunks(bool branch, int32_t n) { return branch ? (n > 6144 ? 2 : 1) : n > 8192 ? 4 : 1; }
 // Workgroups: as many as run beside each other, each with a few rows, since its sums'
 // bytes are written and read again; but no compute unit is left without.
 static int32_t back_groups(bool branch, int32_t rows, int32_t n, int32_t cus)
@@ -933,7 +934,7 @@ static int32_t back_groups(bool branch, int32_t rows, int32_t n, int32_t cus)
 }
 static int32_t sum_blocks(bool branch, int32_t rows, int32_t n, int32_t cus)
 {
-    return back_fits(n) ? back_groups(branch, rows, n, cus) : strip_blocks(rows, n, cus);
+    return back_fits(branch, n) ? back_groups(branch, rows, n, cus) : strip_blocks(rows, n, cus);
 }
 static size_t part_bytes(bool branch, int32_t rows, int32_t n, int sums, int32_t cus)
 {
@@ -942,7 +943,7 @@ static size_t part_bytes(bool branch, int32_t rows, int32_t n, int sums, int32_t
 size_t edge_back_work(int32_t rows, int32_t n, int sums, int32_t cus)
 {
     if (n == 0) return 0;
-    return std::max(part_bytes(false, rows, n, sums, cus), part_bytes(true, rows, n, sums, cus)) + (back_fits(n) ? 0 : (size_t)rows * 2 * sizeof(BackStat));
+    return std::max(part_bytes(false, rows, n, sums, cus), part_bytes(true, rows, n, sums, cus)) + (back_fits(true, n) ? 0 : (size_t)rows * 2 * sizeof(BackStat));
 }
 
 template <class X> static hipError_t total_t(TotalArgs t, hipStream_t s)
@@ -958,18 +959,14 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool MEANS> static void
     const int chunks = back_chunks(BRANCH, a.n), waves = team_waves(a.n, chunks);
     const dim3 grid((unsigned)a.blocks), block((unsigned)team_threads(waves));
     // (the fewer waves, the more registers each)
-    if constexpr (BRANCH)
-        if (chunks == 2) {
-            hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 2, 8>), grid, block, 0, s, a, waves);
-            return;
-        }
-    if (waves <= 8) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 8>), grid, block, 0, s, a, waves);
+    if (chunks > 1) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, BRANCH ? 2 : 4, 8>), grid, block, 0, s, a, waves);
+    else if (waves <= 8) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 8>), grid, block, 0, s, a, waves);
     else if (waves <= 12) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 12>), grid, block, 0, s, a, waves);
     else if constexpr (!BRANCH) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 16>), grid, block, 0, s, a, waves);
 }
 template <class X, bool BRANCH, bool AFTER, bool BEFORE> static hipError_t edge_back_t(const EdgeBackArgs &a, int32_t cus, hipStream_t s)
 {
-    if (a.rows > 0 && back_fits(a.n)) {
+    if (a.rows > 0 && back_fits(BRANCH, a.n)) {
         if constexpr (AFTER || BEFORE) {
             if ((AFTER && a.after.kind == DBS_NORM_LAYER) || (BEFORE && a.before.kind == DBS_NORM_LAYER)) edge_back_m<X, BRANCH, AFTER, BEFORE, true>(a, s);
             else edge_back_m<X, BRANCH, AFTER, BEFORE, false>(a, s);
@@ -1009,7 +1006,7 @@ hipError_t launch_edge_back(bool bf16, EdgeBackArgs a, bool has_branch, void *wo
     a.blocks = sum_blocks(has_branch, a.rows, a.n, cus);
     a.part = (float *)work;
     const bool norms = a.before.kind != DBS_NORM_NONE || a.after.kind != DBS_NORM_NONE;
-    a.stat = norms && a.rows > 0 && !back_fits(a.n) ? (BackStat *)((uint8_t *)work + part_bytes(has_branch, a.rows, a.n, a.sums, cus)) : nullptr;
+    a.stat = norms && a.rows > 0 && !back_fits(has_branch, a.n) ? (BackStat *)((uint8_t *)work + part_bytes(has_branch, a.rows, a.n, a.sums, cus)) : nullptr;
     return bf16 ? edge_back_x<Bf16>(a, has_branch, cus, s) : edge_back_x<Fp16>(a, has_branch, cus, s);
 }
 

@@ -181,7 +181,7 @@ __global__ __launch_bounds__(P8_TPB) void k_unpack8(Blocks b, int32_t rows, int3
 {
     const int64_t chunks = (int64_t)rows * per;
     for (int64_t c = (int64_t)blockIdx.x * P8_TPB + threadIdx.x; c < chunks; c += (int64_t)gridDim.x * P8_TPB) {
-        const int64_t row = c / per;
+        const int64_t row = chunks <= UINT32_MAX ? (uint32_t)c / (uint32_t)per : c / per;
         const int col = 8 * (int)(c - row * per), left = cols - col;
         float v[8];
         e8_values<X>(*(const uint2 *)(b.codes + row * b.ld + col), (int)b.exps[(row >> b.shift) * b.lde + col / E8_BLOCK] - E8_BIAS, v);
