@@ -323,7 +323,7 @@ __device__ __forceinline__ void team_stats(Team &team, const Cols<C> &k, float b
             if (var > 3.402823466e38f && out[q].f == 1.f) out[q].f = DOWN, again = true;
             out[q].rstd = rsqrtf(var + nm[q]->eps * out[q].f * out[q].f);
         }
-        if (again) continue;  // (the same for the whole team)
+        if (__builtin_amdgcn_readfirstlane(again)) continue;  // (the same for the whole team)
         if (!MEANS)
 #pragma unroll
             for (int q = 0; q < N; ++q) out[q].rstd *= out[q].f;
@@ -450,6 +450,12 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __lau
 #pragma unroll
                 for (int i = 0; i < 8 * C; ++i) u[i] = __builtin_fmaf(st[0].xh(u[i]), wa[i], ba[i]);
             }
+            // (the next row is taken as arrived here, before this one's stores, which the
+            // same counter counts: later the wait would be for them)
+            if (AHEAD) {
+                res.hold(), branch.hold();
+                if (gates) gnext.hold();
+            }
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 if (a.drop.threshold) {
@@ -474,6 +480,7 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __lau
             const float *x[1] = {s};
             Stat st[1];
             team_stats<true>(team, k, by, nm, x, st);
+            if (AHEAD && !BRANCH) res.hold();
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 float h[8];
@@ -742,6 +749,13 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
             const BackStat b{sb, m[0] * by, MEANS && a.before.kind == DBS_NORM_LAYER ? m[MEANS] * by : 0.f};
 #pragma unroll
             for (int i = 0; i < 8 * C; ++i) d[i] += dx_of<MEANS>(b, dh[i] * wb[i], xb[i]);
+        }
+        // (the next row is taken as arrived here, before this one's stores, which the
+        // same counter counts: later the wait would be for them)
+        if (AHEAD) {
+            if (a.ds) nds.hold();
+            if constexpr (BEFORE) ndh.hold(), nxs.hold();
+            if constexpr (BRANCH) nxu.hold();
         }
         if (a.dres)
 #pragma unroll
