@@ -149,8 +149,8 @@ __global__ __launch_bounds__(256, (Tile8<MT, H, NS>::PER_CU)) void k_mul8(Gemm8A
     // The workgroups of an XCD that run beside each other share their rows of P by four
     // (those of a group of tiles) and of Q by eight: each asks for its share of a later
     // step's lines once, so that the loads of all find them in L2.  What is read is not
-    // used.  (The large tile has two stages, one step of time for a load; 4096x4096 ->
-    // 11008 190 -> 183 us, 8192^3 469 -> 447 us.)
+    // used.  (The large tile has two stages, one step of time for a load: 4096x4096 ->
+    // 11008 190 -> 182 us, 8192^3 469 -> 436.  The others, with more, lose 2% by it.)
     constexpr bool ASK = NS == 2;
     __shared__ uint32_t asked[ASK ? 64 : 1];
     auto ask = [&](int step) {
@@ -341,7 +341,7 @@ template <class X, int MT, int H, int NS> static hipError_t launch_tile8(const L
 // Which tile: the one with the least time by the rule above.
 template <class X> static hipError_t mul8_t(const LayerWork &w, const Gemm8Args &b, hipStream_t s)
 {
-    constexpr double QUAD[4] = {7.0, 2.25, 2.53, 3.8};
+    constexpr double QUAD[4] = {6.75, 2.25, 2.53, 3.8};
     GemmArgs g = b.g;
     double cost[4];
     cost[0] = lay_out8<Tile8<8, 2, 2>>(w, g, QUAD[0]);
