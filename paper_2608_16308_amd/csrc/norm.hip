@@ -268,7 +268,9 @@ struct Team {
 // Statistics of one or two rows held eight columns a chunk, C chunks a lane.
 template <int C> struct Cols {
     int col[C], left[C];  // of a lane's chunks; left <= 0: behind the row
+    int at[C];            // where it reads: a row's last, partial chunk at the row's last eight columns
     bool full;            // all chunks of the wave have eight columns
+    bool narrow;          // the row has less than eight
 };
 // MEANS: some may be a layer norm; without, xh is x rstd (and f in rstd).
 template <bool MEANS> __device__ __forceinline__ float xh_of(const Stat &s, float x) { return MEANS ? s.xh(x) : x * s.rstd; }
@@ -363,22 +365,43 @@ template <int C> struct Share : Cols<C> {
         for (int i = 0; i < C; ++i) this->col[i] = 8 * (i * 64 * waves + at), this->left[i] = n - this->col[i];
         bool ragged = false;
 #pragma unroll
-        for (int i = 0; i < C; ++i) ragged |= this->left[i] < 8;
-        this->full = ballot(ragged) == 0;
+        for (int i = 0; i < C; ++i) this->at[i] = max(0, min(this->col[i], n - 8)), ragged |= this->left[i] < 8;
+        this->full = ballot(ragged) == 0, this->narrow = n < 8;
     }
 };
 typedef uint32_t v4u_t __attribute__((ext_vector_type(4)));
 template <class X, int C> struct Chunks {
     typename X::V8 v[C];
+    // A partial chunk comes as the row's last eight columns, in one load as the others:
+    // parts of 4, 2 and 1 are put together behind a wait of their own, which the whole
+    // team then meets at its next barrier (join backward of 4096x5119 in fp16 145 ->
+    // 116 us, x5004 139 -> 107, x5003 119 -> 112).  It is settled where the row is used.
     __device__ __forceinline__ void load(const void *base, int64_t ld, int64_t row, const Cols<C> &k)
     {
         const typename X::T *p = (const typename X::T *)base + row * ld;
-        if (k.full) {
 #pragma unroll
-            for (int i = 0; i < C; ++i) v[i] = load_eight<X>(at_col(p, k.col[i]));
-        } else
+        for (int i = 0; i < C; ++i) {
+            if (k.narrow) v[i] = get_eight<X>(p, k.left[i]);
+            else v[i] = load_eight<X>(at_col(p, k.at[i]));
+        }
+    }
+    // A partial chunk moved down to its place, zeros behind it.
+    __device__ __forceinline__ void settle(const Cols<C> &k)
+    {
+        if (k.full || k.narrow) return;
 #pragma unroll
-            for (int i = 0; i < C; ++i) v[i] = get_eight<X>(p + k.col[i], k.left[i]);
+        for (int i = 0; i < C; ++i) {
+            const v4u_t w = __builtin_bit_cast(v4u_t, v[i]);
+            uint32_t w0 = w[0], w1 = w[1], w2 = w[2], w3 = w[3];
+            const int by = 8 - max(0, min(8, k.left[i]));
+            if (by & 4) w0 = w2, w1 = w3, w2 = 0, w3 = 0;
+            if (by & 2) w0 = w1, w1 = w2, w2 = w3, w3 = 0;
+            const int bits = by & 1 ? 16 : 0;
+            w0 = __builtin_amdgcn_alignbit(w1, w0, bits), w1 = __builtin_amdgcn_alignbit(w2, w1, bits);
+            w2 = __builtin_amdgcn_alignbit(w3, w2, bits), w3 >>= bits;
+            const v4u_t z = {by == 8 ? 0 : w0, by == 8 ? 0 : w1, by == 8 ? 0 : w2, by == 8 ? 0 : w3};
+            v[i] = __builtin_bit_cast(typename X::V8, z);
+        }
     }
     __device__ __forceinline__ void vector(const void *p, const Cols<C> &k, float none)
     {
@@ -432,6 +455,11 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __lau
     if (AHEAD && k.row < a.rows) load(k.row);
     for (int row = k.row; row < a.rows; row += k.step) {
         if (!AHEAD) load(row);
+        res.settle(k);
+        if constexpr (BRANCH) {
+            branch.settle(k);
+            if (gates) gnext.settle(k);
+        }
         float s[8 * C], u[8 * C];
 #pragma unroll
         for (int i = 0; i < 8 * C; ++i) {
@@ -702,6 +730,7 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
     if (AHEAD && k.row < a.rows) load(k.row);
     for (int row = k.row; row < a.rows; row += k.step) {
         if (!AHEAD) load(row);
+        nds.settle(k), ndh.settle(k), nxs.settle(k), nxu.settle(k);
         const Chunks<X, C> dh = ndh;
         if constexpr (TEAM > 8 || C > 1) {
             if constexpr (BEFORE) wb.hold();
@@ -709,7 +738,7 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
             if constexpr (BRANCH) gate.hold();
         }
         if constexpr (BRANCH)
-            if (gates) gate.load(a.gate, a.ldg, row, k);
+            if (gates) gate.load(a.gate, a.ldg, row, k), gate.settle(k);
         float d[8 * C], xb[8 * C], u[8 * C];
         Stat sb{}, sa{};
 #pragma unroll
