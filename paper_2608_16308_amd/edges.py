@@ -14,6 +14,7 @@ from __future__ import annotations
 import collections
 import ctypes
 import math
+import operator
 
 from . import _lib
 from ._lib import check
@@ -69,7 +70,10 @@ def _drop_desc(torch, p, rng, device):
     if isinstance(rng, torch.Tensor):
         check_vector(rng, "rng", torch.int64, device, 2)
         return _lib.DropDesc(p, 0, 0, rng.data_ptr()), rng
-    seed, offset = (int(v) for v in rng)
+    try:
+        seed, offset = (operator.index(v) for v in rng)
+    except (TypeError, ValueError):
+        raise _arg_error(f"rng is {rng!r}, expected (seed, offset), or an int64 tensor of the two") from None
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise _arg_error("seed and offset are whole numbers of 64 bits, not negative")
     return _lib.DropDesc(p, seed, offset, None), None

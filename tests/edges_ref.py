@@ -31,15 +31,15 @@ def threshold(p):
     return int(np.floor(p * 65536 + 0.5))
 
 
-def factor(rows, n, p, rng):
-    """What dropout multiplies each element by."""
+def factor(rows, n, p, rng, first=0):
+    """What dropout multiplies each element by (of rows from `first` on)."""
     t = threshold(p)
     if t == 0:
         return torch.ones((rows, n), dtype=torch.float64)
     chunks = -(-n // 8)
     bits = np.zeros((rows, chunks * 8), np.int64)
     seed, offset = rng
-    c = np.arange(rows * chunks, dtype=np.uint64)
+    c = np.arange(first * chunks, (first + rows) * chunks, dtype=np.uint64)
     x = [c & np.uint64(MASK), c >> np.uint64(32), np.full_like(c, offset & MASK), np.full_like(c, offset >> 32)]
     k = [seed & MASK, seed >> 32]
     for _ in range(10):

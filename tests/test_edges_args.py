@@ -114,6 +114,8 @@ def test_dropout():
     passes(c.dropout, x[1], 1.0, (1, 2), y=x[1])
     rejects(c.dropout, x, 0.5, None)
     rejects(c.dropout, x, 2.0, (1, 2))
+    for rng in (5, (5,), (1, 2, 3), (1.5, 2), "ab", (1, -2), (1 << 64, 0), z(2), torch.zeros(3, dtype=torch.int64)):
+        rejects(c.dropout, x, 0.5, rng)
     rejects(c.dropout, x.float(), 0.5, (1, 2))
     buf = z(200)
     rejects(c.dropout, buf[:96].view(6, 16), 0.5, (1, 2), y=buf[8:104].view(6, 16))

@@ -337,3 +337,48 @@ def test_no_graph(ctx):
             out.float().sum().backward()
         assert word in str(e.value)
     assert not ctx.norm(x, nm).requires_grad
+
+
+def test_offsets_past_32_bits(ctx):
+    """Rows more than 2^31 elements apart: the same results as of rows beside each other."""
+    dt, (t, n) = torch.float16, (3, 1003)
+    g = gen(15)
+    far = (1 << 31) + 8
+    buf = torch.empty(2 * far + 8 * n, dtype=dt, device="cuda")
+    spread = [buf.as_strided((t, n), (far, 1), i * (n + 1)) for i in range(7)]
+    x = [rnd(g, (t, n), dt) for _ in range(5)]
+    for a, b in zip(spread, x):
+        a.copy_(b)
+    args = dict(after=make_norm(g, n, dt, "layer"), before=make_norm(g, n, dt, "rms"), p=0.2, rng=(7, 8))
+    s, h = ctx.join(x[0], x[1], gate=x[2], **args)
+    s2, h2 = ctx.join(spread[0], spread[1], gate=spread[2], stream=spread[5], **args)
+    assert torch.equal(s2, s) and torch.equal(h2, h)
+    d = ctx.join_backward(x[3], x[4], x[0], s, gate=x[2], **args)
+    d2 = ctx.join_backward(spread[3], spread[4], spread[0], s2, gate=spread[2], **args)
+    assert all(torch.equal(a, b) for a, b in zip(d, d2))
+    nm = args["before"]
+    assert torch.equal(ctx.norm(spread[0], nm, y=spread[6]), ctx.norm(x[0], nm))
+    assert torch.equal(ctx.dropout(spread[0], 0.3, (1, 2), y=spread[6]), ctx.dropout(x[0], 0.3, (1, 2)))
+    for a, b in zip(ctx.norm_backward(spread[3], spread[0], nm, add=spread[4]), ctx.norm_backward(x[3], x[0], nm, add=x[4])):
+        assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
+    long = 20000  # (and the rows that registers do not hold)
+    a = buf.as_strided((t, long), (far - long, 1), 0)
+    a.copy_(torch.randn((t, long), generator=g, device="cuda"))
+    nm = make_norm(g, long, dt, "layer")
+    b = a.contiguous()
+    assert torch.equal(ctx.norm(a, nm), ctx.norm(b, nm))
+    for u, v in zip(ctx.norm_backward(a, a, nm), ctx.norm_backward(b, b, nm)):
+        assert torch.equal(u, v)
+
+
+def test_more_than_32_bits_of_elements(ctx):
+    """The last rows of a matrix of more than 2^31 elements, where they are and alone."""
+    t, n = 70001, 31000
+    x = torch.zeros((t, n), dtype=torch.bfloat16, device="cuda")
+    last = x[-3:]
+    last.copy_(torch.randn((3, n), generator=gen(16), device="cuda"))
+    nm = Norm(None, None, kind="layer", eps=1e-5)
+    assert torch.equal(ctx.norm(x, nm)[-3:], ctx.norm(last, nm))
+    y = ctx.dropout(x, 0.25, (5, 6))[-3:]
+    want = last.cpu().double() * ref.factor(3, n, 0.25, (5, 6), first=t - 3)
+    check(y, (want, layer_ref.rounded(want, 2.0 ** -23 * want.abs(), torch.bfloat16)), "dropout")

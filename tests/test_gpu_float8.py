@@ -254,3 +254,86 @@ def test_no_graph(ctx):
     with pytest.raises(dbs.DbsError) as e:
         out.float().sum().backward()
     assert "linear8_backward" in str(e.value)
+
+
+def test_other_stream():
+    side = torch.cuda.Stream()
+    own, ctx = dbs.LayerContext(side), dbs.LayerContext()
+    g = gen(15)
+    x, dy = rnd(g, (70, 900), torch.float16), rnd(g, (70, 300), torch.float16)
+    w = rnd(g, (300, 900), torch.float16)
+
+    def step(c):
+        w8, x8 = c.pack8(w, block="tile"), c.pack8(x)
+        return [c.linear8(x8, w8), c.linear8(x, w8), c.linear8(x[:1], w8), *c.linear8_backward(dy, x8, w8, bias=True), c.unpack8(w8)]
+    want = step(ctx)
+    side.wait_stream(torch.cuda.current_stream())
+    got = step(own)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_weights_of_the_other_type(ctx):
+    """(a block's values are the same numbers in both)"""
+    g = gen(16)
+    w8 = ctx.pack8(rnd(g, (136, 260), torch.float16), block="tile")
+    other = Blocks8(w8.codes, w8.exponents, "tile", w8.shape, torch.bfloat16)
+    for t in (2, 150):
+        x, dy = rnd(g, (t, 260), torch.bfloat16), rnd(g, (t, 136), torch.bfloat16)
+        assert torch.equal(ctx.linear8(x, w8), ctx.linear8(x, other))
+        for a, b in zip(ctx.linear8_backward(dy, x, w8), ctx.linear8_backward(dy, x, other)):
+            assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
+
+
+def test_offsets_past_32_bits(ctx):
+    """Rows more than 2^31 elements apart: the same results as of rows beside each other."""
+    dt, (n, m) = torch.float16, (1003, 333)
+    g = gen(17)
+    w8 = ctx.pack8(rnd(g, (m, n), dt, n ** -0.5), block="tile")
+    far = (1 << 31) + 24
+    buf = torch.empty(2 * far + 8 * n, dtype=dt, device="cuda")
+    x, r, y = (buf.as_strided((3, k), (far, 1), i * (n + 1)) for i, k in enumerate((n, m, m)))
+    x.copy_(rnd(g, (3, n), dt)), r.copy_(rnd(g, (3, m), dt))
+    xc, rc = x.contiguous(), r.contiguous()
+    for across in (False, True):
+        a, b = ctx.pack8(x, across=across), ctx.pack8(xc, across=across)
+        assert torch.equal(a.codes.view(torch.uint8), b.codes.view(torch.uint8)) and torch.equal(a.exponents, b.exponents)
+    assert torch.equal(ctx.linear8(x, w8, residual=r, y=y), ctx.linear8(xc, w8, residual=rc))
+    assert torch.equal(ctx.unpack8(ctx.pack8(rc), y=y), ctx.unpack8(ctx.pack8(rc)))
+    for a, b in zip(ctx.linear8_backward(r, x, w8, bias=True), ctx.linear8_backward(rc, xc, w8, bias=True)):
+        assert torch.equal(a, b)
+    # many tokens, with codes of more than 2^31 bytes of each factor's side
+    t, n = 17000, 130000
+    x8 = ctx.pack8(torch.zeros((t, n), dtype=dt, device="cuda"))
+    last = rnd(g, (300, n), dt)
+    part = ctx.pack8(last)
+    x8.codes[-300:].view(torch.uint8).copy_(part.codes.view(torch.uint8))
+    x8.exponents[-300:].copy_(part.exponents)
+    w8 = ctx.pack8(rnd(g, (40, n), dt, n ** -0.5), block="tile")
+    y = ctx.linear8(x8, w8)
+    want, err = ref.product(ref.values(part), ref.values(w8), dt)
+    layer_ref.check(y[-300:].cpu(), want, err, "the last of many tokens")
+    assert float(y[:-300].float().abs().max()) == 0.0
+
+
+def test_captured_in_parts(ctx):
+    """A sum that several workgroups share, through the context's workspace, in a graph."""
+    side = torch.cuda.Stream()
+    own = dbs.LayerContext(side)
+    g = gen(18)
+    dt = torch.float16
+    x, w8 = rnd(g, (40, 9000), dt), ctx.pack8(rnd(g, (264, 9000), dt, 0.01), block="tile")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        own.linear8(x, w8)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = own.linear8(x, w8), own.linear8(x[:33], w8)
+    for i in range(3):
+        x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], ctx.linear8(x, w8)) and torch.equal(out[1], ctx.linear8(x[:33], w8)), i
+        torch.cuda.synchronize()
