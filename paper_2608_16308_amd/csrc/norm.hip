@@ -232,45 +232,73 @@ __device__ __forceinline__ float sum16(float v)
     v += ror(std::integral_constant<int, dppc::ROW_ROR + 8>{}, v);
     return v;
 }
-__device__ __forceinline__ float sum64(float v)
+struct Pair {
+    float a, b;
+};
+__device__ __forceinline__ Pair swap16(float x, float y)  // rows x0 y0 x2 y2 and x1 y1 x3 y3
 {
-    v = sum16(v);
-    const auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
-    const uint32_t a0 = a[0], a1 = a[1];  // rows 0 0 2 2 and 1 1 3 3
-    v = __builtin_bit_cast(float, a0) + __builtin_bit_cast(float, a1);
-    const auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
-    const uint32_t b0 = b[0], b1 = b[1];
-    return __builtin_bit_cast(float, b0) + __builtin_bit_cast(float, b1);
+    const auto v = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
+    const uint32_t a = v[0], b = v[1];
+    return {__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
 }
+__device__ __forceinline__ Pair swap32(float x, float y)  // rows x0 x1 y0 y1 and x2 x3 y2 y3
+{
+    const auto v = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
+    const uint32_t a = v[0], b = v[1];
+    return {__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+__device__ __forceinline__ float add(Pair v) { return v.a + v.b; }
 
 // A team: the waves that have a row, a workgroup or one of its waves.  Sums over
-// it, the same in all its lanes.
+// it, the same in all its lanes.  One or two values are folded into one register first
+// (two: the lower and the upper half of the lanes), so that both take the steps of
+// one (join backward of 4096x4096 with two layer norms in fp16 95 -> 91 us).
 constexpr int MAX_TEAM = 16;
 struct Team {
-    float (*red)[2][MAX_TEAM];  // [round][value][wave]
+    float (*red)[2][4][MAX_TEAM];  // [round][register][row of lanes][wave]
     int waves, round;
-    template <int N> __device__ __forceinline__ void sum(float (&v)[N])
+    template <int N> static __device__ __forceinline__ float fold(const float (&v)[N])
+    {
+        static_assert(N == 1 || N == 2, "");
+        const float s = add(swap32(v[0], v[N - 1]));
+        return sum16(add(swap16(s, s)));
+    }
+    template <int N> static __device__ __forceinline__ void unfold(float s, float (&v)[N])
     {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = sum64(v[i]);
-        if (waves == 1) return;
-        const int lane = lane_id(), of = lane & 15;
-        if (lane == 0)
+        for (int i = 0; i < N; ++i) v[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, s), 32 * i));
+    }
+    // Of R registers that are the same in a wave's rows of lanes, lane l gets those of
+    // wave l % 16 (zeros behind the last).
+    template <int R> __device__ __forceinline__ void spread(float (&s)[R])
+    {
+        const int lane = lane_id(), row = lane >> 4, of = lane & 15;
+        if (of == 0)
 #pragma unroll
-            for (int i = 0; i < N; ++i) red[round][i][wave_id()] = v[i];
+            for (int i = 0; i < R; ++i) red[round][i][row][wave_id()] = s[i];
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = sum16(of < waves ? red[round][i][of] : 0.f);
+        for (int i = 0; i < R; ++i) s[i] = of < waves ? red[round][i][row][of] : 0.f;
         round ^= 1;  // (one barrier each: the other round's values have been read by all when it is passed)
+    }
+    template <int N> __device__ __forceinline__ void sum(float (&v)[N])
+    {
+        float s[1] = {fold(v)};
+        if (waves > 1) spread(s), s[0] = sum16(s[0]);
+        unfold(s[0], v);
     }
 };
 
-// Statistics of one or two rows held eight columns a chunk, C chunks a lane.
+// Statistics of one or two rows held eight columns a chunk, C chunks a lane.  A layer
+// norm's take one barrier: each wave has the mean and squares of its own columns, and
+// those of all follow from these (the squares around the mean of all are each wave's
+// around its own and its columns times the squared distance of the two: Chan, Golub
+// and LeVeque, 1983).  The mean of all first, behind a barrier of its own: 98 us for 95.
 template <int C> struct Cols {
     int col[C], left[C];  // of a lane's chunks; left <= 0: behind the row
     int at[C];            // where it reads: a row's last, partial chunk at the row's last eight columns
     bool full;            // all chunks of the wave have eight columns
-    bool narrow;          // the row has less than eight
+    float mine, of;       // columns of the lane's wave, and of wave l % 16 of the team
 };
 // MEANS: some may be a layer norm; without, xh is x rstd (and f in rstd).
 template <bool MEANS> __device__ __forceinline__ float xh_of(const Stat &s, float x) { return MEANS ? s.xh(x) : x * s.rstd; }
@@ -283,28 +311,17 @@ __device__ __forceinline__ void team_stats(Team &team, const Cols<C> &k, float b
                                            Stat (&out)[N])
 {
     bool layer = false;
-    float v[N];
+    float m[N], v[N];  // means, squares around them
 #pragma unroll
-    for (int q = 0; q < N; ++q) layer |= MEANS && nm[q]->kind == DBS_NORM_LAYER, out[q] = Stat{1.f, 0.f, 0.f};
-    auto means = [&]() {
-#pragma unroll
-        for (int q = 0; q < N; ++q) {
-            v[q] = 0.f;
-            if (nm[q]->kind == DBS_NORM_LAYER)
-#pragma unroll
-                for (int i = 0; i < 8 * C; ++i) v[q] = __builtin_fmaf(x[q][i], by * out[q].f, v[q]);
-        }
-        team.sum(v);
-#pragma unroll
-        for (int q = 0; q < N; ++q) out[q].mean = v[q];
-    };
+    for (int q = 0; q < N; ++q) layer |= MEANS && nm[q]->kind == DBS_NORM_LAYER, out[q] = Stat{1.f, 0.f, 0.f}, m[q] = 0.f;
+    const float by_mine = MEANS ? 1.f / fmaxf(k.mine, 1.f) : 0.f;
     auto squares = [&](bool masked, bool plain) {
 #pragma unroll
         for (int q = 0; q < N; ++q) {
             v[q] = 0.f;
 #pragma unroll
             for (int i = 0; i < 8 * C; ++i) {
-                float d = plain ? x[q][i] : __builtin_fmaf(x[q][i], out[q].f, -out[q].mean);
+                float d = plain ? x[q][i] : __builtin_fmaf(x[q][i], out[q].f, -m[q]);
                 if (masked && (i & 7) >= k.left[i >> 3]) d = 0.f;
                 v[q] = __builtin_fmaf(d, d, v[q]);
             }
@@ -313,15 +330,39 @@ __device__ __forceinline__ void team_stats(Team &team, const Cols<C> &k, float b
     // (without means, zeros stand behind the row)
     const bool masked = layer && !k.full;
     for (bool first = true;; first = false) {
-        if (layer) means();
+        float s[2];  // the wave's own, which take no barrier
+        if (layer) {
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                m[q] = 0.f;
+                if (nm[q]->kind == DBS_NORM_LAYER)
+#pragma unroll
+                    for (int i = 0; i < 8 * C; ++i) m[q] = __builtin_fmaf(x[q][i], by_mine * out[q].f, m[q]);
+            }
+            s[1] = team.fold(m), team.unfold(s[1], m);
+        }
         if (masked) squares(true, false);
         else if (!MEANS && first) squares(false, true);
         else squares(false, false);
-        team.sum(v);
+        s[0] = team.fold(v);
+        if (team.waves > 1) {
+            if (layer) {
+                // the waves' together: the mean of all, and for each wave its distance from that
+                team.spread(s);
+                const float mean = sum16(s[1] * (k.of * by)), d = s[1] - mean;
+                s[0] = sum16(__builtin_fmaf(k.of * d, d, s[0])), s[1] = mean;
+                team.unfold(s[1], m);
+            } else {
+                float t[1] = {s[0]};
+                team.spread(t), s[0] = sum16(t[0]);
+            }
+        }
+        team.unfold(s[0], v);
         bool again = false;
 #pragma unroll
         for (int q = 0; q < N; ++q) {
             const float var = v[q] * by;
+            out[q].mean = m[q];
             if (var > 3.402823466e38f && out[q].f == 1.f) out[q].f = DOWN, again = true;
             out[q].rstd = rsqrtf(var + nm[q]->eps * out[q].f * out[q].f);
         }
@@ -365,8 +406,15 @@ template <int C> struct Share : Cols<C> {
         for (int i = 0; i < C; ++i) this->col[i] = 8 * (i * 64 * waves + at), this->left[i] = n - this->col[i];
         bool ragged = false;
 #pragma unroll
-        for (int i = 0; i < C; ++i) this->at[i] = max(0, min(this->col[i], n - 8)), ragged |= this->left[i] < 8;
-        this->full = ballot(ragged) == 0, this->narrow = n < 8;
+        for (int i = 0; i < C; ++i) this->at[i] = min(this->col[i], n - 8), ragged |= this->left[i] < 8;
+        this->full = ballot(ragged) == 0;
+        auto columns = [&](int wave) {
+            int all = 0;
+#pragma unroll
+            for (int i = 0; i < C; ++i) all += wave < waves ? min(512, max(0, n - 512 * (i * waves + wave))) : 0;
+            return (float)all;
+        };
+        this->mine = columns(waves == 1 ? 0 : wave_id()), this->of = columns(lane_id() & 15);
     }
 };
 typedef uint32_t v4u_t __attribute__((ext_vector_type(4)));
@@ -380,26 +428,23 @@ template <class X, int C> struct Chunks {
     {
         const typename X::T *p = (const typename X::T *)base + row * ld;
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-            if (k.narrow) v[i] = get_eight<X>(p, k.left[i]);
-            else v[i] = load_eight<X>(at_col(p, k.at[i]));
-        }
+        for (int i = 0; i < C; ++i) v[i] = load_eight<X>(at_col(p, k.at[i]));
     }
     // A partial chunk moved down to its place, zeros behind it.
     __device__ __forceinline__ void settle(const Cols<C> &k)
     {
-        if (k.full || k.narrow) return;
+        if (k.full) return;
+        auto pick = [](uint32_t mask, uint32_t there, uint32_t here) { return (there & mask) | (here & ~mask); };
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const v4u_t w = __builtin_bit_cast(v4u_t, v[i]);
             uint32_t w0 = w[0], w1 = w[1], w2 = w[2], w3 = w[3];
-            const int by = 8 - max(0, min(8, k.left[i]));
-            if (by & 4) w0 = w2, w1 = w3, w2 = 0, w3 = 0;
-            if (by & 2) w0 = w1, w1 = w2, w2 = w3, w3 = 0;
-            const int bits = by & 1 ? 16 : 0;
-            w0 = __builtin_amdgcn_alignbit(w1, w0, bits), w1 = __builtin_amdgcn_alignbit(w2, w1, bits);
-            w2 = __builtin_amdgcn_alignbit(w3, w2, bits), w3 >>= bits;
-            const v4u_t z = {by == 8 ? 0 : w0, by == 8 ? 0 : w1, by == 8 ? 0 : w2, by == 8 ? 0 : w3};
+            const uint32_t by = 8 - max(0, min(8, k.left[i])), by4 = 0u - (by >> 2 & 1), by2 = 0u - (by >> 1 & 1), some = 0u - (by < 8);
+            w0 = pick(by4, w2, w0), w1 = pick(by4, w3, w1), w2 &= ~by4, w3 &= ~by4;
+            w0 = pick(by2, w1, w0), w1 = pick(by2, w2, w1), w2 = pick(by2, w3, w2), w3 &= ~by2;
+            const uint32_t bits = 16 * (by & 1);
+            const v4u_t z = {__builtin_amdgcn_alignbit(w1, w0, bits) & some, __builtin_amdgcn_alignbit(w2, w1, bits) & some,
+                             __builtin_amdgcn_alignbit(w3, w2, bits) & some, w3 >> bits & some};
             v[i] = __builtin_bit_cast(typename X::V8, z);
         }
     }
@@ -427,7 +472,7 @@ template <class X, int C> struct Chunks {
 // for the rows) come from the caches each time.
 template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __launch_bounds__(64 * MAX_TEAM) void k_edge(EdgeArgs a, int waves)
 {
-    __shared__ float red[2][2][MAX_TEAM];
+    __shared__ float red[2][2][4][MAX_TEAM];
     Team team{red, waves, 0};
     const Share<C> k(a.n, waves);
     uint64_t seed, offset;
@@ -697,13 +742,28 @@ template <class X, bool BRANCH> __global__ __launch_bounds__(64 * STRIP_WAVES) v
     }
 }
 
+// The kernel's arguments (its first), read anew from here on: kept over the rows, the
+// many of them take more scalar registers than there are, and each use a lane's read
+// (join backward of 4096x5003 in fp16 109 -> 102 us).
+template <class A> using Args4 = const __attribute__((address_space(4))) A;
+template <class A> __device__ __forceinline__ Args4<A> *args_again()
+{
+    auto *p = (Args4<A> *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return p;
+}
+template <class N> __device__ __forceinline__ NormOf norm_of(N &n) { return NormOf{n.kind, n.eps, n.w, n.b}; }
+
 // The same for the gradients: a lane holds the sums over its team's rows of its
-// columns, the workgroups' are added afterwards.  Bound by the bytes and, where a
-// compute unit has one workgroup, by the four sums over a row one after the other.
+// columns, the workgroups' are added afterwards.  A norm alone is bound by the bytes
+// (8192x4096 in bf16: 53 us, 5.1 TB/s); a join by the vector ALUs: some 600 instructions
+// for a wave's 64 chunks, and a compute unit has registers for one team, whose waves
+// meet at three barriers a row (4096x4096 in fp16 with two layer norms, gate and
+// dropout: 88 us with the sums' end, where a copy of its bytes takes 42).
 template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool MEANS, int C, int TEAM>
 __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs a, int waves)
 {
-    __shared__ float red[2][2][MAX_TEAM], lanes[4][C * 512];
+    __shared__ float red[2][2][4][MAX_TEAM], lanes[4][C * 512];
     Team team{red, waves, 0};
     const Share<C> k(a.n, waves);
     uint64_t seed, offset;
@@ -721,6 +781,7 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
     float sum[BRANCH ? SUMS : 2][8 * C] = {};
     Chunks<X, C> nds{}, ndh, nxs, nxu{};
     auto load = [&](int row) {
+        const auto &a = *args_again<EdgeBackArgs>();
         if (a.ds) nds.load(a.ds, a.ldds, row, k);
         if constexpr (BEFORE) ndh.load(a.dh, a.lddh, row, k), nxs.load(a.stream, a.lds, row, k);
         if constexpr (BRANCH)
@@ -732,6 +793,7 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
         if (!AHEAD) load(row);
         nds.settle(k), ndh.settle(k), nxs.settle(k), nxu.settle(k);
         const Chunks<X, C> dh = ndh;
+        const auto &a = *args_again<EdgeBackArgs>();
         if constexpr (TEAM > 8 || C > 1) {
             if constexpr (BEFORE) wb.hold();
             if constexpr (AFTER) wa.hold(), ba.hold();
@@ -749,13 +811,13 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
         }
         if (AHEAD && row + k.step < a.rows) load(row + k.step);
         if constexpr (AFTER && BEFORE) {
-            const NormOf *nm[2] = {&a.before, &a.after};
+            const NormOf before = norm_of(a.before), after = norm_of(a.after), *nm[2] = {&before, &after};
             const float *x[2] = {xb, u};
             Stat st[2];
             team_stats<MEANS>(team, k, by, nm, x, st);
             sb = st[0], sa = st[1];
         } else if constexpr (AFTER || BEFORE) {
-            const NormOf *nm[1] = {BEFORE ? &a.before : &a.after};
+            const NormOf one = norm_of(BEFORE ? a.before : a.after), *nm[1] = {&one};
             const float *x[1] = {BEFORE ? xb : u};
             Stat st[1];
             team_stats<MEANS>(team, k, by, nm, x, st);
@@ -795,11 +857,12 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
                 put_chunk<X, C>(a.dres, a.lddr, row, k, c, v);
             }
         if constexpr (BRANCH) {
+            const auto &a = *args_again<EdgeBackArgs>();
             float m[MEANS ? 2 : 1] = {};
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 uint32_t kept = 255u;
-                if (a.drop.threshold) kept = kept_of(a.drop, seed, offset, row * chunks + k.col[c] / 8);
+                if (a.drop.threshold) kept = kept_of(a.drop.threshold, seed, offset, row * chunks + k.col[c] / 8);
                 const float by_kept = a.drop.threshold ? a.drop.scale : 1.f;
                 if constexpr (AFTER)
 #pragma unroll
@@ -931,7 +994,7 @@ static int team_rows(int waves) { return waves == 1 ? 4 : 1; }
 
 template <class X, bool BRANCH, bool AFTER, bool BEFORE> static hipError_t edge_t(const EdgeArgs &a, int32_t cus, hipStream_t s)
 {
-    if (a.n > 1024 * MAX_TEAM) {
+    if (a.n < 8 || a.n > 1024 * MAX_TEAM) {
         hipLaunchKernelGGL((k_edge_long<X, BRANCH>), dim3((unsigned)std::min(a.rows, 2 * cus)), dim3(64 * LONG_WAVES), 0, s, a);
         return hipGetLastError();
     }
@@ -963,9 +1026,9 @@ static int32_t strip_blocks(int32_t rows, int32_t n, int32_t cus)
     const int64_t strips = ((int64_t)n + STRIP - 1) / STRIP, want = strips ? (4 * (int64_t)cus + strips - 1) / strips : 1;
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ((int64_t)rows + STRIP_WAVES - 1) / STRIP_WAVES, 65535}));
 }
-// Rows of up to 8192 columns (a norm alone: 16384) are held in registers: one chunk a
+// Rows of 8 (a load) up to 8192 columns (a norm alone: 16384) are held in registers: one chunk a
 // lane, or, where 16 waves have no registers for the sums, two or four of eight waves.
-static bool back_fits(bool branch, int32_t n) { return n <= (branch ? 8192 : 16384); }
+static bool back_fits(bool branch, int32_t n) { return n >= 8 && n <= (branch ? 8192 : 16384); }
 static int back_chunks(bool branch, int32_t n) { return branch ? (n > 6144 ? 2 : 1) : n > 8192 ? 4 : 1; }
 // Workgroups: as many as run beside each other, each with a few rows, since its sums'
 // bytes are written and read again; but no compute unit is left without.

@@ -38,13 +38,13 @@ __device__ __forceinline__ uint4 philox(uint64_t lo, uint64_t hi, uint64_t key)
     return uint4{c0, c1, c2, c3};
 }
 // Which of the eight values of chunk `chunk` of a matrix stay, a bit each.
-__device__ __forceinline__ uint32_t kept_of(const Drop &d, uint64_t seed, uint64_t offset, uint64_t chunk)
+__device__ __forceinline__ uint32_t kept_of(uint32_t threshold, uint64_t seed, uint64_t offset, uint64_t chunk)
 {
     const uint4 w = philox(chunk, offset, seed);
     const uint32_t r[4] = {w.x, w.y, w.z, w.w};
     uint32_t bits = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) bits |= (uint32_t)((i & 1 ? r[i >> 1] >> 16 : r[i >> 1] & 0xFFFFu) >= d.threshold) << i;
+    for (int i = 0; i < 8; ++i) bits |= (uint32_t)((i & 1 ? r[i >> 1] >> 16 : r[i >> 1] & 0xFFFFu) >= threshold) << i;
     return bits;
 }
 // Multiplies or drops the eight values of a chunk.
