@@ -1,4 +1,5 @@
 // Products of matrices in blocks of 8-bit floating point on the matrix cores.
+#include <algorithm>
 #include <utility>
 
 #include "float8.hpp"
@@ -115,6 +116,11 @@ template <int MT, int H, int NS> struct Tile8 {
 //
 // Exponents come four steps at a time (a quad), a word for each row, through
 // registers into an order in LDS that gives a lane all of a step's in one read.
+//
+// Bound by the waits for lines that are not in L2 (with all of them there a fifth of the
+// time is gone; the matrix cores are busy 49% of it): 8192x8192->8192 in bf16 436 us,
+// 2520 TFLOP/s; 4096x11008->4096 142 (2600), 4096x4096->11008 177 (2090: 2.7 rounds of
+// tiles).
 template <class X, int MT, int H, int NS>
 __global__ __launch_bounds__(256, (Tile8<MT, H, NS>::PER_CU)) void k_mul8(Gemm8Args b)
 {
@@ -303,8 +309,9 @@ __global__ __launch_bounds__(256, (Tile8<MT, H, NS>::PER_CU)) void k_mul8(Gemm8A
 
 // The tiles of a call, how many of them are taken whole and in how many parts the
 // others; microseconds that this takes, a quad with all compute units at it taking
-// `quad`, and joining a launch and the bytes of the parts written and read.
-template <class C> static double lay_out8(const LayerWork &w, GemmArgs &a, double quad)
+// `quad` (`alone` with one tile on each), and joining a launch and the bytes of the
+// parts written and read.
+template <class C> static double lay_out8(const LayerWork &w, GemmArgs &a, double quad, double alone)
 {
     const int64_t tq = ((int64_t)a.qn + C::TQ - 1) / C::TQ, tp = ((int64_t)a.pn + C::TP - 1) / C::TP, ntile = tq * tp;
     if (ntile > MAX_TILES) return 1e30;
@@ -313,20 +320,21 @@ template <class C> static double lay_out8(const LayerWork &w, GemmArgs &a, doubl
     a.full = (int32_t)(ntile - rest), a.splits = 1;
     const double whole = (double)(ntile / slots) * (double)quads * quad;
     if (rest == 0) return whole;
-    double best = (double)quads * quad;
+    auto round = [&](int64_t parts) { return parts <= w.cus ? alone : quad; };
+    double best = (double)quads * round(rest);
     for (int64_t s = 2; s <= 16 && s <= quads; ++s) {
         const int64_t bytes = rest * s * C::TP * C::TQ * 4;
         if (bytes > (int64_t)w.part_bytes) break;
-        const double cost = (double)((rest * s + slots - 1) / slots) * (double)((quads + s - 1) / s) * quad + 4 + (double)bytes * 0.45e-6;
+        const double cost = (double)((rest * s + slots - 1) / slots) * (double)((quads + s - 1) / s) * round(rest * s) + 4 + (double)bytes * 0.45e-6;
         if (cost < best) best = cost, a.splits = (int32_t)s;
     }
     return whole + best;
 }
 
-template <class X, int MT, int H, int NS> static hipError_t launch_tile8(const LayerWork &w, Gemm8Args b, double quad, hipStream_t s)
+template <class X, int MT, int H, int NS> static hipError_t launch_tile8(const LayerWork &w, Gemm8Args b, double quad, double alone, hipStream_t s)
 {
     using C = Tile8<MT, H, NS>;
-    if (lay_out8<C>(w, b.g, quad) >= 1e30) return hipErrorInvalidConfiguration;
+    if (lay_out8<C>(w, b.g, quad, alone) >= 1e30) return hipErrorInvalidConfiguration;
     const int ntile = b.g.tp * b.g.tq;
     const hipError_t e = launch_parts(b.g.full + (int64_t)(ntile - b.g.full) * b.g.splits, C::NT, [&](int32_t first, dim3 grid) {
         b.g.first = first;
@@ -338,25 +346,30 @@ template <class X, int MT, int H, int NS> static hipError_t launch_tile8(const L
     return hipGetLastError();
 }
 
-// Which tile: the one with the least time by the rule above.
+// Which tile: the one with the least time by the rule above.  us with each tile forced
+// (256x256, 128x128, 128x256 and 64x128 of q and p), bf16, both factors in blocks:
+//   17x4096->4096         31.9    16.3    22.0    13.9
+//   256x4096->11008       35.4    23.0    28.3    23.6
+//   512x4096->4096        30.1    21.9    25.0    17.0
+//   777x11008->4096       59.2    47.4    51.1    57.7
+//   777x4096->11008       61.9    60.9    54.5    54.5
+//   1531x7001->5003       69.4    65.6    56.2    71.3
+//   2048x4096->11008     104.4   118.1   101.0   114.4
+//   4096x4096->4096       61.8    80.1    70.7    84.4
+//   4096x4096->11008     176.8   217.4   202.1   229.6
+// (a tile that has a compute unit for itself takes a quad in 1.65 us, two in 2.53: without
+// the difference 512x4096->4096 went to 128x128, 64x4096->11008 to fewer parts, 17.6 us for 15.3)
 template <class X> static hipError_t mul8_t(const LayerWork &w, const Gemm8Args &b, hipStream_t s)
 {
-    constexpr double QUAD[4] = {6.75, 2.25, 2.53, 3.8};
+    constexpr double BIG = 6.75, SQUARE = 2.25, FLAT = 3.8, SMALL = 2.53, SMALL_ALONE = 1.65;
     GemmArgs g = b.g;
-    double cost[4];
-    cost[0] = lay_out8<Tile8<8, 2, 2>>(w, g, QUAD[0]);
-    cost[1] = lay_out8<Tile8<4, 1, 4>>(w, g, QUAD[1]);
-    cost[2] = lay_out8<Tile8<2, 1, 3>>(w, g, QUAD[2]);
-    cost[3] = lay_out8<Tile8<4, 2, 3>>(w, g, QUAD[3]);
-    int tile = 0;
-    for (int i = 1; i < 4; ++i)
-        if (cost[i] < cost[tile]) tile = i;
-    switch (tile) {
-    case 0: return launch_tile8<X, 8, 2, 2>(w, b, QUAD[0], s);
-    case 1: return launch_tile8<X, 4, 1, 4>(w, b, QUAD[1], s);
-    case 2: return launch_tile8<X, 2, 1, 3>(w, b, QUAD[2], s);
-    default: return launch_tile8<X, 4, 2, 3>(w, b, QUAD[3], s);
-    }
+    const double big = lay_out8<Tile8<8, 2, 2>>(w, g, BIG, BIG), square = lay_out8<Tile8<4, 1, 4>>(w, g, SQUARE, SQUARE);
+    const double flat = lay_out8<Tile8<4, 2, 3>>(w, g, FLAT, FLAT), small = lay_out8<Tile8<2, 1, 3>>(w, g, SMALL, SMALL_ALONE);
+    const double least = std::min(std::min(big, square), std::min(flat, small));
+    if (least == big) return launch_tile8<X, 8, 2, 2>(w, b, BIG, BIG, s);
+    if (least == square) return launch_tile8<X, 4, 1, 4>(w, b, SQUARE, SQUARE, s);
+    if (least == flat) return launch_tile8<X, 4, 2, 3>(w, b, FLAT, FLAT, s);
+    return launch_tile8<X, 2, 1, 3>(w, b, SMALL, SMALL_ALONE, s);
 }
 
 hipError_t launch_mul8(const LayerWork &w, bool bf16, const Mul8Args &m, hipStream_t s)

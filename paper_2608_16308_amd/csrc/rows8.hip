@@ -11,7 +11,12 @@ typedef int v4i_t __attribute__((ext_vector_type(4)));
 
 constexpr int R8_U = 8;               // blocks that a wave has on their way
 constexpr int R8_WAVES = 8;
-constexpr int64_t R8_PACK = 128;      // blocks of x that a workgroup packs itself
+// Blocks of x that a workgroup packs itself, for each of its waves; above, a launch of
+// its own does it once for all.  In here and with the launch, bf16: 4096->11008 (four
+// waves), 1 token 11.2 and 15.1 us, 4 (32 a wave) 15.2 and 15.1, 8 21.1 and 16.8;
+// 14336->4096 (eight), 2 tokens (28) 16.9 and 17.2; 28672->8192 (28) 49.4 and 54.9;
+// 1024->4096 (one), 16 tokens (128) 19.5 and 14.1.
+constexpr int64_t R8_PACK = 32;
 
 struct Rows8Args {
     Mul8Args m;
@@ -24,7 +29,8 @@ struct Rows8Args {
 // A workgroup takes 16 rows of p, its waves share the blocks along k; their sums are
 // added in LDS, in their order.  x (RAW: 16-bit values) is brought into blocks in LDS
 // while the first weights are on their way: a launch of its own would take as long as
-// half of the product of one token.  Bound by the bytes of the weights.
+// half of the product of one token.  Bound by the bytes of the weights (1 token,
+// 4096->11008 in bf16: 11.2 us, 4.0 TB/s with the launch; 28672->8192 4.8 TB/s).
 template <class X, bool RAW> __global__ __launch_bounds__(64 * R8_WAVES) void k_rows8(Rows8Args a)
 {
     typedef typename X::T T;
@@ -100,15 +106,17 @@ template <class X, bool RAW> __global__ __launch_bounds__(64 * R8_WAVES) void k_
 
 static int64_t token_bytes(int64_t blocks) { return blocks * E8_BLOCK + 16; }
 
+static int64_t rows8_waves(int64_t blocks) { return std::max<int64_t>(1, std::min<int64_t>(R8_WAVES, (blocks + R8_U - 1) / R8_U)); }
 bool rows8_pack(int64_t tokens, int64_t cols)
 {
-    return tokens <= ROWS8_TOKENS && tokens * e8_blocks(cols) <= R8_PACK;
+    const int64_t blocks = e8_blocks(cols);
+    return tokens <= ROWS8_TOKENS && tokens * blocks <= R8_PACK * rows8_waves(blocks);
 }
 
 template <class X> static hipError_t rows8_t(Rows8Args a, hipStream_t s)
 {
     const int64_t groups = ((int64_t)a.m.pn + 15) / 16;
-    const int waves = (int)std::max<int64_t>(1, std::min<int64_t>(R8_WAVES, (a.blocks + R8_U - 1) / R8_U));
+    const int waves = (int)rows8_waves(a.blocks);
     const int64_t x = a.x ? a.m.qn * ((int64_t)a.ldl + a.blocks) : 0;
     const unsigned lds = (unsigned)std::max<int64_t>(x, waves * 1024);
     return launch_parts(groups, 64 * waves, [&](int32_t first, dim3 grid) {

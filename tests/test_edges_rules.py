@@ -23,10 +23,11 @@ def linear(t, n, m, x8=None):
 
 
 def test_few_tokens():
-    """Up to 16 tokens without tiles; up to 128 blocks of x packed on the way."""
+    """Up to 16 tokens without tiles; up to 32 blocks of x for each wave packed on the way."""
     fake_hip.run(CALLS + """
 size = ctypes.c_size_t()
-for t, n, alone in ((1, 4096, True), (4, 4096, True), (5, 4096, False), (16, 1024, True), (16, 1025, False), (1, 16384, True), (1, 16385, False)):
+for t, n, alone in ((1, 4096, True), (4, 4096, True), (5, 4096, False), (4, 1024, True), (5, 1024, False), (16, 1024, False), (2, 14336, True), (3, 14336, False),
+                    (1, 32768, True), (1, 32769, False)):
     got = linear(t, n, 512)[0]
     assert got == (["k_rows8"] if alone else ["k_pack8_rows", "k_rows8"]), (t, n, got)
     assert linear(t, n, 512, b8)[0] == ["k_rows8"]
@@ -42,7 +43,8 @@ def tile(t, n, m):
     return {re.search("k_mul8.*?(Li[0-9]+ELi[0-9]+ELi[0-9]+E)E", v).group(1) for v in names if "k_mul8" in v}.pop()
 big, square, flat, small = "Li8ELi2ELi2E", "Li4ELi1ELi4E", "Li4ELi2ELi3E", "Li2ELi1ELi3E"
 for t, n, m, want in ((4096, 4096, 11008, big), (4096, 11008, 4096, big), (8192, 8192, 8192, big), (1531, 7001, 5003, flat), (2048, 4096, 4096, flat),
-                      (1024, 11008, 4096, square), (777, 4096, 4096, square), (32, 4096, 11008, small), (320, 4096, 11008, small)):
+                      (1024, 11008, 4096, square), (777, 4096, 4096, square), (32, 4096, 11008, small), (320, 4096, 11008, small),
+                      (512, 4096, 4096, small)):
     assert tile(t, n, m) == want, (t, n, m, tile(t, n, m))
 """)
 
