@@ -516,7 +516,8 @@ dbs_status dbs_basic_spmspv(dbs_basic_matrix *B, dbs_path path, int32_t x_nnz, c
 /* A layer context holds the workspace of one stream, the one that it is created
  * for: calls on it run in stream order and are asynchronous; it is used by one
  * host thread at a time.  Calls allocate nothing and may be captured into a
- * graph, which needs the context as long as it is replayed.                  */
+ * graph, which needs the context as long as it is replayed; graphs captured on
+ * one context share its workspace and must not run at the same time.         */
 typedef struct dbs_layer dbs_layer;
 dbs_status dbs_layer_create(void *stream, dbs_layer **out);
 void dbs_layer_destroy(dbs_layer *L);

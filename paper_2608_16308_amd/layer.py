@@ -58,7 +58,9 @@ class LayerContext(EdgeOps, Float8Ops):
     A call is asynchronous on the context's stream.  Where that is not torch's
     current stream, outputs belong to the context's stream and inputs are
     marked as used there; the caller orders the two streams, as for any work
-    on a stream of its own.  One host thread at a time may use a context.
+    on a stream of its own.  One host thread at a time may use a context, and
+    graphs captured on one context share its workspace: they are not replayed
+    at the same time.
 
     No call builds an autograd graph: the gradients are those of the
     ``_backward`` calls, and a result that autograd follows back to one of the
