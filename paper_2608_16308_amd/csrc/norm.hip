@@ -756,6 +756,12 @@ template <class A> __device__ __forceinline__ Args4<A> *args_again()
 }
 template <class N> __device__ __forceinline__ NormOf norm_of(N &n) { return NormOf{n.kind, n.eps, n.w, n.b}; }
 
+// Waves of a SIMD whose registers the compiler is to fit.  With one norm at most two
+// teams of eight waves run on a compute unit (join backward with a layer norm after,
+// gate and dropout, 4096x4096 in bf16: 54 us; with one team's registers 62); those of
+// both norms do not fit into as few (196 for 89).
+constexpr int back_simd(int team, int chunks, bool both) { return team == 8 && chunks == 1 && !both ? 4 : team / 4; }
+
 // The same for the gradients: a lane holds the sums over its team's rows of its
 // columns, the workgroups' are added afterwards.  A norm alone is bound by the bytes
 // (8192x4096 in bf16: 53 us, 5.1 TB/s); a join by the vector ALUs: some 600 instructions
@@ -763,7 +769,7 @@ template <class N> __device__ __forceinline__ NormOf norm_of(N &n) { return Norm
 // meet at three barriers a row (4096x4096 in fp16 with two layer norms, gate and
 // dropout: 88 us with the sums' end, where a copy of its bytes takes 42).
 template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool MEANS, int C, int TEAM>
-__global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs a, int waves)
+__global__ __launch_bounds__(64 * TEAM, back_simd(TEAM, C, AFTER && BEFORE)) void k_edge_back(EdgeBackArgs a, int waves)
 {
     __shared__ float red[2][2][4][MAX_TEAM], lanes[4][C * 512];
     Team team{red, waves, 0};
@@ -796,7 +802,7 @@ __global__ __launch_bounds__(64 * TEAM, TEAM / 4) void k_edge_back(EdgeBackArgs 
         nds.settle(k), ndh.settle(k), nxs.settle(k), nxu.settle(k);
         const Chunks<X, C> dh = ndh;
         const auto &a = *args_again<EdgeBackArgs>();
-        if constexpr (TEAM > 8 || C > 1) {
+        if constexpr (TEAM > 8 || C > 1 || (BRANCH && !(AFTER && BEFORE))) {
             if constexpr (BEFORE) wb.hold();
             if constexpr (AFTER) wa.hold(), ba.hold();
             if constexpr (BRANCH) gate.hold();
@@ -1034,26 +1040,35 @@ static int32_t strip_blocks(int32_t rows, int32_t n, int32_t cus)
 // lane, or, where 16 waves have no registers for the sums, two or four of eight waves.
 static bool back_fits(bool branch, int32_t n) { return n >= 8 && n <= (branch ? 8192 : 16384); }
 static int back_chunks(bool branch, int32_t n) { return branch ? (n > 6144 ? 2 : 1) : n > 8192 ? 4 : 1; }
+// The most waves of a team that a kernel is made for: the fewer, the more registers
+// each.  With both norms a team of up to four waves gets the registers of three on a
+// SIMD, so that three run on a compute unit (2048x8192 in bf16 with two layer norms 84 ->
+// 72 us; teams of five and six, which have two waves on one SIMD, would run alone as they do).
+static int back_team(bool both, int waves, int chunks) { return chunks > 1 ? 8 : waves <= 8 && (!both || waves > 4) ? 8 : waves <= 12 ? 12 : 16; }
 // Workgroups: as many as run beside each other, each with a few rows, since its sums'
-// bytes are written and read again; but no compute unit is left without.
-static int32_t back_groups(bool branch, int32_t rows, int32_t n, int32_t cus)
+// bytes are written and read again; but no compute unit is left without.  (A workgroup's
+// waves go to the SIMDs in turn; one with five counts as one with eight.  More workgroups than
+// that: 2560x8192 128 us for 107; fewer: 1024x16384 88 for 75.)
+static int32_t back_groups(bool branch, bool both, int32_t rows, int32_t n, int32_t cus)
 {
-    const int waves = team_waves(n, back_chunks(branch, n)), each = team_rows(waves);
-    const int64_t teams = ((int64_t)rows + each - 1) / each, most = (int64_t)cus * std::max(1, 1024 / team_threads(waves));
-    return (int32_t)std::min(std::min(teams, most), std::max<int64_t>(cus, (teams + 7) / 8));
+    const int chunks = back_chunks(branch, n), waves = team_waves(n, chunks), each = team_rows(waves), team = back_team(both, waves, chunks);
+    const int simd = back_simd(team, chunks, both), beside = waves == 2 ? 2 * simd : simd / ((team_threads(waves) + 255) / 256);
+    const int64_t teams = ((int64_t)rows + each - 1) / each;
+    return (int32_t)std::min(std::min(teams, (int64_t)cus * std::max(1, beside)), std::max<int64_t>(cus, (teams + 7) / 8));
 }
-static int32_t sum_blocks(bool branch, int32_t rows, int32_t n, int32_t cus)
+static int32_t sum_blocks(bool branch, bool both, int32_t rows, int32_t n, int32_t cus)
 {
-    return back_fits(branch, n) ? back_groups(branch, rows, n, cus) : strip_blocks(rows, n, cus);
+    return back_fits(branch, n) ? back_groups(branch, both, rows, n, cus) : strip_blocks(rows, n, cus);
 }
-static size_t part_bytes(bool branch, int32_t rows, int32_t n, int sums, int32_t cus)
+static size_t part_bytes(bool branch, bool both, int32_t rows, int32_t n, int sums, int32_t cus)
 {
-    return ((size_t)sum_blocks(branch, rows, n, cus) * sums * n * 4 + 255) / 256 * 256;
+    return ((size_t)sum_blocks(branch, both, rows, n, cus) * sums * n * 4 + 255) / 256 * 256;
 }
 size_t edge_back_work(int32_t rows, int32_t n, int sums, int32_t cus)
 {
     if (n == 0) return 0;
-    return std::max(part_bytes(false, rows, n, sums, cus), part_bytes(true, rows, n, sums, cus)) + (back_fits(true, n) ? 0 : (size_t)rows * 2 * sizeof(BackStat));
+    const size_t part = std::max({part_bytes(false, false, rows, n, sums, cus), part_bytes(true, false, rows, n, sums, cus), part_bytes(true, true, rows, n, sums, cus)});
+    return part + (back_fits(true, n) ? 0 : (size_t)rows * 2 * sizeof(BackStat));
 }
 
 template <class X> static hipError_t total_t(TotalArgs t, hipStream_t s)
@@ -1066,12 +1081,11 @@ template <class X> static hipError_t total_t(TotalArgs t, hipStream_t s)
 }
 template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool MEANS> static void edge_back_m(const EdgeBackArgs &a, hipStream_t s)
 {
-    const int chunks = back_chunks(BRANCH, a.n), waves = team_waves(a.n, chunks);
+    const int chunks = back_chunks(BRANCH, a.n), waves = team_waves(a.n, chunks), team = back_team(AFTER && BEFORE, waves, chunks);
     const dim3 grid((unsigned)a.blocks), block((unsigned)team_threads(waves));
-    // (the fewer waves, the more registers each)
     if (chunks > 1) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, BRANCH ? 2 : 4, 8>), grid, block, 0, s, a, waves);
-    else if (waves <= 8) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 8>), grid, block, 0, s, a, waves);
-    else if (waves <= 12) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 12>), grid, block, 0, s, a, waves);
+    else if (team == 8) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 8>), grid, block, 0, s, a, waves);
+    else if (team == 12) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 12>), grid, block, 0, s, a, waves);
     else if constexpr (!BRANCH) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 16>), grid, block, 0, s, a, waves);
 }
 template <class X, bool BRANCH, bool AFTER, bool BEFORE> static hipError_t edge_back_t(const EdgeBackArgs &a, int32_t cus, hipStream_t s)
@@ -1113,10 +1127,11 @@ hipError_t launch_edge_back(bool bf16, EdgeBackArgs a, bool has_branch, void *wo
     if (a.n == 0) return hipSuccess;
     a.sums = 0;
     for (int q = 0; q < SUMS; ++q) a.at[q] = a.sum[q] ? a.sums++ : -1;
-    a.blocks = sum_blocks(has_branch, a.rows, a.n, cus);
-    a.part = (float *)work;
     const bool norms = a.before.kind != DBS_NORM_NONE || a.after.kind != DBS_NORM_NONE;
-    a.stat = norms && a.rows > 0 && !back_fits(has_branch, a.n) ? (BackStat *)((uint8_t *)work + part_bytes(has_branch, a.rows, a.n, a.sums, cus)) : nullptr;
+    const bool both = a.before.kind != DBS_NORM_NONE && a.after.kind != DBS_NORM_NONE;
+    a.blocks = sum_blocks(has_branch, both, a.rows, a.n, cus);
+    a.part = (float *)work;
+    a.stat = norms && a.rows > 0 && !back_fits(has_branch, a.n) ? (BackStat *)((uint8_t *)work + part_bytes(has_branch, both, a.rows, a.n, a.sums, cus)) : nullptr;
     return bf16 ? edge_back_x<Bf16>(a, has_branch, cus, s) : edge_back_x<Fp16>(a, has_branch, cus, s);
 }
 
