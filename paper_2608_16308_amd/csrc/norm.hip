@@ -1009,8 +1009,11 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE> static hipError_t edge_
         return hipGetLastError();
     }
     const int c = a.n <= 512 * MAX_TEAM ? 1 : 2, waves = team_waves(a.n, c), rows = team_rows(waves);
-    // (as many as fit beside each other: 2048 threads a compute unit)
-    const int64_t most = (int64_t)cus * (2048 / team_threads(waves));
+    // As many workgroups as run beside each other: four waves on a SIMD, of a norm alone
+    // six.  (With eight for all, rounded up to whole teams: join of 8192x4096 in bf16 with
+    // two layer norms 61 us for 59, 4096x5003 61 for 56; a norm of it 16.9 for 16.3, with
+    // four 19.5.)
+    const int64_t most = (int64_t)cus * std::max(1, (BRANCH ? 1024 : 1536) / team_threads(waves));
     const dim3 grid((unsigned)std::min<int64_t>(((int64_t)a.rows + rows - 1) / rows, most)), block((unsigned)team_threads(waves));
     if (c == 1) hipLaunchKernelGGL((k_edge<X, BRANCH, AFTER, BEFORE, 1>), grid, block, 0, s, a, waves);
     else hipLaunchKernelGGL((k_edge<X, BRANCH, AFTER, BEFORE, 2>), grid, block, 0, s, a, waves);
