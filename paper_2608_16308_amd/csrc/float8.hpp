@@ -88,12 +88,12 @@ template <class X> __device__ __forceinline__ float value16(uint32_t bits)
 template <class X> __device__ __forceinline__ int exp_of(uint32_t bits) { return e8_exp(value16<X>(bits)); }
 // 2^-e (a normal number: -127 <= e <= 120)
 __device__ __forceinline__ float down(int e) { return __builtin_bit_cast(float, (uint32_t)(127 - e) << 23); }
-// Four values as codes.  A value that is not finite becomes NaN: in `odd` chunks,
-// which hold one, by a choice of its own.
+// Four values as codes.  A value that is not finite becomes NaN (ODD: where one may be
+// among them).
 __device__ __forceinline__ float finite_or_nan(float v) { return __builtin_fabsf(v) <= 3.402823466e38f ? v : __builtin_nanf(""); }
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, bool odd)
+template <bool ODD> __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d)
 {
-    if (odd) a = finite_or_nan(a), b = finite_or_nan(b), c = finite_or_nan(c), d = finite_or_nan(d);
+    if (ODD) a = finite_or_nan(a), b = finite_or_nan(b), c = finite_or_nan(c), d = finite_or_nan(d);
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
     return (uint32_t)w;
@@ -102,20 +102,19 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, b
 struct Raw8 {
     uint32_t w[4];
 };
-template <class X> __device__ __forceinline__ bool magnitudes(const Raw8 &r, uint32_t (&m)[4])
+template <class X, bool ODD> __device__ __forceinline__ void magnitudes(const Raw8 &r, uint32_t (&m)[4])
 {
-    uint32_t all = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m[i] = r.w[i] & 0x7FFF7FFFu, all = max2(all, m[i]);
-    const bool odd = (both(all) & 0xFFFFu) >= Bits<X>::INF;
-    if (odd)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if ((m[i] & 0xFFFFu) >= Bits<X>::INF) m[i] &= 0xFFFF0000u;
-            if (m[i] >> 16 >= Bits<X>::INF) m[i] &= 0xFFFFu;
-        }
-    return odd;
+    for (int i = 0; i < 4; ++i) {
+        m[i] = r.w[i] & 0x7FFF7FFFu;
+        if (!ODD) continue;
+        if ((m[i] & 0xFFFFu) >= Bits<X>::INF) m[i] &= 0xFFFF0000u;
+        if (m[i] >> 16 >= Bits<X>::INF) m[i] &= 0xFFFFu;
+    }
 }
+__device__ __forceinline__ uint32_t most_of(const uint32_t (&m)[4]) { return max2(max2(m[0], m[1]), max2(m[2], m[3])); }
+// Whether a half of the word, a largest magnitude, is not finite, in any lane.
+template <class X> __device__ __forceinline__ bool any_odd(uint32_t m) { return ballot((both(m) & 0xFFFFu) >= Bits<X>::INF) != 0; }
 template <class X> __device__ __forceinline__ Raw8 load_raw(const typename X::T *p, int left)
 {
     if (left >= 8) return __builtin_bit_cast(Raw8, load_eight<X>(p));
@@ -125,13 +124,13 @@ template <class X> __device__ __forceinline__ Raw8 load_raw(const typename X::T 
     return __builtin_bit_cast(Raw8, v);
 }
 __device__ __forceinline__ uint32_t half_of(const Raw8 &r, int i) { return i & 1 ? r.w[i >> 1] >> 16 : r.w[i >> 1] & 0xFFFFu; }
-template <class X> __device__ __forceinline__ uint2 codes8(const Raw8 &r, float by, bool odd)
+template <class X, bool ODD> __device__ __forceinline__ uint2 codes8(const Raw8 &r, float by)
 {
     uint32_t w[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-        w[h] = codes4(value16<X>(half_of(r, 4 * h)) * by, value16<X>(half_of(r, 4 * h + 1)) * by, value16<X>(half_of(r, 4 * h + 2)) * by,
-                      value16<X>(half_of(r, 4 * h + 3)) * by, odd);
+        w[h] = codes4<ODD>(value16<X>(half_of(r, 4 * h)) * by, value16<X>(half_of(r, 4 * h + 1)) * by, value16<X>(half_of(r, 4 * h + 2)) * by,
+                           value16<X>(half_of(r, 4 * h + 3)) * by);
     return uint2{w[0], w[1]};
 }
 // Codes of a matrix: rows of whole blocks, zeros behind the last column.

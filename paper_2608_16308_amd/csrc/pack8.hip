@@ -1,5 +1,6 @@
 // 16-bit matrices into blocks of 8-bit floating point and back.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "float8.hpp"
@@ -15,7 +16,7 @@ __device__ __forceinline__ void pad_exps(const Blocks &b, int64_t row, int64_t b
 }
 
 // Row blocks alone: eight columns a lane, 16 lanes a block, P8_U chunks in flight.
-// Bound by the bytes (4096x4096 in bf16: 13.9 us, 3.6 TB/s).
+// Bound by the bytes (4096x4096 in bf16: 13.4 us, 3.8 TB/s).
 constexpr int P8_U = 4;
 template <class X> __global__ __launch_bounds__(P8_TPB) void k_pack8_rows(Pack8Args a)
 {
@@ -36,19 +37,33 @@ template <class X> __global__ __launch_bounds__(P8_TPB) void k_pack8_rows(Pack8A
             r[u] = Raw8{};
             if (c < all && col[u] < a.cols) r[u] = load_raw<X>((const T *)a.x + row[u] * a.ldx + col[u], a.cols - col[u]);
         }
+        uint32_t most[P8_U], any = 0;
 #pragma unroll
         for (int u = 0; u < P8_U; ++u) {
             uint32_t m[4];
-            const bool odd = magnitudes<X>(r[u], m);
-            const uint32_t most = both(max16(max2(max2(m[0], m[1]), max2(m[2], m[3])))) & 0xFFFFu;
-            if (c0 + u * stride >= all) continue;
-            const int e = exp_of<X>(most), block = col[u] / E8_BLOCK;
-            *(uint2 *)(a.to.codes + row[u] * a.to.ld + col[u]) = codes8<X>(r[u], down(e), odd);
-            if (col[u] % E8_BLOCK == 0) {
-                a.to.exps[row[u] * a.to.lde + block] = (uint8_t)(e + E8_BIAS);
-                if (block + 1 == per / 16) pad_exps(a.to, row[u], per / 16);
-            }
+            magnitudes<X, false>(r[u], m);
+            most[u] = most_of(m), any = max2(any, most[u]);
         }
+        auto put = [&](auto odd) {
+            constexpr bool ODD = decltype(odd)::value;
+#pragma unroll
+            for (int u = 0; u < P8_U; ++u) {
+                if (ODD) {
+                    uint32_t m[4];
+                    magnitudes<X, true>(r[u], m);
+                    most[u] = most_of(m);
+                }
+                const int e = exp_of<X>(both(max16(most[u])) & 0xFFFFu), block = col[u] / E8_BLOCK;
+                if (c0 + u * stride >= all) continue;
+                *(uint2 *)(a.to.codes + row[u] * a.to.ld + col[u]) = codes8<X, ODD>(r[u], down(e));
+                if (col[u] % E8_BLOCK == 0) {
+                    a.to.exps[row[u] * a.to.lde + block] = (uint8_t)(e + E8_BIAS);
+                    if (block + 1 == per / 16) pad_exps(a.to, row[u], per / 16);
+                }
+            }
+        };
+        if (any_odd<X>(any)) put(std::true_type{});
+        else put(std::false_type{});
     }
 }
 
@@ -60,20 +75,22 @@ __device__ __forceinline__ uint2 *unit_at(uint8_t *lines, int line, int u) { ret
 __device__ __forceinline__ void put_lines(uint8_t *lines, const Blocks &to, int tr, int tc, int32_t cols)
 {
     __syncthreads();
+    int line = (int)threadIdx.x >> 3;
+    const int u = 2 * ((int)threadIdx.x & 7), left = cols - tc * E8_BLOCK;
+    uint8_t *at = to.codes + ((int64_t)tc * E8_BLOCK + line) * to.ld + (int64_t)tr * E8_BLOCK + 8 * u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = i * P8_TPB + (int)threadIdx.x, line = c >> 3, u = 2 * (c & 7);
-        const int64_t col = (int64_t)tc * E8_BLOCK + line;
+    for (int i = 0; i < 4; ++i, line += P8_TPB / 8, at += P8_TPB / 8 * to.ld) {
         const uint2 lo = *unit_at(lines, line, u), hi = *unit_at(lines, line, u + 1);
-        if (col < cols) *(uint4 *)(to.codes + col * to.ld + (int64_t)tr * E8_BLOCK + 8 * u) = uint4{lo.x, lo.y, hi.x, hi.y};
+        if (line < left) *(uint4 *)at = uint4{lo.x, lo.y, hi.x, hi.y};
     }
 }
 
 // Everything else.  A workgroup takes a tile of 128 x 128, a thread 8 rows of 8
 // columns of it: the 16 lanes beside each other have a row's block, the 16 groups of
 // them a column's.  Turned codes change places in LDS, so that both results are
-// written in whole lines of 128 bytes.  Bound by the bytes (8192x4096 in bf16 across: 20.4
-// us, 4.9 TB/s; 4096x11008 both ways and its sums 48 us, 3.8 TB/s).
+// written in whole lines of 128 bytes.  Bound by the bytes (8192x4096 in bf16 across: 18.9
+// us, 5.3 TB/s; 4096x11008 both ways and its sums 46 us, 3.9 TB/s: bands of tiles below
+// each other, for longer runs of turned lines, do not change it).
 template <class X, bool CODES> __global__ __launch_bounds__(P8_TPB) void k_pack8(Pack8Args a)
 {
     typedef typename X::T T;
@@ -86,32 +103,40 @@ template <class X, bool CODES> __global__ __launch_bounds__(P8_TPB) void k_pack8
     const int row0 = tr * E8_BLOCK + 8 * rg, col0 = tc * E8_BLOCK + 8 * cc, left = a.cols - col0;
 
     Raw8 v[8];
+    const T *x = (const T *)a.x + (int64_t)row0 * a.ldx + col0;
+    const uint8_t *from = a.from.codes + (int64_t)row0 * a.from.ld + col0, *from_e = a.from.exps + (int64_t)row0 * a.from.lde + tc;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t row = row0 + i;
+    for (int i = 0; i < 8; ++i, x += a.ldx, from += a.from.ld, from_e += a.from.lde) {
         v[i] = Raw8{};
-        if (row >= a.rows || left <= 0) continue;
+        if (row0 + i >= a.rows || left <= 0) continue;
         if constexpr (CODES) {
             float f[8];
-            e8_values<X>(*(const uint2 *)(a.from.codes + row * a.from.ld + col0), (int)a.from.exps[row * a.from.lde + tc] - E8_BIAS, f);
+            e8_values<X>(*(const uint2 *)from, (int)*from_e - E8_BIAS, f);
             typename X::V8 t;
 #pragma unroll
             for (int j = 0; j < 8; ++j) t[j] = j < left ? (T)f[j] : (T)0.f;
             v[i] = __builtin_bit_cast(Raw8, t);
-        } else v[i] = load_raw<X>((const T *)a.x + row * a.ldx + col0, left);
+        } else v[i] = load_raw<X>(x, left);
     }
     // largest magnitudes: mr of the thread's rows, two to a word, mc of its columns
-    uint32_t mr[4] = {}, mc[4] = {};
-    bool odd = false;
+    uint32_t mr[4], mc[4];
+    auto sizes = [&](auto odd) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        uint32_t m[4];
-        odd |= magnitudes<X>(v[i], m);
+        for (int k = 0; k < 4; ++k) mr[k] = mc[k] = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mc[k] = max2(mc[k], m[k]);
-        const uint32_t r = both(max2(max2(m[0], m[1]), max2(m[2], m[3])));
-        mr[i >> 1] |= i & 1 ? r & 0xFFFF0000u : r & 0xFFFFu;
-    }
+        for (int i = 0; i < 8; ++i) {
+            uint32_t m[4];
+            magnitudes<X, decltype(odd)::value>(v[i], m);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mc[k] = max2(mc[k], m[k]);
+            const uint32_t r = both(most_of(m));
+            mr[i >> 1] |= i & 1 ? r & 0xFFFF0000u : r & 0xFFFFu;
+        }
+    };
+    sizes(std::false_type{});
+    // (a way of its own, for a wave that has one)
+    const bool odd = any_odd<X>(most_of(mc));
+    if (odd) sizes(std::true_type{});
     if (a.tile || a.turned.codes || a.sums) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -143,35 +168,44 @@ template <class X, bool CODES> __global__ __launch_bounds__(P8_TPB) void k_pack8
         const int c = (int)threadIdx.x, col = tc * E8_BLOCK + c;
         if (col < a.cols) a.sums[tr * (int64_t)a.cols + col] = sums[0][c] + sums[1][c] + sums[2][c] + sums[3][c];
     }
-    if (a.to.codes) {
+    auto put = [&](auto odd_t) {
+        uint8_t *to = a.to.codes + (int64_t)row0 * a.to.ld + col0, *exp = a.to.exps + (int64_t)(row0 >> a.to.shift) * a.to.lde + tc;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mr[k] = max16(mr[k]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t row = row0 + i;
+        for (int i = 0; i < 8; ++i, to += a.to.ld, exp += a.to.lde) {
             const int e = exp_of<X>(i & 1 ? mr[i >> 1] >> 16 : mr[i >> 1] & 0xFFFFu);
-            if (row >= a.rows) continue;
-            *(uint2 *)(a.to.codes + row * a.to.ld + col0) = codes8<X>(v[i], down(e), odd);
-            if (cc == 0 && (!a.tile || (rg == 0 && i == 0))) {
-                const int64_t at = row >> a.to.shift;
-                a.to.exps[at * a.to.lde + tc] = (uint8_t)(e + E8_BIAS);
-                if (tc == a.tiles_c - 1) pad_exps(a.to, at, a.tiles_c);
+            if (row0 + i >= a.rows) continue;
+            *(uint2 *)to = codes8<X, decltype(odd_t)::value>(v[i], down(e));
+            if (cc == 0 && (!a.tile || (rg == 0 && i == 0))) {  // (of a tile one, the first)
+                *exp = (uint8_t)(e + E8_BIAS);
+                if (tc == a.tiles_c - 1) pad_exps(a.to, (int64_t)(row0 + i) >> a.to.shift, a.tiles_c);
             }
         }
-    }
-    if (a.turned.codes) {
+    };
+    auto turn = [&](auto odd_t) {
+        constexpr bool ODD = decltype(odd_t)::value;
+        uint8_t *exp = a.turned.exps + (int64_t)(col0 >> a.turned.shift) * a.turned.lde + tr;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < 8; ++j, exp += a.turned.lde) {
             const int e = exp_of<X>(j & 1 ? mc[j >> 1] >> 16 : mc[j >> 1] & 0xFFFFu);
             const float by = down(e);
             auto at = [&](int i) { return value16<X>(half_of(v[i], j)) * by; };
-            *unit_at(lines, 8 * cc + j, rg) = uint2{codes4(at(0), at(1), at(2), at(3), odd), codes4(at(4), at(5), at(6), at(7), odd)};
+            *unit_at(lines, 8 * cc + j, rg) = uint2{codes4<ODD>(at(0), at(1), at(2), at(3)), codes4<ODD>(at(4), at(5), at(6), at(7))};
             if (rg == 0 && j < left && (!a.tile || (cc == 0 && j == 0))) {
-                const int64_t col = (int64_t)(col0 + j) >> a.turned.shift, blocks = e8_blocks(a.rows);
-                a.turned.exps[col * a.turned.lde + tr] = (uint8_t)(e + E8_BIAS);
-                if (tr == blocks - 1) pad_exps(a.turned, col, blocks);
+                const int64_t blocks = e8_blocks(a.rows);
+                *exp = (uint8_t)(e + E8_BIAS);
+                if (tr == blocks - 1) pad_exps(a.turned, (int64_t)(col0 + j) >> a.turned.shift, blocks);
             }
         }
+    };
+    if (a.to.codes) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mr[k] = max16(mr[k]);
+        if (odd) put(std::true_type{});
+        else put(std::false_type{});
+    }
+    if (a.turned.codes) {
+        if (odd) turn(std::true_type{});
+        else turn(std::false_type{});
         put_lines(lines, a.turned, tr, tc, a.cols);
     }
 }
@@ -217,11 +251,12 @@ __global__ __launch_bounds__(P8_TPB) void k_turn8(Blocks b, int32_t rows, int32_
     const int64_t tile = (int64_t)blockIdx.x + first;
     const int tr = (int)(tile / tiles_c), tc = (int)(tile % tiles_c), rg = (int)threadIdx.x >> 4, cc = (int)threadIdx.x & 15;
     uint32_t w[2][2][4];  // [upper four rows][left four columns][row]
+    const int row0 = tr * E8_BLOCK + 8 * rg;
+    const uint8_t *from = b.codes + (int64_t)row0 * b.ld + (int64_t)tc * E8_BLOCK + 8 * cc;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t row = (int64_t)tr * E8_BLOCK + 8 * rg + i;
+    for (int i = 0; i < 8; ++i, from += b.ld) {
         uint2 v = {0, 0};
-        if (row < rows) v = *(const uint2 *)(b.codes + row * b.ld + (int64_t)tc * E8_BLOCK + 8 * cc);
+        if (row0 + i < rows) v = *(const uint2 *)from;
         w[i >> 2][0][i & 3] = v.x, w[i >> 2][1][i & 3] = v.y;
     }
 #pragma unroll

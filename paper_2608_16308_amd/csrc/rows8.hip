@@ -64,10 +64,12 @@ template <class X, bool RAW> __global__ __launch_bounds__(64 * R8_WAVES) void k_
             Raw8 v{};
             if (row < t && col < m.kn) v = load_raw<X>((const T *)a.x + row * a.ldx + col, m.kn - col);
             uint32_t mag[4];
-            const bool odd = magnitudes<X>(v, mag);
-            const int e = exp_of<X>(both(max16(max2(max2(mag[0], mag[1]), max2(mag[2], mag[3])))) & 0xFFFFu);
+            magnitudes<X, false>(v, mag);
+            const bool odd = any_odd<X>(most_of(mag));
+            if (odd) magnitudes<X, true>(v, mag);
+            const int e = exp_of<X>(both(max16(most_of(mag))) & 0xFFFFu);
             if (row >= t) continue;
-            *(uint2 *)(xs + row * a.ldl + col) = codes8<X>(v, down(e), odd);
+            *(uint2 *)(xs + row * a.ldl + col) = odd ? codes8<X, true>(v, down(e)) : codes8<X, false>(v, down(e));
             if (r == 0) xe[row * a.blocks + b] = (uint8_t)(e + E8_BIAS);
         }
         __syncthreads();
