@@ -382,3 +382,43 @@ def test_more_than_32_bits_of_elements(ctx):
     y = ctx.dropout(x, 0.25, (5, 6))[-3:]
     want = last.cpu().double() * ref.factor(3, n, 0.25, (5, 6), first=t - 3)
     check(y, (want, layer_ref.rounded(want, 2.0 ** -23 * want.abs(), torch.bfloat16)), "dropout")
+
+
+# several rows one after the other for each team of waves, of each number of them
+@pytest.mark.parametrize("size", [(3001, 40), (1600, 905), (1100, 1501), (1100, 2048), (560, 2304), (530, 4090), (525, 5003), (300, 6151), (290, 8192),
+                                  (270, 9001), (270, 15000)], ids=str)
+def test_many_rows(ctx, size):
+    g = gen(size[1])
+    log(f"many rows {size}")
+    for dt, form in ((torch.bfloat16, FORMS[0]), (torch.float16, FORMS[1]), (torch.float16, FORMS[3]), (torch.bfloat16, FORMS[5])):
+        args = make_join(g, size, dt, form)
+        branch, residual, ds = rnd(g, size, dt, 2.0, 0.5), rnd(g, size, dt, 3.0), rnd(g, size, dt)
+        want = ref.join(branch, residual, **args)
+        stream, h = ctx.join(branch, residual, **args)
+        check(stream, want["stream"], f"{size} {form} stream")
+        dh = None
+        if h is not None:
+            check(h, want["h"], f"{size} {form} h")
+            dh = rnd(g, size, dt)
+        check_all(ctx.join_backward(ds, dh, branch, stream, **args), ref.join_backward(ds, dh, branch, stream, **args), f"{size} {form}")
+    for kind in ("rms", "layer"):
+        nm = make_norm(g, size[1], dt, kind)
+        check(ctx.norm(branch, nm), ref.norm(branch, nm), f"{size} {kind}")
+        for k, v in zip(("dx", "dweight", "dbias"), ctx.norm_backward(ds, branch, nm, add=residual)):
+            check(v, ref.norm_backward(ds, branch, nm, residual)[k], f"{size} {kind} {k}")
+
+
+@pytest.mark.parametrize("n", [200, 1111, 4096, 9000, 20000])
+def test_means_far_from_zero(ctx, n):
+    """Rows far from zero, and ones whose parts lie far apart."""
+    g = gen(17 + n)
+    size, dt = (5, n), torch.float16
+    far = rnd(g, size, dt, 1.0, 900.0)
+    parts = rnd(g, size, dt, 1.0) + (torch.arange(n, device="cuda") // 512 % 3 - 1) * 1000.0
+    for x in (far, parts.to(dt)):
+        nm, dy = make_norm(g, n, dt, "layer"), rnd(g, size, dt)
+        check(ctx.norm(x, nm), ref.norm(x, nm), f"{n}")
+        for k, v in zip(("dx", "dweight", "dbias"), ctx.norm_backward(dy, x, nm)):
+            check(v, ref.norm_backward(dy, x, nm)[k], f"{n} {k}")
+        args = dict(after=nm, before=nm, gate=None, scale=1.0, p=0.0, rng=None)
+        check_all(ctx.join_backward(dy, dy, x, x, **args), ref.join_backward(dy, dy, x, x, **args), f"{n} join")
