@@ -222,7 +222,7 @@ template <class X, bool BRANCH> __global__ __launch_bounds__(64 * LONG_WAVES) vo
 // ---------------------------------------------------------------------------
 // rows that a workgroup's registers hold
 // ---------------------------------------------------------------------------
-// The sum over a wave, in all its lanes.
+// The sum over 16 neighbouring lanes, in all of them.
 __device__ __forceinline__ float sum16(float v)
 {
     auto ror = [](auto ctrl, float x) { return __builtin_bit_cast(float, dpp_mov<decltype(ctrl)::value>(0u, __builtin_bit_cast(uint32_t, x))); };

@@ -54,6 +54,7 @@ def test_rows_in_registers():
 def fwd(n):
     return taken(lib.dbs_norm(L, 3, 9, n, p, n, norm(), p, n, None))[0]
 assert fwd(16384) == ["k_edge"] and fwd(16385) == ["k_edge_long"]
+assert fwd(8) == ["k_edge"] and fwd(7) == ["k_edge_long"]
 def back(n):
     return taken(lib.dbs_norm_backward(L, 3, 9, n, p, n, p, n, norm(2), None, n, p, n, p, p, p, room))[0]
 assert back(16384) == ["k_edge_back", "k_edge_total"] and back(16385) == ["k_edge_back_rows", "k_edge_back_strip", "k_edge_total"]
@@ -62,10 +63,25 @@ def jback(n):
 assert jback(8192) == ["k_edge_back", "k_edge_total"] and jback(8193) == ["k_edge_back_rows", "k_edge_back_strip", "k_edge_total"]
 # the workspace that is asked for is enough on both sides
 size = ctypes.c_size_t()
-for n in (500, 6144, 6145, 8192, 8193, 16384, 16385):
+for n in (7, 8, 500, 900, 2048, 2049, 6144, 6145, 8192, 8193, 16384, 16385):
     for rows in (1, 9, 100000):
         assert lib.dbs_edge_work(L, rows, n, 2, ctypes.byref(size)) == 0
         taken(lib.dbs_norm_backward(L, 3, rows, n, p, n, p, n, norm(2), None, n, p, n, p, p, p, size.value))
         assert lib.dbs_edge_work(L, rows, n, 5, ctypes.byref(size)) == 0
         taken(lib.dbs_join_backward(L, 3, rows, n, p, n, p, n, p, n, p, n, norm(), norm(), p, 0, 1.0, None, p, n, p, n, p, n, p, p, p, p, p, size.value))
+""")
+
+
+def test_teams_of_the_gradients():
+    """The waves that a join's gradients are compiled for, by the norms and the columns."""
+    fake_hip.run(CALLS + """
+def team(n, after, before):
+    a, b = norm() if after else None, norm() if before else None
+    names = taken(lib.dbs_join_backward(L, 3, 900, n, p, n, p if before else None, n, p, n, p, n, a, b, p, 0, 1.0, None, p, n, p, n, p, n,
+                                        p if after else None, p if after else None, p if before else None, p if before else None, p, room))[1]
+    return [tuple(map(int, re.search("k_edge_back.*?Li([0-9]+)ELi([0-9]+)E", v).groups())) for v in names if "k_edge_backI" in v][0]
+for n, want in ((500, (1, 12)), (2048, (1, 12)), (2049, (1, 8)), (4096, (1, 8)), (4097, (1, 12)), (6144, (1, 12)), (6145, (2, 8)), (8192, (2, 8))):
+    assert team(n, True, True) == want, (n, team(n, True, True))
+for n, want in ((500, (1, 8)), (4096, (1, 8)), (4097, (1, 12)), (6145, (2, 8))):
+    assert team(n, True, False) == want and team(n, False, True) == want, n
 """)
