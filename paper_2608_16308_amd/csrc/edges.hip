@@ -148,7 +148,9 @@ dbs_status dbs_join_backward(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t n
         CHECK(check_operand(fn, "dh", d_dh, rows, n, lddh));
         CHECK(check_operand(fn, "stream", d_stream, rows, n, lds));
     } else if (d_dh) return dbs_fail(DBS_ERR_ARG, "%s: dh without a norm", fn);
-    if (a.after.kind != DBS_NORM_NONE || d_gate) CHECK(check_operand(fn, "branch", d_branch, rows, n, ldb));
+    // (the kernels read a branch that they get: one that is not needed is neither checked nor handed on)
+    const bool reads_branch = a.after.kind != DBS_NORM_NONE || d_gate;
+    if (reads_branch) CHECK(check_operand(fn, "branch", d_branch, rows, n, ldb));
     if (d_dresidual) CHECK(check_operand(fn, "dresidual", d_dresidual, rows, n, lddr));
     if (d_dbranch) CHECK(check_operand(fn, "dbranch", d_dbranch, rows, n, lddb));
     if (d_dgate && !d_gate) return dbs_fail(DBS_ERR_ARG, "%s: dgate without a gate", fn);
@@ -165,7 +167,7 @@ dbs_status dbs_join_backward(dbs_layer *L, dbs_dtype dt, int32_t rows, int32_t n
     int sums = 0;
     for (void *v : a.sum) sums += v != nullptr;
     CHECK(check_room(fn, edge_back_work(rows, n, sums, L->w.cus), d_work, work_bytes));
-    a.ds = d_dstream, a.ldds = ldds, a.dh = d_dh, a.lddh = lddh, a.branch = d_branch, a.ldb = ldb, a.stream = d_stream, a.lds = lds;
+    a.ds = d_dstream, a.ldds = ldds, a.dh = d_dh, a.lddh = lddh, a.branch = reads_branch ? d_branch : nullptr, a.ldb = ldb, a.stream = d_stream, a.lds = lds;
     a.gate = d_gate, a.ldg = ldg, a.scale = scale, a.dres = d_dresidual, a.lddr = lddr, a.dbranch = d_dbranch, a.lddb = lddb;
     a.rows = rows, a.n = n;
     LAYER_TRY(launch_edge_back(dt == DBS_BF16, a, true, d_work, L->w.cus, L->stream), fn);

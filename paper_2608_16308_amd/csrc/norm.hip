@@ -772,7 +772,7 @@ constexpr int back_simd(int team, int chunks, bool both) { return team == 8 && c
 // The same for the gradients: a lane holds the sums over its team's rows of its
 // columns, the workgroups' are added afterwards.  A norm alone is bound by the bytes
 // (8192x4096 in bf16: 52 us, 5.2 TB/s), a join with an rms norm before nearly (4096x4096
-// in bf16: 42 us with the sums' end, a copy of as many bytes 35); one with both norms by the
+// in bf16: 37 us with the sums' end, a copy of as many bytes 35); one with both norms by the
 // vector ALUs, some 600 instructions for a wave's 64 chunks, and by the three barriers of
 // a row (4096x4096 in bf16 with layer norms 70 us, fp16 rows of 5003 92; a copy 42 and 51).
 template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool MEANS, int C, int TEAM>

@@ -180,6 +180,9 @@ static int nkernels;
 static __thread char launched[1 << 12];
 const char *fake_launched(void) { return launched; }
 void fake_forget(void) { launched[0] = 0; }
+/* the first fake_keep (at most 64) bytes of each launch's first argument, 16 launches */
+long fake_keep, fake_kept;
+uint64_t fake_first[16][8];
 err_t hipLaunchKernel(const void *f, dim_t g, dim_t b, void **args, size_t lds, void *s)
 {
     const size_t at = strlen(launched);
@@ -188,8 +191,8 @@ err_t hipLaunchKernel(const void *f, dim_t g, dim_t b, void **args, size_t lds, 
             strcpy(launched + at, kernels[i].name);
             strcat(launched, " ");
         }
-    (void)args;
     (void)s;
+    if (fake_keep && fake_kept < 16) memcpy(fake_first[fake_kept++], args[0], fake_keep);
     __sync_fetch_and_add(&fake_launches, 1);
     if ((unsigned long)g.x * b.x > fake_most_threads) fake_most_threads = (unsigned long)g.x * b.x;
     if (lds) last_grid = g.x;
