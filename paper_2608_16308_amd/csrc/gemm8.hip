@@ -41,12 +41,17 @@ __device__ __forceinline__ uint32_t lds_at(void *p) { return (uint32_t)(uintptr_
 // from `to` on.  Written as asm because the compiler, which sees such a load as a
 // write to all of LDS, waits for every one on its way before it reads anything
 // there; the kernel's own waits are counted instead.  (It returns no register, so
-// nothing can be taken for written too soon.  m0, the place, has no other use here.)
+// nothing can be taken for written too soon; m0, the place, is named as written, so that
+// no use of it by the compiler is taken to outlast this, and the warning that the
+// compiler reserves it says no more than that.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 template <int N> __device__ __forceinline__ void to_lds(const uint8_t *base, uint32_t off, uint32_t to)
 {
-    if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base));
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(off), "s"(base));
+    if constexpr (N == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "m0");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(off), "s"(base) : "m0");
 }
+#pragma clang diagnostic pop
 
 // f(0), f(1) .. f(N - 1) with the number known to the compiler.
 template <class F, int... I> __device__ __forceinline__ void each_of(F &&f, std::integer_sequence<int, I...>)
