@@ -139,12 +139,13 @@ class EdgeOps:
                                     n if given is None else ldy, None))
             return out
         out = self._call(body, (x, norm.weight, norm.bias, given))
-        if to8:
-            return out
         inputs = (x, norm.weight, norm.bias)
         if _wants(inputs):
-            out, = _no_graph(torch, "norm", inputs, (out,))
-        return out[0] if one else out
+            if to8:
+                out.codes, = _no_graph(torch, "norm", inputs, (out.codes,))
+            else:
+                out, = _no_graph(torch, "norm", inputs, (out,))
+        return out[0] if one and not to8 else out
 
     def _edge_work(self, rows, n, sums):
         size = ctypes.c_size_t()
@@ -225,7 +226,11 @@ class EdgeOps:
             return out, h8 if to8 else h
         out, h = self._call(body, (*inputs, rng_t, given))
         if _wants(inputs):
-            out, h = _no_graph(torch, "join", inputs, (out, h))
+            out, marked = _no_graph(torch, "join", inputs, (out, h.codes if to8 else h))
+            if to8:
+                h.codes = marked
+            else:
+                h = marked
         if one:
             out, h = out[0], h if to8 or h is None else h[0]
         return out, h

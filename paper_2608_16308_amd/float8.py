@@ -21,6 +21,7 @@ from .layer_args import (MAX_DIM, _arg_error, _check_apart, _choice, _dtype_code
 BLOCK8 = _lib.DBS_BLOCK8
 BLOCKS = {"row": 0, "tile": 1}
 MAX_SUM = 1 << 24  # elements of a product's sum
+BY = "the products' gradients are those of LayerContext.linear8_backward"
 
 
 def _up(n, by):
@@ -33,7 +34,8 @@ class Blocks8:
     ``exponents`` uint8, one for each block of 128 columns of a row (block
     "row") or of 128 rows ("tile"), rows of them in whole fours (both contiguous
     device tensors); a value is code * 2^(exponent - 127).  ``dtype`` is the type
-    of its values (float16 or bfloat16)."""
+    of its values (float16 or bfloat16).  Where it was made of a tensor that requires
+    a gradient, its codes do too: what autograd follows back to it raises."""
 
     __slots__ = ("codes", "exponents", "block", "shape", "dtype")
 
@@ -46,7 +48,7 @@ class Blocks8:
 
     @property
     def requires_grad(self):
-        return False
+        return self.codes.requires_grad
 
     def nbytes(self):
         return self.codes.numel() + self.exponents.numel()
@@ -110,7 +112,10 @@ class Float8Ops:
             out = self._new_blocks(*((cols, rows) if across else (rows, cols)), block, x.dtype)
             check(self._fn.dbs_pack8(self._h, dt, rows, cols, x.data_ptr(), ld, tile, 1 if across else 0, out._ref()))
             return out
-        return self._call(body, (x,))
+        out = self._call(body, (x,))
+        if x.requires_grad:
+            out.codes, = _no_graph(torch, "pack8", (x,), (out.codes,), BY)
+        return out
 
     def unpack8(self, c, y=None):
         """The values of a Blocks8 [rows, cols] in its type, limited to that type's
@@ -132,7 +137,10 @@ class Float8Ops:
             check(self._fn.dbs_unpack8(self._h, DBS_BF16 if c.dtype == torch.bfloat16 else DBS_F16, rows, cols, tile, c._ref(),
                                        out.data_ptr(), ld))
             return out
-        return self._call(body, (c, y))
+        out = self._call(body, (c, y))
+        if c.requires_grad:
+            out, = _no_graph(torch, "unpack8", (c.codes,), (out,), BY)
+        return out
 
     def linear8(self, x, w, bias=None, residual=None, y=None):
         """y = x w^T + bias + residual with both factors in 8 bits: w Blocks8 [n_out,
@@ -181,9 +189,9 @@ class Float8Ops:
                 out.data_ptr(), n_out if given is None else ldy, None if work is None else work.data_ptr(), size))
             return out
         out = self._call(body, (x, w, bias, residual, given))
-        if (not held and x.requires_grad) or bias is not None and bias.requires_grad or \
+        if x.requires_grad or w.requires_grad or bias is not None and bias.requires_grad or \
                 residual is not None and residual.requires_grad:
-            out, = _no_graph(torch, "linear8", (None if held else x, bias, residual), (out,))
+            out, = _no_graph(torch, "linear8", (x.codes if held else x, w.codes, bias, residual), (out,))
         return out[0] if one else out
 
     def linear8_backward(self, dy, x, w, bias=False, need_dx=True, need_dw=True):
