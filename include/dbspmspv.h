@@ -637,7 +637,8 @@ typedef struct {
 /* norm(x) = xh * weight + bias, by rows:  DBS_NORM_RMS xh = x / sqrt(mean(x^2) +
  * eps);  DBS_NORM_LAYER xh = (x - mean(x)) / sqrt(var(x) + eps), var the mean
  * square around the mean.  weight, bias: NULL stands for ones and zeros.  A NULL
- * descriptor or DBS_NORM_NONE: no norm.                                      */
+ * descriptor or DBS_NORM_NONE: no norm.  eps: at least 0; with 0 a row without
+ * spread is 0 / 0, NaN, and one however small keeps its bits.                */
 typedef enum { DBS_NORM_NONE = 0, DBS_NORM_RMS = 1, DBS_NORM_LAYER = 2 } dbs_norm_kind;
 typedef struct {
     dbs_norm_kind kind;

@@ -126,7 +126,18 @@ __device__ __forceinline__ void rng_of(const Drop &d, uint64_t &seed, uint64_t &
     offset = d.rng ? d.rng[1] : d.offset;
 }
 
-constexpr float DOWN = 8.271806125530277e-25f;  // 2^-80
+// What a row is multiplied by where its squares would leave the range of 32 bits (else
+// 1), from its variance and mean as it is.  Above 2^128 squares are infinite.  Below 2^-126 they
+// lose bits, which counts where variance and eps are below 2^-120: then all of x - mean is
+// below 2^-45 (in rows of 2^30), and a mean below 2^20 leaves x 2^100 in range.  (Beside a
+// larger mean numbers of 24 bits that differ at all have a larger variance.)
+constexpr float DOWN = 8.271806125530277e-25f, UP = 1.2676506002282294e30f;  // 2^-80, 2^100
+constexpr float LEAST_VAR = 7.5231638452626401e-37f;                          // 2^-120
+__device__ __forceinline__ float again_by(float var, float eps, float mean)
+{
+    if (var > 3.402823466e38f) return DOWN;
+    return var + eps < LEAST_VAR && __builtin_fabsf(mean) < 1048576.f ? UP : 1.f;
+}
 
 // The statistics of a row whose values `at(chunk, v)` gives: the mean first, then
 // the squares around it, so that a large mean costs no precision.
@@ -134,7 +145,7 @@ template <int WAVES, class F>
 __device__ __forceinline__ Stat row_stat(const NormOf &nm, int n, GroupSum<WAVES> &total, F &&at)
 {
     const float by = 1.f / (float)n;
-    for (float f = 1.f;; f = DOWN) {
+    for (float f = 1.f;;) {
         float mean = 0.f, var = 0.f;
         if (nm.kind == DBS_NORM_LAYER) {
             for (int c = (int)threadIdx.x; 8 * c < n; c += 64 * WAVES) {
@@ -155,8 +166,9 @@ __device__ __forceinline__ Stat row_stat(const NormOf &nm, int n, GroupSum<WAVES
             }
         }
         var = total(var) * by;
-        if (!(var > 3.402823466e38f) || f != 1.f)
-            return Stat{f, mean, rsqrtf(var + nm.eps * f * f)};
+        const float again = f == 1.f ? again_by(var, nm.eps, mean) : 1.f;
+        if (again == 1.f) return Stat{f, mean, rsqrtf(var + nm.eps * f * f)};
+        f = again;
     }
 }
 
@@ -300,13 +312,17 @@ template <int C> struct Cols {
     bool full;            // all chunks of the wave have eight columns
     float mine, of;       // columns of the lane's wave, and of wave l % 16 of the team
 };
-// MEANS: some may be a layer norm; without, xh is x rstd (and f in rstd).
+// MEANS: some may be a layer norm; without, xh is x rstd (and f in rstd).  TINY: some eps is
+// below LEAST_VAR, so that rows may have to be taken 2^100 fold: kernels of their own, since the
+// others would pay in registers (join backward of 8192x4096 in bf16 with two rms norms 110 us for
+// 99, two layer norms 122 for 115; norm backward with rms 50 for 50, of 4096x5003 42 for 38;
+// forward the same).  TINY is with MEANS.
 template <bool MEANS> __device__ __forceinline__ float xh_of(const Stat &s, float x) { return MEANS ? s.xh(x) : x * s.rstd; }
-template <bool MEANS> __device__ __forceinline__ float dx_of(const BackStat &b, float g, float xh)
+template <bool MEANS, bool TINY> __device__ __forceinline__ float dx_of(const BackStat &b, float g, float xh)
 {
-    return MEANS ? b.dx(g, xh) : __builtin_fmaf(-xh, b.m1, g) * b.s.rstd;
+    return TINY ? b.dx_any(g, xh) : MEANS ? b.dx(g, xh) : __builtin_fmaf(-xh, b.m1, g) * b.s.rstd;
 }
-template <bool MEANS, int N, int C>
+template <bool MEANS, bool TINY, int N, int C>
 __device__ __forceinline__ void team_stats(Team &team, const Cols<C> &k, float by, const NormOf *const (&nm)[N], const float *const (&x)[N],
                                            Stat (&out)[N])
 {
@@ -363,7 +379,9 @@ __device__ __forceinline__ void team_stats(Team &team, const Cols<C> &k, float b
         for (int q = 0; q < N; ++q) {
             const float var = v[q] * by;
             out[q].mean = m[q];
-            if (var > 3.402823466e38f && out[q].f == 1.f) out[q].f = DOWN, again = true;
+            if constexpr (TINY) {
+                if (out[q].f == 1.f) out[q].f = again_by(var, nm[q]->eps, m[q]), again |= out[q].f != 1.f;
+            } else if (var > 3.402823466e38f && out[q].f == 1.f) out[q].f = DOWN, again = true;
             out[q].rstd = rsqrtf(var + nm[q]->eps * out[q].f * out[q].f);
         }
         if (__builtin_amdgcn_readfirstlane(again)) continue;  // (the same for the whole team)
@@ -472,7 +490,8 @@ template <class X, int C> struct Chunks {
 // for the rows) come from the caches each time.  Bound by the bytes (join of 8192x4096
 // in bf16 between two norms, with dropout: 57 us, 4.7 TB/s); a row or a few by the
 // launch and one memory latency after the other (norm of 1x4096: 3.0 us).
-template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __launch_bounds__(64 * MAX_TEAM) void k_edge(EdgeArgs a, int waves)
+template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool TINY, int C>
+__global__ __launch_bounds__(64 * MAX_TEAM) void k_edge(EdgeArgs a, int waves)
 {
     __shared__ float red[2][2][4][MAX_TEAM];
     Team team{red, waves, 0};
@@ -525,7 +544,7 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __lau
                 const NormOf *nm[1] = {&a.after};
                 const float *x[1] = {u};
                 Stat st[1];
-                team_stats<true>(team, k, by, nm, x, st);
+                team_stats<true, TINY>(team, k, by, nm, x, st);
                 if (C > 1) vectors();
 #pragma unroll
                 for (int i = 0; i < 8 * C; ++i) u[i] = __builtin_fmaf(st[0].xh(u[i]), wa[i], ba[i]);
@@ -560,7 +579,7 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE, int C> __global__ __lau
             const NormOf *nm[1] = {&a.before};
             const float *x[1] = {s};
             Stat st[1];
-            team_stats<true>(team, k, by, nm, x, st);
+            team_stats<true, TINY>(team, k, by, nm, x, st);
             if (C > 1) vectors_before();
             if (AHEAD && !BRANCH) res.hold();
 #pragma unroll
@@ -602,7 +621,7 @@ __device__ __forceinline__ void back_before(const EdgeBackArgs &a, int64_t row, 
     for (int i = 0; i < 8; ++i) {
         k.xb[i] = b.s.xh(k.xb[i]);
         k.g[i] = k.dh[i] * (float)w[i];
-        if (means) k.d[i] += b.dx(k.g[i], k.xb[i]);
+        if (means) k.d[i] += b.dx_any(k.g[i], k.xb[i]);
     }
 }
 // The part from ds* to the gradient behind `after` (with `means` through it).
@@ -727,7 +746,7 @@ template <class X, bool BRANCH> __global__ __launch_bounds__(64 * STRIP_WAVES) v
                 if (a.after.kind != DBS_NORM_NONE) {
                     sum[SUM_AFTER_W][i] = __builtin_fmaf(v[i], k.ub[i], sum[SUM_AFTER_W][i]);
                     sum[SUM_AFTER_B][i] += v[i];
-                    v[i] = f.dx(v[i] * (float)wa[i], k.ub[i]);
+                    v[i] = f.dx_any(v[i] * (float)wa[i], k.ub[i]);
                 }
             }
             if (a.dbranch) put_eight<X>((T *)a.dbranch + row * a.lddb + col, left, v);
@@ -775,7 +794,7 @@ constexpr int back_simd(int team, int chunks, bool both) { return team == 8 && c
 // in bf16: 37 us with the sums' end, a copy of as many bytes 35); one with both norms by the
 // vector ALUs, some 600 instructions for a wave's 64 chunks, and by the three barriers of
 // a row (4096x4096 in bf16 with layer norms 70 us, fp16 rows of 5003 92; a copy 42 and 51).
-template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool MEANS, int C, int TEAM>
+template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool MEANS, bool TINY, int C, int TEAM>
 __global__ __launch_bounds__(64 * TEAM, back_simd(TEAM, C, AFTER && BEFORE)) void k_edge_back(EdgeBackArgs a, int waves)
 {
     __shared__ float red[2][2][4][MAX_TEAM], lanes[4][C * 512];
@@ -829,13 +848,13 @@ __global__ __launch_bounds__(64 * TEAM, back_simd(TEAM, C, AFTER && BEFORE)) voi
             const NormOf before = norm_of(a.before), after = norm_of(a.after), *nm[2] = {&before, &after};
             const float *x[2] = {xb, u};
             Stat st[2];
-            team_stats<MEANS>(team, k, by, nm, x, st);
+            team_stats<MEANS, TINY>(team, k, by, nm, x, st);
             sb = st[0], sa = st[1];
         } else if constexpr (AFTER || BEFORE) {
             const NormOf one = norm_of(BEFORE ? a.before : a.after), *nm[1] = {&one};
             const float *x[1] = {BEFORE ? xb : u};
             Stat st[1];
-            team_stats<MEANS>(team, k, by, nm, x, st);
+            team_stats<MEANS, TINY>(team, k, by, nm, x, st);
             (BEFORE ? sb : sa) = st[0];
         }
         if constexpr (BEFORE) {
@@ -854,7 +873,7 @@ __global__ __launch_bounds__(64 * TEAM, back_simd(TEAM, C, AFTER && BEFORE)) voi
             team.sum(m);
             const BackStat b{sb, m[0] * by, MEANS && a.before.kind == DBS_NORM_LAYER ? m[MEANS] * by : 0.f};
 #pragma unroll
-            for (int i = 0; i < 8 * C; ++i) d[i] += dx_of<MEANS>(b, dh[i] * wb[i], xb[i]);
+            for (int i = 0; i < 8 * C; ++i) d[i] += dx_of<MEANS, TINY>(b, dh[i] * wb[i], xb[i]);
         }
         // (the next row is taken as arrived here, before this one's stores, which the
         // same counter counts: later the wait would be for them)
@@ -921,7 +940,7 @@ __global__ __launch_bounds__(64 * TEAM, back_simd(TEAM, C, AFTER && BEFORE)) voi
                 team.sum(m);
                 const BackStat b{sa, m[0] * by, MEANS && a.after.kind == DBS_NORM_LAYER ? m[MEANS] * by : 0.f};
 #pragma unroll
-                for (int i = 0; i < 8 * C; ++i) d[i] = dx_of<MEANS>(b, d[i] * wa[i], u[i]);
+                for (int i = 0; i < 8 * C; ++i) d[i] = dx_of<MEANS, TINY>(b, d[i] * wa[i], u[i]);
             }
             if (a.dbranch)
 #pragma unroll
@@ -1009,7 +1028,13 @@ static int team_waves(int32_t n, int c) { return (int)(((int64_t)n + 512 * c - 1
 static int team_threads(int waves) { return 64 * (waves == 1 ? 4 : waves); }
 static int team_rows(int waves) { return waves == 1 ? 4 : 1; }
 
-template <class X, bool BRANCH, bool AFTER, bool BEFORE> static hipError_t edge_t(const EdgeArgs &a, int32_t cus, hipStream_t s)
+// Whether some norm's eps is below LEAST_VAR.
+static bool any_tiny(const NormOf &after, const NormOf &before)
+{
+    return (after.kind != DBS_NORM_NONE && after.eps < LEAST_VAR) || (before.kind != DBS_NORM_NONE && before.eps < LEAST_VAR);
+}
+
+template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool TINY> static hipError_t edge_t(const EdgeArgs &a, int32_t cus, hipStream_t s)
 {
     if (a.n < 8 || a.n > 1024 * MAX_TEAM) {
         hipLaunchKernelGGL((k_edge_long<X, BRANCH>), dim3((unsigned)std::min(a.rows, 2 * cus)), dim3(64 * LONG_WAVES), 0, s, a);
@@ -1022,16 +1047,20 @@ template <class X, bool BRANCH, bool AFTER, bool BEFORE> static hipError_t edge_
     // four 19.5.)
     const int64_t most = (int64_t)cus * std::max(1, (BRANCH ? 1024 : 1536) / team_threads(waves));
     const dim3 grid((unsigned)std::min<int64_t>(((int64_t)a.rows + rows - 1) / rows, most)), block((unsigned)team_threads(waves));
-    if (c == 1) hipLaunchKernelGGL((k_edge<X, BRANCH, AFTER, BEFORE, 1>), grid, block, 0, s, a, waves);
-    else hipLaunchKernelGGL((k_edge<X, BRANCH, AFTER, BEFORE, 2>), grid, block, 0, s, a, waves);
+    if (c == 1) hipLaunchKernelGGL((k_edge<X, BRANCH, AFTER, BEFORE, TINY, 1>), grid, block, 0, s, a, waves);
+    else hipLaunchKernelGGL((k_edge<X, BRANCH, AFTER, BEFORE, TINY, 2>), grid, block, 0, s, a, waves);
     return hipGetLastError();
+}
+template <class X, bool TINY> static hipError_t edge_n(const EdgeArgs &a, int32_t cus, hipStream_t s)
+{
+    const bool after = a.after.kind != DBS_NORM_NONE, before = a.before.kind != DBS_NORM_NONE;
+    if (!a.branch) return edge_t<X, false, false, true, TINY>(a, cus, s);
+    if (after) return before ? edge_t<X, true, true, true, TINY>(a, cus, s) : edge_t<X, true, true, false, TINY>(a, cus, s);
+    return before ? edge_t<X, true, false, true, TINY>(a, cus, s) : edge_t<X, true, false, false, false>(a, cus, s);
 }
 template <class X> static hipError_t edge_x(const EdgeArgs &a, int32_t cus, hipStream_t s)
 {
-    const bool after = a.after.kind != DBS_NORM_NONE, before = a.before.kind != DBS_NORM_NONE;
-    if (!a.branch) return edge_t<X, false, false, true>(a, cus, s);
-    if (after) return before ? edge_t<X, true, true, true>(a, cus, s) : edge_t<X, true, true, false>(a, cus, s);
-    return before ? edge_t<X, true, false, true>(a, cus, s) : edge_t<X, true, false, false>(a, cus, s);
+    return any_tiny(a.after, a.before) ? edge_n<X, true>(a, cus, s) : edge_n<X, false>(a, cus, s);
 }
 hipError_t launch_edge(bool bf16, const EdgeArgs &a, int32_t cus, hipStream_t s)
 {
@@ -1089,22 +1118,24 @@ template <class X> static hipError_t total_t(TotalArgs t, hipStream_t s)
         hipLaunchKernelGGL(k_edge_total<X>, grid, dim3(64 * TOTAL_WAVES), 0, s, t);
     });
 }
-template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool MEANS> static void edge_back_m(const EdgeBackArgs &a, hipStream_t s)
+template <class X, bool BRANCH, bool AFTER, bool BEFORE, bool MEANS, bool TINY> static void edge_back_m(const EdgeBackArgs &a, hipStream_t s)
 {
     const int chunks = back_chunks(BRANCH, a.n), waves = team_waves(a.n, chunks), team = back_team(AFTER && BEFORE, waves, chunks);
     const dim3 grid((unsigned)a.blocks), block((unsigned)team_threads(waves));
-    if (chunks > 1) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, BRANCH ? 2 : 4, 8>), grid, block, 0, s, a, waves);
-    else if (team == 8) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 8>), grid, block, 0, s, a, waves);
-    else if (team == 12) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 12>), grid, block, 0, s, a, waves);
-    else if constexpr (!BRANCH) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, 1, 16>), grid, block, 0, s, a, waves);
+    if (chunks > 1) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, TINY, BRANCH ? 2 : 4, 8>), grid, block, 0, s, a, waves);
+    else if (team == 8) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, TINY, 1, 8>), grid, block, 0, s, a, waves);
+    else if (team == 12) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, TINY, 1, 12>), grid, block, 0, s, a, waves);
+    else if constexpr (!BRANCH) hipLaunchKernelGGL((k_edge_back<X, BRANCH, AFTER, BEFORE, MEANS, TINY, 1, 16>), grid, block, 0, s, a, waves);
 }
 template <class X, bool BRANCH, bool AFTER, bool BEFORE> static hipError_t edge_back_t(const EdgeBackArgs &a, int32_t cus, hipStream_t s)
 {
     if (a.rows > 0 && back_fits(BRANCH, a.n)) {
         if constexpr (AFTER || BEFORE) {
-            if ((AFTER && a.after.kind == DBS_NORM_LAYER) || (BEFORE && a.before.kind == DBS_NORM_LAYER)) edge_back_m<X, BRANCH, AFTER, BEFORE, true>(a, s);
-            else edge_back_m<X, BRANCH, AFTER, BEFORE, false>(a, s);
-        } else edge_back_m<X, BRANCH, AFTER, BEFORE, false>(a, s);
+            if (any_tiny(a.after, a.before)) edge_back_m<X, BRANCH, AFTER, BEFORE, true, true>(a, s);
+            else if ((AFTER && a.after.kind == DBS_NORM_LAYER) || (BEFORE && a.before.kind == DBS_NORM_LAYER))
+                edge_back_m<X, BRANCH, AFTER, BEFORE, true, false>(a, s);
+            else edge_back_m<X, BRANCH, AFTER, BEFORE, false, false>(a, s);
+        } else edge_back_m<X, BRANCH, AFTER, BEFORE, false, false>(a, s);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     } else if (a.rows > 0) {

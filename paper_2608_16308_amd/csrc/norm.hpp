@@ -68,18 +68,23 @@ struct NormOf {
     const void *w, *b;  // NULL: ones, zeros
 };
 
-// xh = (x f - mean) rstd.  f is 1, or 2^-80 where the squares of a row would
-// leave the range of 32 bits.
+// xh = (x f - mean) rstd.  f is 1, or 2^-80 or 2^100 where the squares of a row would
+// leave the range of 32 bits above or below.
 struct Stat {
     float f, mean, rstd;
     __device__ __forceinline__ float xh(float x) const { return __builtin_fmaf(x, f, -mean) * rstd; }
 };
 // A row's norm and the two means that its gradient subtracts:
-// dx = rstd f (g - xh m1 - m2), m1 the mean of g xh, m2 (layer) that of g.
+// dx = rstd f (g - xh m1 - m2), m1 the mean of g xh, m2 (layer) that of g.  (With an f above
+// 1 rstd f may leave the range of 32 bits where dx does not.)
 struct BackStat {
     Stat s;
     float m1, m2;
     __device__ __forceinline__ float dx(float g, float xh) const { return (g - __builtin_fmaf(xh, m1, m2)) * (s.rstd * s.f); }
+    __device__ __forceinline__ float dx_any(float g, float xh) const
+    {
+        return (g - __builtin_fmaf(xh, m1, m2)) * (s.rstd * fminf(s.f, 1.f)) * fmaxf(s.f, 1.f);
+    }
 };
 
 // stream = scale * res + gate * drop(after(branch)); h = before(stream).
