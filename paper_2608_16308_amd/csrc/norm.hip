@@ -140,32 +140,39 @@ __device__ __forceinline__ float again_by(float var, float eps, float mean)
 }
 
 // The statistics of a row whose values `at(chunk, v)` gives: the mean first, then
-// the squares around it, so that a large mean costs no precision.
+// the squares around it, so that a large mean costs no precision.  Eight terms are added
+// in 32 bits and these sums in 64: one after the other in 32 bits a lane's 2^18 of a row of 2^28
+// equal numbers were off by 0.4%.
 template <int WAVES, class F>
 __device__ __forceinline__ Stat row_stat(const NormOf &nm, int n, GroupSum<WAVES> &total, F &&at)
 {
     const float by = 1.f / (float)n;
     for (float f = 1.f;;) {
-        float mean = 0.f, var = 0.f;
+        float mean = 0.f;
+        double sum = 0.0;
         if (nm.kind == DBS_NORM_LAYER) {
             for (int c = (int)threadIdx.x; 8 * c < n; c += 64 * WAVES) {
                 float v[8];
                 at(c, v);
+                float part = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) mean += 8 * c + i < n ? v[i] * f * by : 0.f;
+                for (int i = 0; i < 8; ++i) part += 8 * c + i < n ? v[i] * f * by : 0.f;
+                sum += part;
             }
-            mean = total(mean);
+            mean = total((float)sum), sum = 0.0;
         }
         for (int c = (int)threadIdx.x; 8 * c < n; c += 64 * WAVES) {
             float v[8];
             at(c, v);
+            float part = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float d = 8 * c + i < n ? __builtin_fmaf(v[i], f, -mean) : 0.f;
-                var = __builtin_fmaf(d, d, var);
+                part = __builtin_fmaf(d, d, part);
             }
+            sum += part;
         }
-        var = total(var) * by;
+        const float var = total((float)sum) * by;
         const float again = f == 1.f ? again_by(var, nm.eps, mean) : 1.f;
         if (again == 1.f) return Stat{f, mean, rsqrtf(var + nm.eps * f * f)};
         f = again;
@@ -658,35 +665,39 @@ template <class X, bool BRANCH> __global__ __launch_bounds__(64 * LONG_WAVES) vo
         if (a.before.kind != DBS_NORM_NONE) {
             const T *x = (const T *)a.stream + row * a.lds;
             b.s = row_stat(a.before, a.n, total, [&](int c, float(&v)[8]) { get_floats<X>(x + 8 * c, a.n - 8 * c, v); });
-            float m1 = 0.f, m2 = 0.f;
+            double m1 = 0.0, m2 = 0.0;  // (as in row_stat)
             for (int c = (int)threadIdx.x; 8 * c < a.n; c += 64 * LONG_WAVES) {
                 BackChunk<X, BRANCH> k;
                 back_before(a, row, 8 * c, a.n - 8 * c, b, false, k);
+                float s1 = 0.f, s2 = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (8 * c + i < a.n) m1 = __builtin_fmaf(k.g[i], k.xb[i], m1), m2 += k.g[i];
+                    if (8 * c + i < a.n) s1 = __builtin_fmaf(k.g[i], k.xb[i], s1), s2 += k.g[i];
+                m1 += s1, m2 += s2;
             }
-            b.m1 = total(m1) * by;
-            if (a.before.kind == DBS_NORM_LAYER) b.m2 = total(m2) * by;
+            b.m1 = total((float)m1) * by;
+            if (a.before.kind == DBS_NORM_LAYER) b.m2 = total((float)m2) * by;
         }
         if (BRANCH && a.after.kind != DBS_NORM_NONE) {
             const T *x = (const T *)a.branch + row * a.ldb;
             f.s = row_stat(a.after, a.n, total, [&](int c, float(&v)[8]) { get_floats<X>(x + 8 * c, a.n - 8 * c, v); });
-            float m1 = 0.f, m2 = 0.f;
+            double m1 = 0.0, m2 = 0.0;
             for (int c = (int)threadIdx.x; 8 * c < a.n; c += 64 * LONG_WAVES) {
                 BackChunk<X, BRANCH> k;
                 const int left = a.n - 8 * c;
                 back_before(a, row, 8 * c, left, b, true, k);
                 back_after(a, row, 8 * c, left, seed, offset, f, k);
                 const typename X::V8 w = get_vector<X>(a.after.w, 8 * c, left, 1.f);
+                float s1 = 0.f, s2 = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float g = k.du[i] * (float)w[i];
-                    if (i < left) m1 = __builtin_fmaf(g, k.ub[i], m1), m2 += g;
+                    if (i < left) s1 = __builtin_fmaf(g, k.ub[i], s1), s2 += g;
                 }
+                m1 += s1, m2 += s2;
             }
-            f.m1 = total(m1) * by;
-            if (a.after.kind == DBS_NORM_LAYER) f.m2 = total(m2) * by;
+            f.m1 = total((float)m1) * by;
+            if (a.after.kind == DBS_NORM_LAYER) f.m2 = total((float)m2) * by;
         }
         if (threadIdx.x == 0) a.stat[2 * (int64_t)row] = b, a.stat[2 * (int64_t)row + 1] = f;
     }
@@ -1068,12 +1079,16 @@ hipError_t launch_edge(bool bf16, const EdgeArgs &a, int32_t cus, hipStream_t s)
     return bf16 ? edge_x<Bf16>(a, cus, s) : edge_x<Fp16>(a, cus, s);
 }
 
+// The most rows that a lane adds up in a row: of 2^13 equal terms a sum in 32 bits may be off by
+// half a step of fp16 (2^16 of them: 0.1%).
+constexpr int64_t MOST_ROWS = 2048;
 // Workgroups along the rows: enough to fill the device, none with less than a row
 // for each wave.
 static int32_t strip_blocks(int32_t rows, int32_t n, int32_t cus)
 {
     const int64_t strips = ((int64_t)n + STRIP - 1) / STRIP, want = strips ? (4 * (int64_t)cus + strips - 1) / strips : 1;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, ((int64_t)rows + STRIP_WAVES - 1) / STRIP_WAVES, 65535}));
+    const int64_t least = ((int64_t)rows + STRIP_WAVES * MOST_ROWS - 1) / (STRIP_WAVES * MOST_ROWS);
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({std::max(want, least), ((int64_t)rows + STRIP_WAVES - 1) / STRIP_WAVES, 65535}));
 }
 // Rows of 8 (a load) up to 8192 columns (a norm alone: 16384) are held in registers: one chunk a
 // lane, or, where 16 waves have no registers for the sums, two or four of eight waves.
@@ -1093,7 +1108,8 @@ static int32_t back_groups(bool branch, bool both, int32_t rows, int32_t n, int3
     const int chunks = back_chunks(branch, n), waves = team_waves(n, chunks), each = team_rows(waves), team = back_team(both, waves, chunks);
     const int simd = back_simd(team, chunks, both), beside = waves == 2 ? 2 * simd : simd / ((team_threads(waves) + 255) / 256);
     const int64_t teams = ((int64_t)rows + each - 1) / each;
-    return (int32_t)std::min(std::min(teams, (int64_t)cus * std::max(1, beside)), std::max<int64_t>(cus, (teams + 7) / 8));
+    const int64_t groups = std::min(std::min(teams, (int64_t)cus * std::max(1, beside)), std::max<int64_t>(cus, (teams + 7) / 8));
+    return (int32_t)std::max(groups, (teams + MOST_ROWS - 1) / MOST_ROWS);
 }
 static int32_t sum_blocks(bool branch, bool both, int32_t rows, int32_t n, int32_t cus)
 {
