@@ -352,7 +352,9 @@ template <class X, int MT, int H, int NS> static hipError_t launch_tile8(const L
 }
 
 // Which tile: the one with the least time by the rule above.  us with each tile forced
-// (256x256, 128x128, 128x256 and 64x128 of q and p), bf16, both factors in blocks:
+// (256x256, 128x128, 128x256 and 64x128 of q and p), bf16, both factors in blocks, calls back to
+// back, so that the last-level cache has the factors (1531x7001->5003 in fp16 56 us so, 70
+// behind the packing of x in a call of its own; the rule has not been measured there):
 //   17x4096->4096         31.9    16.3    22.0    13.9
 //   256x4096->11008       35.4    23.0    28.3    23.6
 //   512x4096->4096        30.1    21.9    25.0    17.0

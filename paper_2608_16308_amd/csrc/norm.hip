@@ -704,7 +704,9 @@ template <class X, bool BRANCH> __global__ __launch_bounds__(64 * LONG_WAVES) vo
 }
 
 // Everything else: a workgroup has a strip of 512 columns and a range of rows,
-// a lane eight columns, whose sums it holds.
+// a lane eight columns, whose sums it holds.  Both kernels read a row again, from the caches at
+// best: join backward of 2048x14336 in bf16 with an rms norm before 128 us, with two layer
+// norms 257, a copy of the bytes of one reading 61 and 73.
 constexpr int STRIP = 512, STRIP_WAVES = 4;
 __host__ __device__ __forceinline__ int first_row(int64_t rows, int blocks, int block) { return (int)(rows * block / blocks); }
 
@@ -1096,13 +1098,13 @@ static bool back_fits(bool branch, int32_t n) { return n >= 8 && n <= (branch ? 
 static int back_chunks(bool branch, int32_t n) { return branch ? (n > 6144 ? 2 : 1) : n > 8192 ? 4 : 1; }
 // The most waves of a team that a kernel is made for: the fewer, the more registers
 // each.  With both norms a team of up to four waves gets the registers of three on a
-// SIMD, so that three run on a compute unit (2048x8192 in bf16 with two layer norms 84 ->
-// 72 us; teams of five and six, which have two waves on one SIMD, would run alone as they do).
+// SIMD, so that three run on a compute unit (8192x2048 in bf16 with two layer norms 84 ->
+// 71 us; teams of five and six, which have two waves on one SIMD, would run alone as they do).
 static int back_team(bool both, int waves, int chunks) { return chunks > 1 ? 8 : waves <= 8 && (!both || waves > 4) ? 8 : waves <= 12 ? 12 : 16; }
 // Workgroups: as many as run beside each other, each with a few rows, since its sums'
 // bytes are written and read again; but no compute unit is left without.  (A workgroup's
 // waves go to the SIMDs in turn; one with five counts as one with eight.  More workgroups than
-// that: 2560x8192 128 us for 107; fewer: 1024x16384 88 for 75.)
+// that: 8192x2560 128 us for 107; fewer: 16384x1024 88 for 75.)
 static int32_t back_groups(bool branch, bool both, int32_t rows, int32_t n, int32_t cus)
 {
     const int chunks = back_chunks(branch, n), waves = team_waves(n, chunks), each = team_rows(waves), team = back_team(both, waves, chunks);
