@@ -64,7 +64,8 @@ class LayerContext(EdgeOps, Float8Ops):
 
     No call builds an autograd graph: the gradients are those of the
     ``_backward`` calls, and a result that autograd follows back to one of the
-    forward calls raises."""
+    forward calls raises.  (A Checkpoint holds whole numbers, through which
+    autograd follows nothing.)"""
 
     def __init__(self, stream=None):
         import torch
